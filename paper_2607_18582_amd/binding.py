@@ -11,9 +11,12 @@ import ctypes as C
 import itertools
 import operator
 import os
+import weakref
 from typing import Dict, Optional, Sequence
 
 import numpy as np
+
+from . import seq as _seq
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmure.so")
@@ -149,6 +152,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         f = getattr(lib, name)
         f.restype = res
         f.argtypes = args
+    _seq.declare(lib)
     _lib = lib
     return lib
 
@@ -178,7 +182,7 @@ def layer_descriptors(nodes) -> "C.Array":
     return arr
 
 
-class Mure:
+class Mure(_seq.SeqOps):
     """One library context on a GPU (``device`` >= 0) or a planning-only
     context (``device`` = -1)."""
 
@@ -188,6 +192,8 @@ class Mure:
         if device >= 0 and stream is None:
             import torch
             stream = torch.cuda.current_stream(device).cuda_stream
+        self.stream = int(stream or 0)
+        self._batches = weakref.WeakSet()
         self.ctx = C.c_void_p()
         st = self.lib.mure_create(C.byref(self.ctx), device, C.c_void_p(stream or 0))
         if st != MURE_OK:
@@ -198,6 +204,7 @@ class Mure:
         self.classes = 0
 
     def close(self):
+        self._close_batches()
         if getattr(self, "ctx", None):
             self.lib.mure_destroy(self.ctx)
             self.ctx = None

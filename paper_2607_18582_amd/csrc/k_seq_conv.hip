@@ -1,0 +1,135 @@
+// Causal depthwise convolution along the sequences of a batch:
+//   y[t][c] = act(b[c] + sum_k w[c][k] x[t - K + 1 + k][c]).
+//
+// 2 K operations for 2 elements moved: bound by HBM.  A thread owns 16 bytes
+// of channels (8 bfloat16, 4 float32) of one run of consecutive tokens; the
+// last K - 1 rows stay in its registers, so that a row is read once, but for
+// the K - 1 rows before the run, which the run before reads too.  Rows are
+// loaded ROWS at a time, ahead of their use, to keep several loads in flight.
+// Widths that fill no whole vector: the last vector of a row starts early (its
+// first `dup` channels are the neighbour's and are not stored).
+#include <algorithm>
+
+#include "seq_dev.hpp"
+
+namespace mure {
+
+template <typename T, int K, int N>
+__global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dvec, uint32_t total) {
+  constexpr int ROWS = 4, H = K - 1;
+  const mure_seq_conv_args& a = k.a;
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x;
+  if (id >= total) return;
+  int item, v;
+  divmodu(dvec, id, item, v);
+  const SeqItem it = k.items[item];
+  const int64_t m = blockIdx.y;
+  const int C = a.channels;
+  int c = v * N, dup = 0;
+  if (c + N > C) dup = c + N - C, c = C - N;           // N == 1 where C < the vector
+  const T* x = static_cast<const T*>(a.x.p) + m * a.x.mutant_stride + (int64_t)it.row0 * a.x.row_stride + c;
+  T* y = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (int64_t)it.row0 * a.out.row_stride + c;
+  const int64_t held = (int64_t)it.seq * H * C + c;    // of this sequence's state
+  const T* st = a.state ? static_cast<const T*>(a.state) + m * a.state_mutant_stride + held : nullptr;
+
+  float w[K][N], b[N];
+  {
+    const T* wp = static_cast<const T*>(a.taps) + m * a.taps_mutant_stride + (int64_t)c * K;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {                      // K vectors hold the channels' K taps each
+      float t[N];
+      load_n<T, N>(wp + i * N, t);
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[(i * N + j) % K][(i * N + j) / K] = t[j];
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) b[j] = a.bias.p ? a.bias.p[m * a.bias.mutant_stride + c + j] : 0.f;
+  }
+  float r[H + ROWS][N];                                // rows t - H ... t + ROWS - 1
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const int pos = it.pos0 - H + i;
+    if (pos >= 0) load_n<T, N>(x - (int64_t)(H - i) * a.x.row_stride, r[i]);
+    else if (st) load_n<T, N>(st + (int64_t)(H + pos) * C, r[i]);
+    else
+#pragma unroll
+      for (int j = 0; j < N; ++j) r[i][j] = 0.f;
+  }
+  for (int t = 0; t < it.len; t += ROWS) {
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u)                     // rows past the run repeat its last one; they are not stored
+      load_n<T, N>(x + (int64_t)min(t + u, it.len - 1) * a.x.row_stride, r[H + u]);
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+      float s[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        s[j] = b[j];
+#pragma unroll
+        for (int i = 0; i < K; ++i) s[j] = fmaf(w[i][j], r[u + i][j], s[j]);
+        if (a.activation == MURE_SEQ_SILU) s[j] = seq_silu(s[j]);
+      }
+      if (t + u < it.len) store_from<T, N>(y + (int64_t)(t + u) * a.out.row_stride, s, dup);
+    }
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) r[i][j] = r[ROWS + i][j];
+  }
+  // The new state, by the sequence's first run: it has read the old one, which
+  // may lie in the same place.  Row j comes from position total - H + j: from
+  // the old state's row total + j, which is not before row j, or from x.
+  if (it.pos0 == 0 && a.state_out) {
+    T* so = static_cast<T*>(a.state_out) + m * a.state_out_mutant_stride + held;
+#pragma unroll
+    for (int j = 0; j < H; ++j) {
+      const int pos = it.total - H + j;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if (e < dup) continue;
+        T q = T(0);
+        if (pos >= 0) q = x[(int64_t)pos * a.x.row_stride + e];
+        else if (st) q = st[(int64_t)(H + pos) * C + e];
+        so[(int64_t)j * C + e] = q;
+      }
+    }
+  }
+}
+
+template <typename T, int K, int N>
+static hipError_t conv_n(SeqConvArgs k, hipStream_t s) {
+  const int vecs = (k.a.channels + N - 1) / N;
+  const int most = (1 << 30) / vecs;                   // items of a launch: its grid has fewer than 2^32 threads
+  for (int left = k.n_items; left > 0; left -= most, k.items += most) {
+    const uint32_t total = (uint32_t)std::min(left, most) * (uint32_t)vecs;
+    seq_conv_kernel<T, K, N><<<dim3((total + 255) / 256, (unsigned)k.a.n_mutants), 256, 0, s>>>(k, make_divu32((uint32_t)vecs), total);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename T, int K>
+static hipError_t conv_k(const SeqConvArgs& k, hipStream_t s) {
+  return k.a.channels >= Vec<T>::N ? conv_n<T, K, Vec<T>::N>(k, s) : conv_n<T, K, 1>(k, s);
+}
+
+template <typename T>
+static hipError_t conv_t(const SeqConvArgs& k, hipStream_t s) {
+  switch (k.a.n_taps) {
+    case 1: return conv_k<T, 1>(k, s);
+    case 2: return conv_k<T, 2>(k, s);
+    case 3: return conv_k<T, 3>(k, s);
+    case 4: return conv_k<T, 4>(k, s);
+    case 5: return conv_k<T, 5>(k, s);
+    case 6: return conv_k<T, 6>(k, s);
+    case 7: return conv_k<T, 7>(k, s);
+    case 8: return conv_k<T, 8>(k, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_seq_conv(const SeqConvArgs& k, hipStream_t s) {
+  return k.a.dtype == MURE_F32 ? conv_t<float>(k, s) : conv_t<bf16_t>(k, s);
+}
+
+}  // namespace mure

@@ -20,6 +20,7 @@
 #include "kernels.hpp"
 #include "plan.hpp"
 #include "run.hpp"
+#include "seq.hpp"
 
 using namespace mure;
 
@@ -169,6 +170,10 @@ struct mure_ctx {
     return e == hipErrorOutOfMemory ? MURE_E_NOMEM : MURE_E_DEVICE;
   }
 };
+
+namespace mure {
+CtxView ctx_view(mure_ctx* ctx) { return {ctx->plan_only ? -1 : ctx->device, ctx->stream, &ctx->err}; }
+}  // namespace mure
 
 #define HIPTRY(expr)                                  \
   do {                                                \

@@ -1,0 +1,68 @@
+// Device helpers of the sequence operators: vectors of elements at any
+// alignment, activations.
+#pragma once
+
+#include "dev.hpp"
+#include "seq.hpp"
+
+namespace mure {
+
+// 16 bytes of elements of T at the alignment of T: the GPU's global loads and
+// stores take any address (a vector that crosses a cache line costs both).
+template <typename T> struct Vec {
+  static constexpr int N = 16 / sizeof(T);
+  typedef T raw __attribute__((ext_vector_type(N)));
+  typedef raw __attribute__((aligned(sizeof(T)))) any;
+};
+
+// N elements at p (N = Vec<T>::N: one 16-byte load; N = 1: one element) as floats
+template <typename T, int N> __device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
+  if constexpr (N == 1) {
+    v[0] = to_f<T>(*p);
+  } else {
+    const typename Vec<T>::raw r = *reinterpret_cast<const typename Vec<T>::any*>(p);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = to_f<T>(r[j]);
+  }
+}
+
+template <typename T, int N> __device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
+  if constexpr (N == 1) {
+    *p = from_f<T>(v[0]);
+  } else if constexpr (sizeof(T) == 2) {
+    typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+    typedef words __attribute__((aligned(2))) any;
+    words r;
+#pragma unroll
+    for (int j = 0; j < N; j += 2) r[j / 2] = f2bf2(v[j], v[j + 1]);
+    *reinterpret_cast<any*>(p) = r;
+  } else {
+    typename Vec<T>::raw r;
+#pragma unroll
+    for (int j = 0; j < N; ++j) r[j] = v[j];
+    *reinterpret_cast<typename Vec<T>::any*>(p) = r;
+  }
+}
+
+// Elements first ... N - 1 of v only.
+template <typename T, int N> __device__ __forceinline__ void store_from(T* p, const float (&v)[N], int first) {
+  if (first == 0) {
+    store_n<T, N>(p, v);
+    return;
+  }
+#pragma unroll
+  for (int j = 1; j < N; ++j)
+    if (j >= first) p[j] = from_f<T>(v[j]);
+}
+
+// sigmoid(z) = 1 / (1 + e^-z) from the hardware exponential and reciprocal
+// (each within an ulp) with one Newton step on the reciprocal; the fix-up
+// gives 0 where the denominator is infinite, and keeps a NaN.
+__device__ __forceinline__ float seq_sigmoid(float z) {
+  const float d = 1.f + __expf(-z);
+  const float r = __builtin_amdgcn_rcpf(d);
+  return __builtin_amdgcn_div_fixupf(fmaf(fmaf(-d, r, 1.f), r, r), d, 1.f);
+}
+__device__ __forceinline__ float seq_silu(float z) { return z * seq_sigmoid(z); }
+
+}  // namespace mure

@@ -58,7 +58,7 @@ extern "C" {
 /* A sequence of more tokens than this is scanned in chunks that run side by
  * side (by its own length alone, so that its results do not depend on the
  * batch); 16 384 tokens are 128 chunks. */
-#define MURE_SEQ_SPLIT_TOKENS 1024
+#define MURE_SEQ_SPLIT_TOKENS 512
 
 /* A batch of sequences: their lengths and work lists, on the context's GPU. */
 typedef struct mure_seq mure_seq;

@@ -14,6 +14,27 @@
 
 namespace mure {
 
+// N elements copied as they are
+template <typename T, int N> struct Bits {
+  typedef T one __attribute__((ext_vector_type(N)));
+  typedef one __attribute__((aligned(sizeof(T)))) any;
+  static __device__ __forceinline__ one load(const T* p) { return *reinterpret_cast<const any*>(p); }
+  static __device__ __forceinline__ void store_from(T* p, one v, int first) {
+    if (first == 0) {
+      *reinterpret_cast<any*>(p) = v;
+      return;
+    }
+#pragma unroll
+    for (int j = 1; j < N; ++j)
+      if (j >= first) p[j] = v[j];
+  }
+};
+template <typename T> struct Bits<T, 1> {
+  typedef T one;
+  static __device__ __forceinline__ one load(const T* p) { return *p; }
+  static __device__ __forceinline__ void store_from(T* p, one v, int) { *p = v; }
+};
+
 template <typename T, int K, int N>
 __global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dvec, uint32_t total) {
   constexpr int ROWS = 4, H = K - 1;
@@ -22,7 +43,7 @@ __global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dve
   if (id >= total) return;
   int item, v;
   divmodu(dvec, id, item, v);
-  const SeqItem it = k.items[item];
+  const SeqItem it = seq_item(k.items, k.item0 + item);
   const int64_t m = blockIdx.y;
   const int C = a.channels;
   int c = v * N, dup = 0;
@@ -55,6 +76,19 @@ __global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dve
 #pragma unroll
       for (int j = 0; j < N; ++j) r[i][j] = 0.f;
   }
+  // The new state, by the sequence's first run: it has read the old one, which
+  // may lie in the same place.  Row j comes from position total - H + j: from
+  // the old state's row total + j, which is not before row j, or from x.
+  const bool carry = H > 0 && it.pos0 == 0 && a.state_out;
+  typename Bits<T, N>::one keep[H + 1];
+  if (carry)
+#pragma unroll
+    for (int j = 0; j < H; ++j) {
+      const int pos = it.total - H + j;
+      keep[j] = typename Bits<T, N>::one(0);
+      if (pos >= 0) keep[j] = Bits<T, N>::load(x + (int64_t)pos * a.x.row_stride);
+      else if (st) keep[j] = Bits<T, N>::load(st + (int64_t)(H + pos) * C);
+    }
   for (int t = 0; t < it.len; t += ROWS) {
 #pragma unroll
     for (int u = 0; u < ROWS; ++u)                     // rows past the run repeat its last one; they are not stored
@@ -76,23 +110,10 @@ __global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dve
 #pragma unroll
       for (int j = 0; j < N; ++j) r[i][j] = r[ROWS + i][j];
   }
-  // The new state, by the sequence's first run: it has read the old one, which
-  // may lie in the same place.  Row j comes from position total - H + j: from
-  // the old state's row total + j, which is not before row j, or from x.
-  if (it.pos0 == 0 && a.state_out) {
+  if (carry) {
     T* so = static_cast<T*>(a.state_out) + m * a.state_out_mutant_stride + held;
 #pragma unroll
-    for (int j = 0; j < H; ++j) {
-      const int pos = it.total - H + j;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        if (e < dup) continue;
-        T q = T(0);
-        if (pos >= 0) q = x[(int64_t)pos * a.x.row_stride + e];
-        else if (st) q = st[(int64_t)(H + pos) * C + e];
-        so[(int64_t)j * C + e] = q;
-      }
-    }
+    for (int j = 0; j < H; ++j) Bits<T, N>::store_from(so + (int64_t)j * C, keep[j], dup);
   }
 }
 
@@ -100,7 +121,7 @@ template <typename T, int K, int N>
 static hipError_t conv_n(SeqConvArgs k, hipStream_t s) {
   const int vecs = (k.a.channels + N - 1) / N;
   const int most = (1 << 30) / vecs;                   // items of a launch: its grid has fewer than 2^32 threads
-  for (int left = k.n_items; left > 0; left -= most, k.items += most) {
+  for (int left = k.n_items; left > 0; left -= most, k.item0 += most) {
     const uint32_t total = (uint32_t)std::min(left, most) * (uint32_t)vecs;
     seq_conv_kernel<T, K, N><<<dim3((total + 255) / 256, (unsigned)k.a.n_mutants), 256, 0, s>>>(k, make_divu32((uint32_t)vecs), total);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;

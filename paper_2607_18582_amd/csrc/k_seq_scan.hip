@@ -11,7 +11,9 @@
 // then steps through the four tokens, each lane broadcasting its token's D
 // and D u to the quad, and the partial sums over n go back to the token's
 // lane, which stores y.  b and c of TILE tokens stand in LDS as floats, shared
-// by the block; the next tile's loads are issued before a tile is computed.
+// by the block, twice: the next tile's loads (of all inputs) are issued before
+// a tile is computed.  Runs of fewer than four tokens read b and c from memory:
+// a single token needs neither LDS nor a barrier.
 //
 // A sequence of at most MURE_SEQ_SPLIT_TOKENS tokens is one run.  A longer
 // one is scanned in chunks: the scan is linear in h, so a chunk's last state
@@ -25,19 +27,19 @@
 
 namespace mure {
 
-constexpr int TILE = 32;                               // tokens whose b and c stand in LDS
+constexpr int TILE = 16;                               // tokens whose b and c stand in LDS
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // log(1 + e^s) = max(s, 0) + log1p(e^-|s|), and with e = e^-|s| and w = 1 + e
 // rounded, log1p(e) = log(w) e / (w - 1), or e where w = 1 (D. Goldberg, "What
 // every computer scientist should know about floating-point arithmetic", ACM
-// Computing Surveys 23 (1991), Theorem 4): the error in w cancels.
+// Computing Surveys 23 (1991), Theorem 4): the error in w cancels.  The
+// hardware's logarithm and reciprocal are within a unit or two.
 __device__ __forceinline__ float softplus(float s) {
-  const float e = __expf(-fabsf(s));
+  const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(s));
   const float w = 1.f + e, d = w - 1.f;
-  const float l = __builtin_amdgcn_logf(w) * (1.f / LOG2E);
-  const float p = d == 0.f ? e : l * (e / d);
-  return fmaxf(s, 0.f) + p;
+  const float p = __builtin_amdgcn_logf(w) * ((1.f / LOG2E) * e) * __builtin_amdgcn_rcpf(d);
+  return fmaxf(s, 0.f) + (d == 0.f ? e : p);
 }
 
 // Lane j's value of every quad, in all its lanes.
@@ -51,117 +53,215 @@ __device__ __forceinline__ float quad_xor2(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4e, 0xf, 0xf, true));
 }
 
-// Q: states per lane (4 Q in all); PAD: some of them are past N; ENDS: only
-// the state that the run reaches from zero.
-template <typename T, int Q, bool PAD, bool ENDS>
+// Q: states per lane (4 Q in all); PAD: some of them are past N.
+// KIND: RUNS; ENDS, only the state that a run reaches from zero; STEPS, runs of
+// fewer than four tokens all, which need no LDS and half the registers.
+enum { RUNS = 0, ENDS_ONLY = 1, STEPS = 2 };
+template <typename T, int Q, bool PAD, int KIND>
 __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb, DivU32 dm, DivU32 dtile) {
-  constexpr int NP = 4 * Q;
+  constexpr bool ENDS = KIND == ENDS_ONLY;
+  constexpr int NP = 4 * Q, GROUPS = TILE / 4;
+  constexpr int BC = TILE * NP * (ENDS ? 1 : 2), PER = (BC + 255) / 256;       // b and c of a tile; of a thread
   typedef float vq __attribute__((ext_vector_type(Q)));
-  __shared__ __attribute__((aligned(16))) float sb[TILE][NP];
-  __shared__ __attribute__((aligned(16))) float sc[ENDS ? 1 : TILE][NP];
+  typedef vq __attribute__((aligned(4))) vq_any;
+  __shared__ __attribute__((aligned(16))) float lds[2][KIND == STEPS ? 4 : BC];   // [b, c][TILE][NP]
   const mure_seq_scan_args& a = k.a;
-  const int tid = threadIdx.x, q = tid & 3, nthr = blockDim.x;
+  const int tid = threadIdx.x, q = tid & 3;
   int rest, cb, item, mi, group, tile;
   divmodu(dcb, blockIdx.x, rest, cb);                  // channel block fastest, then the mutant
   divmodu(dm, (uint32_t)rest, item, mi);
   divmodu(dtile, (uint32_t)cb, group, tile);
-  const SeqItem it = k.items[item];
+  const SeqItem it = seq_item(k.items, k.item0 + item);
   const int64_t m = mi;
   const int D = a.channels, N = a.states, width = D / a.groups;
   const int dg = tile * 64 + (tid >> 2);               // in the group
   const bool live = dg < width;
   const int d = group * width + min(dg, width - 1);
+  const int64_t su = a.u.row_stride, sd = a.dt.row_stride, sz = a.gate.row_stride, sy = a.out.row_stride;
+  const T* u = static_cast<const T*>(a.u.p) + m * a.u.mutant_stride + it.row0 * su + d;
+  const T* dt = static_cast<const T*>(a.dt.p) + m * a.dt.mutant_stride + it.row0 * sd + d;
+  const T* z = static_cast<const T*>(a.gate.p) + m * a.gate.mutant_stride + it.row0 * sz + d;
+  const T* b = static_cast<const T*>(a.b.p) + m * a.b.mutant_stride + it.row0 * a.b.row_stride + group * N;
+  const T* c = static_cast<const T*>(a.c.p) + m * a.c.mutant_stride + it.row0 * a.c.row_stride + group * N;
+  T* y = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * sy + d;
+  const bool gated = !ENDS && a.gate.p;
+
+  // A tile's inputs, as they come from memory: b and c; u, dt and gate of its whole groups of four tokens, and of
+  // the one to three tokens after them, where the run ends.
+  T bc[PER], ru[GROUPS + 1], rd[GROUPS + 1], rz[GROUPS + 1];
+  // Row t + lane_t of them, t the same in all lanes: kept opaque, or the compiler holds an address for every group
+  // of a tile in registers (156 of them for 16 states, and now 90).
+  auto fetch_row = [&](int t, int lane_t, T& fu, T& fd, T& fz) {
+    asm("" : "+s"(t));
+    fu = (u + t * su)[lane_t * su];
+    fd = (dt + t * sd)[lane_t * sd];
+    if (gated) fz = (z + t * sz)[lane_t * sz];
+  };
+  auto fetch_bc = [&](int t0, int count) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = tid + 256 * i, r = e / NP, n = e % NP;
+      const int64_t t = t0 + min(r % TILE, count - 1);  // rows past the run are not used
+      bc[i] = T(0);
+      if ((BC % 256 == 0 || e < BC) && (!PAD || n < N)) bc[i] = r < TILE ? b[t * a.b.row_stride + n] : c[t * a.c.row_stride + n];
+    }
+  };
+  auto fetch_group = [&](int t0, int count, int g) {   // g = GROUPS: the tokens after the whole groups
+    if (g < GROUPS && 4 * g + 4 <= count) fetch_row(t0 + 4 * g, q, ru[g], rd[g], rz[g]);
+    if (g == GROUPS && count % 4) fetch_row(t0 + count / 4 * 4, min(q, count % 4 - 1), ru[g], rd[g], rz[g]);
+  };
+  const bool tiled = KIND != STEPS && it.len >= 4;
+  if (tiled) {
+    const int count = min(TILE, it.len);
+    fetch_bc(0, count);
+#pragma unroll
+    for (int g = 0; g <= GROUPS; ++g) fetch_group(0, count, g);
+  } else if (it.len) {
+    fetch_row(0, min(q, it.len - 1), ru[GROUPS], rd[GROUPS], rz[GROUPS]);
+  }
 
   float al[Q], h[Q];                                   // a log2(e): exp(D a) is one hardware exp2
-  const float* ap = a.a.p + m * a.a.mutant_stride + (int64_t)d * N;
-  const int64_t state = ((int64_t)it.seq * D + d) * N;
+  const float* ap = a.a.p + m * a.a.mutant_stride + (int64_t)d * N + q * Q;
+  const int64_t state = ((int64_t)it.seq * D + d) * N + q * Q;
+  const int64_t slot = ((m * k.n_slots + it.slot) * D + d) * N + q * Q;
   const float* hp = nullptr;                           // the first state
   if (!ENDS) {
-    if (it.slot >= 0) hp = k.ws_h + ((m * k.n_slots + it.slot) * D + d) * N;
+    if (it.slot >= 0) hp = k.ws_h + slot;
     else if (a.state) hp = a.state + m * a.state_mutant_stride + state;
   }
+  if constexpr (PAD) {
 #pragma unroll
-  for (int i = 0; i < Q; ++i) {
-    const int n = q * Q + i;
-    const bool in = !PAD || n < N;
-    al[i] = in ? ap[n] * LOG2E : 0.f;
-    h[i] = in && hp ? hp[n] : 0.f;
+    for (int i = 0; i < Q; ++i) {
+      const bool in = q * Q + i < N;
+      al[i] = in ? ap[i] * LOG2E : 0.f;
+      h[i] = in && hp ? hp[i] : 0.f;
+    }
+  } else {
+    const vq av = *reinterpret_cast<const vq_any*>(ap);
+    vq hv = {};
+    if (hp) hv = *reinterpret_cast<const vq_any*>(hp);
+#pragma unroll
+    for (int i = 0; i < Q; ++i) al[i] = av[i] * LOG2E, h[i] = hv[i];
   }
   const float bias = a.dt_bias.p ? a.dt_bias.p[m * a.dt_bias.mutant_stride + d] : 0.f;
   const float skip = !ENDS && a.skip.p ? a.skip.p[m * a.skip.mutant_stride + d] : 0.f;
-  const T* u = static_cast<const T*>(a.u.p) + m * a.u.mutant_stride + (int64_t)it.row0 * a.u.row_stride + d;
-  const T* dt = static_cast<const T*>(a.dt.p) + m * a.dt.mutant_stride + (int64_t)it.row0 * a.dt.row_stride + d;
-  const T* z = !ENDS && a.gate.p ? static_cast<const T*>(a.gate.p) + m * a.gate.mutant_stride + (int64_t)it.row0 * a.gate.row_stride + d
-                                 : nullptr;
-  const T* b = static_cast<const T*>(a.b.p) + m * a.b.mutant_stride + (int64_t)it.row0 * a.b.row_stride + group * N;
-  const T* c = static_cast<const T*>(a.c.p) + m * a.c.mutant_stride + (int64_t)it.row0 * a.c.row_stride + group * N;
-  T* y = ENDS ? nullptr
-              : static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (int64_t)it.row0 * a.out.row_stride + d;
 
   float sum_d = 0.f;                                   // of this lane's tokens
-  for (int t0 = 0; t0 < it.len; t0 += TILE) {
-    const int count = min(TILE, it.len - t0);
-    __syncthreads();                                   // the last tile is read
-    for (int e = tid; e < TILE * NP; e += nthr) {
-      const int t = e / NP, n = e % NP;
-      const bool in = t < count && (!PAD || n < N);
-      sb[t][n] = in ? to_f<T>(b[(int64_t)(t0 + t) * a.b.row_stride + n]) : 0.f;
-      if (!ENDS) sc[t][n] = in ? to_f<T>(c[(int64_t)(t0 + t) * a.c.row_stride + n]) : 0.f;
-    }
-    __syncthreads();
-    for (int tq = 0; tq < count; tq += 4) {
-      const int left = count - tq, t = t0 + tq + min(q, left - 1);     // past the run: its last token again
-      const float uv = to_f<T>(u[(int64_t)t * a.u.row_stride]);
-      float dv = to_f<T>(dt[(int64_t)t * a.dt.row_stride]) + bias;
-      const float zv = z ? to_f<T>(z[(int64_t)t * a.gate.row_stride]) : 0.f;
-      if (a.softplus) dv = softplus(dv);
-      const float du = dv * uv;
-      if (ENDS && q < left) sum_d += dv;
-      float yq = 0.f;
-      auto step = [&](auto jc) {
-        constexpr int J = decltype(jc)::value;
-        if (J >= left) return;
-        const float dj = quad_bcast<J>(dv), duj = quad_bcast<J>(du);
-        const vq bv = *reinterpret_cast<const vq*>(&sb[tq + J][q * Q]);
-        float p = 0.f;
-        vq cv;
-        if (!ENDS) cv = *reinterpret_cast<const vq*>(&sc[ENDS ? 0 : tq + J][q * Q]);
+  // token J of the quad's four, with D in dv's lane J and D u in du's
+  auto step = [&](auto jc, float dv, float du, vq bv, vq cv, float& yq) {
+    constexpr int J = decltype(jc)::value;
+    const float dj = quad_bcast<J>(dv), duj = quad_bcast<J>(du);
+    float p = 0.f;
 #pragma unroll
-        for (int i = 0; i < Q; ++i) {
-          h[i] = fmaf(__builtin_amdgcn_exp2f(dj * al[i]), h[i], duj * bv[i]);
-          if (!ENDS) p = fmaf(cv[i], PAD && q * Q + i >= N ? 0.f : h[i], p);
-        }
-        if (!ENDS) {
-          p += quad_xor1(p);
-          p += quad_xor2(p);
-          yq = q == J ? p : yq;
-        }
-      };
-      step(std::integral_constant<int, 0>());
-      step(std::integral_constant<int, 1>());
-      step(std::integral_constant<int, 2>());
-      step(std::integral_constant<int, 3>());
-      if (!ENDS && q < left && live) {
-        float v = fmaf(skip, uv, yq);
-        if (z) v *= seq_silu(zv);
-        y[(int64_t)t * a.out.row_stride] = from_f<T>(v);
-      }
+    for (int i = 0; i < Q; ++i) {
+      h[i] = fmaf(__builtin_amdgcn_exp2f(dj * al[i]), h[i], duj * bv[i]);
+      if (!ENDS) p = fmaf(cv[i], PAD && q * Q + i >= N ? 0.f : h[i], p);
     }
+    if (!ENDS) {
+      p += quad_xor1(p);
+      p += quad_xor2(p);
+      yq = q == J ? p : yq;
+    }
+  };
+  auto prepare = [&](float dv, float uv, float& du) {
+    dv += bias;
+    if (a.softplus) dv = softplus(dv);
+    du = dv * uv;
+    return dv;
+  };
+  auto finish = [&](float yq, float uv, float zv) {
+    const float v = fmaf(skip, uv, yq);
+    return gated ? v * seq_silu(zv) : v;
+  };
+  auto store_row = [&](int t, float v) {
+    asm("" : "+s"(t));
+    (y + t * sy)[q * sy] = from_f<T>(v);
+  };
+  using J0 = std::integral_constant<int, 0>;
+  using J1 = std::integral_constant<int, 1>;
+  using J2 = std::integral_constant<int, 2>;
+  using J3 = std::integral_constant<int, 3>;
+  // the run's last one to three tokens, with their rows of b and c
+  auto last = [&](int t0, int left, T fu, T fd, T fz, auto brow, auto crow) {
+    const float uv = to_f<T>(fu);
+    float du, yq = 0.f;
+    const float dv = prepare(to_f<T>(fd), uv, du);
+    const vq b0 = brow(0), c0 = ENDS ? b0 : crow(0), b1 = brow(min(1, left - 1)), c1 = ENDS ? b1 : crow(min(1, left - 1)),
+             b2 = brow(left - 1), c2 = ENDS ? b2 : crow(left - 1);
+    step(J0(), dv, du, b0, c0, yq);
+    if (left > 1) step(J1(), dv, du, b1, c1, yq);
+    if (left > 2) step(J2(), dv, du, b2, c2, yq);
+    if (q >= left) return;
+    if (ENDS) sum_d += dv;
+    else store_row(t0, finish(yq, uv, to_f<T>(fz)));
+  };
+  if (tiled) {
+    for (int t0 = 0, i = 0; t0 < it.len; t0 += TILE, i ^= 1) {
+      const int count = min(TILE, it.len - t0);
+      float* now = lds[i];
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        if (BC % 256 == 0 || tid + 256 * j < BC) now[tid + 256 * j] = to_f<T>(bc[j]);
+      __syncthreads();                                 // this tile is there, and the one before last is read
+      const int t1 = t0 + TILE, more = min(TILE, it.len - t1);     // the next tile: its inputs take the registers of
+      if (more > 0) fetch_bc(t1, more);                            // this one's as they are used
+      if (!live) continue;
+      const float *bt = now + q * Q, *ct = ENDS ? bt : bt + TILE * NP;
+      auto row = [&](const float* p, int t) { return *reinterpret_cast<const vq*>(p + t * NP); };
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        if (4 * g + 4 > count) break;
+        const float uv = to_f<T>(ru[g]), zv = gated ? to_f<T>(rz[g]) : 0.f;
+        float du, yq = 0.f;
+        const float dv = prepare(to_f<T>(rd[g]), uv, du);
+        fetch_group(t1, more, g);
+        step(J0(), dv, du, row(bt, 4 * g), row(ct, 4 * g), yq);
+        step(J1(), dv, du, row(bt, 4 * g + 1), row(ct, 4 * g + 1), yq);
+        step(J2(), dv, du, row(bt, 4 * g + 2), row(ct, 4 * g + 2), yq);
+        step(J3(), dv, du, row(bt, 4 * g + 3), row(ct, 4 * g + 3), yq);
+        if (ENDS) sum_d += dv;
+        else store_row(t0 + 4 * g, finish(yq, uv, zv));
+      }
+      if (more <= 0 && count % 4) {
+        const int done = count / 4 * 4;
+        last(t0 + done, count - done, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(bt, done + j); },
+             [&](int j) { return row(ct, done + j); });
+      }
+      fetch_group(t1, more, GROUPS);
+    }
+    if (!live) return;
+  } else {
+    if (!live) return;
+    auto row = [&](const T* p, int64_t stride) {
+      vq v;
+#pragma unroll
+      for (int i = 0; i < Q; ++i) v[i] = !PAD || q * Q + i < N ? to_f<T>(p[stride + q * Q + i]) : 0.f;
+      return v;
+    };
+    if (it.len)
+      last(0, it.len, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(b, j * a.b.row_stride); },
+           [&](int j) { return row(c, j * a.c.row_stride); });
   }
-  if (!live) return;
   float* to = nullptr;
   if (ENDS) {
-    to = k.ws_h + ((m * k.n_slots + it.slot) * D + d) * N;
+    to = k.ws_h + slot;
     sum_d += quad_xor1(sum_d);
     sum_d += quad_xor2(sum_d);
     if (q == 0) k.ws_d[(m * k.n_slots + it.slot) * D + d] = sum_d;
   } else if (a.state_out && it.pos0 + it.len == it.total) {
     to = a.state_out + m * a.state_out_mutant_stride + state;
   }
-  if (to)
+  if (!to) return;
+  if constexpr (PAD) {
 #pragma unroll
     for (int i = 0; i < Q; ++i)
-      if (!PAD || q * Q + i < N) to[q * Q + i] = h[i];
+      if (q * Q + i < N) to[i] = h[i];
+  } else {
+    vq hv;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) hv[i] = h[i];
+    *reinterpret_cast<vq_any*>(to) = hv;
+  }
 }
 
 // The chunks' first states from their states from zero, in place.
@@ -201,42 +301,42 @@ int64_t seq_scan_blocks(const mure_seq_scan_args& a) {
   return (int64_t)((a.channels / a.groups + 63) / 64) * a.groups * a.n_mutants;
 }
 
-template <typename T, int Q, bool PAD, bool ENDS>
+template <typename T, int Q, bool PAD, int KIND>
 static hipError_t scan_q(SeqScanArgs k, hipStream_t s) {
-  const int width = k.a.channels / k.a.groups, tiles = (width + 63) / 64;
-  const int threads = 64 * std::min(4, (width + 15) / 16);
+  const int tiles = (k.a.channels / k.a.groups + 63) / 64;
   const int64_t blocks = seq_scan_blocks(k.a);         // of an item: at most SCAN_GRID (checked by the caller)
   const int most = (int)(SCAN_GRID / blocks);
-  for (int left = k.n_items; left > 0; left -= most, k.items += most) {
-    seq_scan_kernel<T, Q, PAD, ENDS><<<(unsigned)(blocks * std::min(left, most)), threads, 0, s>>>(
+  for (int left = k.n_items; left > 0; left -= most, k.item0 += most) {
+    seq_scan_kernel<T, Q, PAD, KIND><<<(unsigned)(blocks * std::min(left, most)), 256, 0, s>>>(
         k, make_divu32((uint32_t)(tiles * k.a.groups)), make_divu32((uint32_t)k.a.n_mutants), make_divu32((uint32_t)tiles));
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-template <typename T, int Q, bool ENDS>
+template <typename T, int Q, int KIND>
 static hipError_t scan_p(const SeqScanArgs& k, hipStream_t s) {
-  return k.a.states == 4 * Q ? scan_q<T, Q, false, ENDS>(k, s) : scan_q<T, Q, true, ENDS>(k, s);
+  return k.a.states == 4 * Q ? scan_q<T, Q, false, KIND>(k, s) : scan_q<T, Q, true, KIND>(k, s);
 }
 
-template <typename T, bool ENDS>
+template <typename T, int KIND>
 static hipError_t scan_t(const SeqScanArgs& k, hipStream_t s) {
   const int N = k.a.states;
-  if (N <= 4) return scan_p<T, 1, ENDS>(k, s);
-  if (N <= 8) return scan_p<T, 2, ENDS>(k, s);
-  if (N <= 16) return scan_p<T, 4, ENDS>(k, s);
-  if (N <= 32) return scan_p<T, 8, ENDS>(k, s);
-  return scan_p<T, 16, ENDS>(k, s);
+  if (N <= 4) return scan_p<T, 1, KIND>(k, s);
+  if (N <= 8) return scan_p<T, 2, KIND>(k, s);
+  if (N <= 16) return scan_p<T, 4, KIND>(k, s);
+  if (N <= 32) return scan_p<T, 8, KIND>(k, s);
+  return scan_p<T, 16, KIND>(k, s);
 }
 
-hipError_t launch_seq_scan(const SeqScanArgs& k, hipStream_t s) {
-  return k.a.dtype == MURE_F32 ? scan_t<float, false>(k, s) : scan_t<bf16_t, false>(k, s);
+template <int KIND>
+static hipError_t scan_any(const SeqScanArgs& k, hipStream_t s) {
+  return k.a.dtype == MURE_F32 ? scan_t<float, KIND>(k, s) : scan_t<bf16_t, KIND>(k, s);
 }
 
-hipError_t launch_seq_scan_ends(const SeqScanArgs& k, hipStream_t s) {
-  return k.a.dtype == MURE_F32 ? scan_t<float, true>(k, s) : scan_t<bf16_t, true>(k, s);
-}
+hipError_t launch_seq_scan(const SeqScanArgs& k, hipStream_t s) { return k.longest < 4 ? scan_any<STEPS>(k, s) : scan_any<RUNS>(k, s); }
+
+hipError_t launch_seq_scan_ends(const SeqScanArgs& k, hipStream_t s) { return scan_any<ENDS_ONLY>(k, s); }
 
 hipError_t launch_seq_scan_join(const SeqScanArgs& k, hipStream_t s) {
   const int64_t DN = (int64_t)k.a.channels * k.a.states;

@@ -53,8 +53,8 @@ struct mure_seq {
   int64_t n_seq = 0, tokens = 0, longest = 0;
   // work lists, in device memory
   Mem lists;
-  const SeqItem* conv[2] = {};                 // runs of at most CONV_RUNS tokens
-  int n_conv[2] = {};
+  const SeqItem* conv[N_RUNS] = {};            // runs of at most CONV_RUNS tokens
+  int n_conv[N_RUNS] = {};
   const SeqItem* scan = nullptr;               // whole sequences and chunks, longest first
   int n_scan = 0;
   const SeqItem* ends = nullptr;               // the chunks but each sequence's last
@@ -199,7 +199,8 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
     if (s->tokens > INT32_MAX) invalid("the batch has 2^31 tokens or more");
     s->longest = std::max(s->longest, lengths[i]);
   }
-  std::vector<SeqItem> conv[2], scan, ends;
+  const bool ones = std::all_of(lengths, lengths + n_seq, [](int64_t n) { return n == 1; });
+  std::vector<SeqItem> conv[N_RUNS], scan, ends;
   std::vector<SeqChunks> chunked;
   int64_t row = 0, slots = 0;
   for (int32_t i = 0; i < (int32_t)n_seq; ++i) {
@@ -210,7 +211,7 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
         v.push_back({i, (int32_t)(row + t), (int32_t)std::min(run, L - t), (int32_t)t, (int32_t)L,
                      slot < 0 ? -1 : (int32_t)(slot + t / run)});
     };
-    for (int k = 0; k < 2; ++k) runs(conv[k], CONV_RUNS[k], -1);
+    for (int k = 0; k < N_RUNS; ++k) runs(conv[k], CONV_RUNS[k], -1);
     if (L <= MURE_SEQ_SPLIT_TOKENS) {
       runs(scan, MURE_SEQ_SPLIT_TOKENS, -1);
     } else {
@@ -227,17 +228,17 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
   std::stable_sort(scan.begin(), scan.end(), [](const SeqItem& a, const SeqItem& b) { return a.len > b.len; });
   s->n_slots = slots;
   std::vector<char> host;
-  size_t at[5];
+  size_t at[N_RUNS + 3];
   int k = 0;
   auto put = [&](const void* p, size_t bytes) {
     at[k++] = host.size();
     host.insert(host.end(), static_cast<const char*>(p), static_cast<const char*>(p) + bytes);
     host.resize((host.size() + 15) / 16 * 16);
   };
-  for (const auto* v : {&conv[0], &conv[1], &scan, &ends}) put(v->data(), v->size() * sizeof(SeqItem));
+  for (const auto& v : conv) put(v.data(), v.size() * sizeof(SeqItem));
+  for (const auto* v : {&scan, &ends}) put(v->data(), v->size() * sizeof(SeqItem));
   put(chunked.data(), chunked.size() * sizeof(SeqChunks));
-  s->n_conv[0] = (int)conv[0].size();
-  s->n_conv[1] = (int)conv[1].size();
+  for (int i = 0; i < N_RUNS; ++i) s->n_conv[i] = (int)conv[i].size();
   s->n_scan = (int)scan.size();
   s->n_ends = (int)ends.size();
   s->n_chunked = (int)chunked.size();
@@ -247,11 +248,11 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
     check(hipMemcpyAsync(s->lists.p, host.data(), host.size(), hipMemcpyHostToDevice, s->stream), "upload of the work lists");
     check(hipStreamSynchronize(s->stream), "upload of the work lists");
     const char* d = static_cast<const char*>(s->lists.p);
-    s->conv[0] = reinterpret_cast<const SeqItem*>(d + at[0]);
-    s->conv[1] = reinterpret_cast<const SeqItem*>(d + at[1]);
-    s->scan = reinterpret_cast<const SeqItem*>(d + at[2]);
-    s->ends = reinterpret_cast<const SeqItem*>(d + at[3]);
-    s->chunked = reinterpret_cast<const SeqChunks*>(d + at[4]);
+    if (!ones)
+      for (int i = 0; i < N_RUNS; ++i) s->conv[i] = reinterpret_cast<const SeqItem*>(d + at[i]);
+    if (!ones) s->scan = reinterpret_cast<const SeqItem*>(d + at[N_RUNS]);
+    s->ends = reinterpret_cast<const SeqItem*>(d + at[N_RUNS + 1]);
+    s->chunked = reinterpret_cast<const SeqChunks*>(d + at[N_RUNS + 2]);
   }
   *out = s.release();
 }
@@ -291,11 +292,12 @@ void conv(mure_seq* s, const mure_seq_conv_args* args) {
     check_apart(so, {out});
   }
   check_device(s->device);
-  // Long runs read fewer rows twice (3 of 35 at 4 taps, short ones 3 of 11),
-  // short ones give four times the threads: they are taken while the long
-  // runs' threads (of 16 bytes of channels) would leave most of the chip idle.
-  const int64_t vecs = (C * es + 15) / 16;
-  const int w = (int64_t)s->n_conv[0] * M * vecs < 256 * 512 ? 1 : 0;
+  // Long runs read fewer rows twice (at 4 taps 3 of 35, 19 and 7), short ones give more threads (of 16 bytes of
+  // channels): the longest is taken that fills the chip, or the next that comes near it.  24 prompts of 18865 tokens
+  // and 1536 bfloat16 channels take 24.4 us in runs of 16 (230 thousand threads) and 27 in runs of 32 or 8; 65536
+  // tokens of 4096 channels 204 us in runs of 32 and 209 in runs of 16.
+  const int64_t vecs = (C * es + 15) / 16 * M;
+  const int w = s->n_conv[0] * vecs >= 1 << 17 ? 0 : s->n_conv[1] * vecs >= 1 << 15 ? 1 : 2;
   k.items = s->conv[w];
   k.n_items = s->n_conv[w];
   check(launch_seq_conv(k, s->stream), "mure_seq_conv");
@@ -341,6 +343,7 @@ void scan(mure_seq* s, const mure_seq_scan_args* args) {
   }
   check_device(s->device);
   k.n_slots = s->n_slots;
+  k.longest = s->longest;
   if (s->n_chunked) {
     const wide need = (wide)M * s->n_slots * D * (N + 1) * 4;
     if (need > MOST) throw Fail{MURE_E_NOMEM, "sequence workspace"};

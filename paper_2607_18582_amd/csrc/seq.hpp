@@ -19,24 +19,30 @@ struct SeqItem {
   int32_t seq, row0, len, pos0, total, slot;
 };
 
+// Item i of a list; a list that is not there (nullptr) is that of sequences of
+// one token each, which a decoding step need not wait for.
+__device__ __forceinline__ SeqItem seq_item(const SeqItem* items, int i) { return items ? items[i] : SeqItem{i, i, 1, 0, 1, -1}; }
+
 // A sequence scanned in chunks: its slots slot0 .. slot0 + n - 1.
 struct SeqChunks {
   int32_t seq, slot0, n;
 };
 
 constexpr int SCAN_CHUNK = 128;                // tokens of a chunk
-constexpr int CONV_RUNS[2] = {32, 8};          // tokens of a convolution's runs
+constexpr int CONV_RUNS[] = {32, 16, 4};       // tokens of a convolution's runs
+constexpr int N_RUNS = 3;
 
 struct SeqConvArgs {
   mure_seq_conv_args a;
   const SeqItem* items = nullptr;
-  int n_items = 0;
+  int n_items = 0, item0 = 0;
 };
 
 struct SeqScanArgs {
   mure_seq_scan_args a;
   const SeqItem* items = nullptr;              // of this launch
-  int n_items = 0;
+  int n_items = 0, item0 = 0;
+  int64_t longest = 0;                         // tokens of the longest sequence
   const SeqChunks* chunks = nullptr;
   int n_chunked = 0;
   int64_t n_slots = 0;

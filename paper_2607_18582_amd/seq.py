@@ -17,6 +17,8 @@ after the call.
 from __future__ import annotations
 
 import ctypes as C
+import struct
+import sys
 from typing import Optional, Sequence
 
 import numpy as np
@@ -68,116 +70,128 @@ def declare(lib: C.CDLL) -> None:
     for name, res, args in (("mure_seq_version", C.c_int32, []),
                             ("mure_seq_create", C.c_int, [P, C.c_int64, P, C.POINTER(P)]),
                             ("mure_seq_destroy", None, [P]),
-                            ("mure_seq_conv", C.c_int, [P, C.POINTER(mure_seq_conv_args)]),
-                            ("mure_seq_scan", C.c_int, [P, C.POINTER(mure_seq_scan_args)]),
-                            ("mure_seq_norm", C.c_int, [P, C.POINTER(mure_seq_norm_args)])):
+                            ("mure_seq_conv", C.c_int, [P, P]), ("mure_seq_scan", C.c_int, [P, P]),
+                            ("mure_seq_norm", C.c_int, [P, P])):
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
+
+
+# The argument blocks as they are filled here: one pack is several times as fast as a Structure's fields, and
+# a call on single tokens takes no longer on the GPU than its marshalling.
+_CONV = struct.Struct("=6i14q")
+_SCAN = struct.Struct("=6i28q")
+_NORM = struct.Struct("=4iq4i2f25q")
+assert (_CONV.size, _SCAN.size, _NORM.size) == tuple(map(C.sizeof, (mure_seq_conv_args, mure_seq_scan_args, mure_seq_norm_args)))
+
+_NONE_ROWS, _NONE = (0, 0, 0), (0, 0)
 
 
 class _Call:
     """The tensors of one call: their checks, the number of mutants, and the
     order against torch's current stream."""
 
+    __slots__ = ("mure", "torch", "device", "dtype", "code", "mutants", "axis", "first")
+
     def __init__(self, mure, first, what: str):
-        import torch
-        self.torch, self.mure = torch, mure
+        torch = self.torch = sys.modules["torch"]
         if not isinstance(first, torch.Tensor):
             raise TypeError(f"{what} must be a torch tensor")
-        self.device, self.dtype = first.device, first.dtype
-        if mure.device >= 0 and (self.device.type != "cuda" or self.device.index != mure.device):
-            raise ValueError(f"{what} is on {self.device}, the context on cuda:{mure.device}")
-        if self.dtype not in (torch.float32, torch.bfloat16):
+        self.mure, self.first, self.dtype, self.device = mure, first, first.dtype, first.get_device()
+        if self.device != mure.device:                 # -1: the CPU, or a planning-only context
+            raise ValueError(f"{what} is on {first.device}, the context on device {mure.device}")
+        if self.dtype is torch.bfloat16:
+            self.code = 1
+        elif self.dtype is torch.float32:
+            self.code = 0
+        else:
             raise TypeError(f"{what} is {self.dtype}; float32 or bfloat16 is needed")
-        if first.dim() not in (2, 3) or first.size(-1) >= 1 << 31:
+        if not 2 <= first.dim() <= 3 or first.shape[-1] >= 1 << 31:
             raise ValueError(f"{what} has shape {tuple(first.shape)}; [rows][channels] is needed, or that of each mutant")
-        self.code = 0 if self.dtype is torch.float32 else 1
         self.mutants, self.axis = 1, False
 
-    def _seen(self, t, what: str, dtype, shape, dense: bool):
-        """The mutant stride of t, a tensor of `shape` or [mutants] + shape; dense:
-        but for the mutant axis it is contiguous, else its last axis is."""
+    def _check(self, t, what: str, dtype):
         if not isinstance(t, self.torch.Tensor):
             raise TypeError(f"{what} must be a torch tensor")
-        if t.device != self.device or t.dtype is not dtype:
-            raise TypeError(f"{what} is {t.dtype} on {t.device}; {dtype} on {self.device} is needed")
-        have, extra = t.shape, t.dim() - len(shape)
-        if not 0 <= extra <= 1 or have[extra:] != shape:
-            raise ValueError(f"{what} has shape {tuple(have)}; {tuple(shape)} is needed, or that of each mutant")
-        if dense:
-            one = t[0] if extra and have[0] else t
-            if not one.is_contiguous():
-                raise ValueError(f"{what} must be contiguous" + (" for each mutant" if extra else ""))
-        elif shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError(f"the last axis of {what} must be contiguous")
-        if not extra:
-            return 0
+        if t.dtype is not dtype or t.get_device() != self.device:
+            raise TypeError(f"{what} is {t.dtype} on {t.device}; {dtype} on {self.first.device} is needed")
+
+    def _mutant_axis(self, n: int, stride: int, what: str) -> int:
+        """The mutant stride of an axis of n mutants."""
         self.axis = True
-        n = have[0]
-        if n == 0:
-            raise ValueError(f"{what} has no mutants")
         if n == 1:
             return 0
-        if self.mutants not in (1, n):
+        if n == 0 or self.mutants not in (1, n):
             raise ValueError(f"{what} has {n} mutants, another argument {self.mutants}")
         self.mutants = n
-        return t.stride(0)
+        return stride
 
     def rows(self, t, what: str, rows: int, width: int, dtype=None):
+        """(address, mutant stride, row stride) of [rows][width] or that of each mutant"""
         if t is None:
-            return _rows()
-        stride = self._seen(t, what, dtype or self.dtype, (rows, width), False)
-        return _rows(t.data_ptr(), stride, t.stride(-2))
-
-    def dense(self, t, what: str, shape, dtype=None):
-        """(address, mutant stride)"""
-        if t is None:
-            return None, 0
-        stride = self._seen(t, what, dtype or self.torch.float32, shape, True)
-        return t.data_ptr(), stride
-
-    def output(self, t, what: str, shape, dtype=None):
-        """t, checked, or a new tensor of the call's mutants; and its strides."""
-        full = (self.mutants, *shape) if self.axis else tuple(shape)
-        if t is None:
-            return self.torch.empty(full, dtype=dtype or self.dtype, device=self.device)
-        if tuple(t.shape) != full or t.dtype is not (dtype or self.dtype) or t.device != self.device:
-            raise ValueError(f"{what} is {tuple(t.shape)} {t.dtype}; {full} {dtype or self.dtype} is needed")
-        if full[-1] > 1 and t.stride(-1) != 1:
+            return _NONE_ROWS
+        self._check(t, what, dtype or self.dtype)
+        shape, stride = t.shape, t.stride()
+        if shape[-2:] != (rows, width) or len(shape) > 3:
+            raise ValueError(f"{what} has shape {tuple(shape)}; {(rows, width)} is needed, or that of each mutant")
+        if stride[-1] != 1 and width > 1:
             raise ValueError(f"the last axis of {what} must be contiguous")
+        if len(shape) == 2:
+            return t.data_ptr(), 0, stride[0]
+        return t.data_ptr(), self._mutant_axis(shape[0], stride[0], what), stride[1]
+
+    def dense(self, t, what: str, shape: tuple, dtype=None):
+        """(address, mutant stride) of a tensor of `shape`, contiguous, or that of each mutant"""
+        if t is None:
+            return _NONE
+        self._check(t, what, dtype or self.torch.float32)
+        have, extra = t.shape, t.dim() - len(shape)
+        if not 0 <= extra <= 1 or have[extra:] != shape:
+            raise ValueError(f"{what} has shape {tuple(have)}; {shape} is needed, or that of each mutant")
+        if not t.is_contiguous() and not (extra and have[0] and t[0].is_contiguous()):
+            raise ValueError(f"{what} must be contiguous" + (" for each mutant" if extra else ""))
+        return t.data_ptr(), self._mutant_axis(have[0], t.stride(0), what) if extra else 0
+
+    def output(self, t, what: str, shape: tuple, dtype=None):
+        """t, checked, or a new tensor of the call's mutants."""
+        full = (self.mutants, *shape) if self.axis else shape
+        if t is None:
+            return self.first.new_empty(full, dtype=dtype or self.dtype)
+        self._check(t, what, dtype or self.dtype)
+        if t.shape != full:
+            raise ValueError(f"{what} has shape {tuple(t.shape)}; {full} is needed")
         return t
 
-    def out_rows(self, t):
-        return _rows(t.data_ptr(), t.stride(0) if self.axis else 0, t.stride(-2))
+    def out_rows(self, t, what: str):
+        stride = t.stride()
+        if stride[-1] != 1 and t.shape[-1] > 1:
+            raise ValueError(f"the last axis of {what} must be contiguous")
+        return t.data_ptr(), stride[0] if self.axis else 0, stride[-2]
 
     def out_dense(self, t, what: str):
-        if not (t[0] if self.axis else t).is_contiguous():
+        if not t.is_contiguous() and not (self.axis and t[0].is_contiguous()):
             raise ValueError(f"{what} must be contiguous" + (" for each mutant" if self.axis else ""))
         return t.data_ptr(), t.stride(0) if self.axis else 0
 
-    def run(self, fn, handle, args) -> None:
-        mure = self.mure
-        if mure.device < 0:
-            mure._check(fn(handle, C.byref(args)))
-            return
-        current = self.torch.cuda.current_stream(self.device)
-        if current.cuda_stream == mure.stream:
-            mure._check(fn(handle, C.byref(args)))
-            return
-        own = self.torch.cuda.ExternalStream(mure.stream, device=self.device) if mure.stream else \
-            self.torch.cuda.default_stream(self.device)
-        own.wait_stream(current)
-        try:
-            mure._check(fn(handle, C.byref(args)))
-        finally:
+    def run(self, fn, handle, args: bytes) -> None:
+        mure, cuda = self.mure, self.torch.cuda
+        if mure.device < 0 or cuda.current_stream(self.device).cuda_stream == mure.stream:
+            status = fn(handle, args)
+        else:
+            current = cuda.current_stream(self.device)
+            own = cuda.ExternalStream(mure.stream, device=self.device) if mure.stream else cuda.default_stream(self.device)
+            own.wait_stream(current)
+            status = fn(handle, args)
             current.wait_stream(own)
+        if status:
+            mure._check(status)
 
 
 def _one_of(table: dict, key, what: str) -> int:
-    try:
-        return table[key]
-    except (KeyError, TypeError):
-        raise ValueError(f"{what} is {key!r}; one of {', '.join(map(repr, table))} is needed") from None
+    if key is None or isinstance(key, str):
+        code = table.get(key)
+        if code is not None:
+            return code
+    raise ValueError(f"{what} is {key!r}; one of {', '.join(map(repr, table))} is needed")
 
 
 class Sequences:
@@ -215,19 +229,14 @@ class Sequences:
         first token (zeros without it).  Returns (out, state_out), state_out being the last
         K - 1 rows of (state, x); both may be given, state_out as the state itself."""
         c = self._call(x, "x")
-        width, K = x.size(-1), taps.size(-1)
-        a = mure_seq_conv_args(dtype=c.code, channels=width, n_taps=K,
-                               activation=_one_of(ACTIVATIONS, activation, "activation"))
+        width, K = x.shape[-1], taps.shape[-1]
         held = (self.count, K - 1, width)
-        a.x = c.rows(x, "x", self.tokens, width)
-        a.taps, a.taps_mutant_stride = c.dense(taps, "taps", (width, K), c.dtype)
-        a.bias = _param(*c.dense(bias, "bias", (width,)))
-        a.state, a.state_mutant_stride = c.dense(state, "state", held, c.dtype)
-        out = c.output(out, "out", (self.tokens, width))
-        state_out = c.output(state_out, "state_out", held)
-        a.state_out, a.state_out_mutant_stride = c.out_dense(state_out, "state_out")
-        a.out, a.n_mutants = c.out_rows(out), c.mutants
-        c.run(self.mure.lib.mure_seq_conv, self.handle, a)
+        px, ptaps = c.rows(x, "x", self.tokens, width), c.dense(taps, "taps", (width, K), c.dtype)
+        pbias, pstate = c.dense(bias, "bias", (width,)), c.dense(state, "state", held, c.dtype)
+        out, state_out = c.output(out, "out", (self.tokens, width)), c.output(state_out, "state_out", held)
+        c.run(self.mure.lib.mure_seq_conv, self.handle,
+              _CONV.pack(c.code, c.mutants, width, K, _one_of(ACTIVATIONS, activation, "activation"), 0, *px, *ptaps, *pbias,
+                         *pstate, *c.out_dense(state_out, "state_out"), *c.out_rows(out, "out")))
         return out, state_out
 
     def scan(self, u, dt, A, B, C_, *, skip=None, dt_bias=None, gate=None, softplus: bool = True, state=None,
@@ -239,26 +248,19 @@ class Sequences:
         [sequences][channels][states] float32 (zeros without it).  Returns (out,
         state_out); both may be given, state_out as the state itself."""
         c = self._call(u, "u")
-        width, N = u.size(-1), A.size(-1)
-        cols = B.size(-1)
+        width, N, cols, T = u.shape[-1], A.shape[-1], B.shape[-1], self.tokens
         if N == 0 or cols % N:
             raise ValueError(f"B has {cols} columns, no multiple of the {N} states of A")
-        a = mure_seq_scan_args(dtype=c.code, channels=width, states=N, groups=cols // N, softplus=bool(softplus))
-        T, held, f32 = self.tokens, (self.count, width, N), c.torch.float32
-        a.u = c.rows(u, "u", T, width)
-        a.dt = c.rows(dt, "dt", T, width)
-        a.b = c.rows(B, "B", T, cols)
-        a.c = c.rows(C_, "C_", T, cols)
-        a.gate = c.rows(gate, "gate", T, width)
-        a.a = _param(*c.dense(A, "A", (width, N)))
-        a.skip = _param(*c.dense(skip, "skip", (width,)))
-        a.dt_bias = _param(*c.dense(dt_bias, "dt_bias", (width,)))
-        a.state, a.state_mutant_stride = c.dense(state, "state", held)
+        held = (self.count, width, N)
+        pu, pdt, pb, pc = c.rows(u, "u", T, width), c.rows(dt, "dt", T, width), c.rows(B, "B", T, cols), c.rows(C_, "C_", T, cols)
+        pz, pa = c.rows(gate, "gate", T, width), c.dense(A, "A", (width, N))
+        pskip, pbias = c.dense(skip, "skip", (width,)), c.dense(dt_bias, "dt_bias", (width,))
+        pstate = c.dense(state, "state", held)
         out = c.output(out, "out", (T, width))
-        state_out = c.output(state_out, "state_out", held, f32)
-        a.state_out, a.state_out_mutant_stride = c.out_dense(state_out, "state_out")
-        a.out, a.n_mutants = c.out_rows(out), c.mutants
-        c.run(self.mure.lib.mure_seq_scan, self.handle, a)
+        state_out = c.output(state_out, "state_out", held, c.torch.float32)
+        c.run(self.mure.lib.mure_seq_scan, self.handle,
+              _SCAN.pack(c.code, c.mutants, width, N, cols // N, bool(softplus), *pu, *pdt, *pb, *pc, *pz, *pa, *pskip, *pbias,
+                         *pstate, *c.out_dense(state_out, "state_out"), *c.out_rows(out, "out")))
         return out, state_out
 
 
@@ -288,34 +290,30 @@ class SeqOps:
         without ``before``; residual_out = False leaves r out (None); residual_out may be the
         residual and out may be y or the gate."""
         c = _Call(self, y, "y")
-        rows, width = y.size(-2), y.size(-1)
-        torch = c.torch
+        torch, (rows, width) = c.torch, y.shape[-2:]
         rtype = c.dtype if residual is None else residual.dtype
-        a = mure_seq_norm_args(dtype=c.code, residual_dtype=0 if rtype is torch.float32 else 1, channels=width, rows=rows,
-                               gate_at=0 if gate is None else _one_of(GATES, gate_at, "gate_at"),
-                               gate_activation=_one_of(ACTIVATIONS, gate_activation, "gate_activation"),
-                               after=_one_of(NORMS, after, "after"), before=_one_of(NORMS, before, "before"),
-                               eps=eps, scale_all=1.0 if isinstance(scale, torch.Tensor) else scale)
-        if rtype not in (torch.float32, torch.bfloat16):
-            raise TypeError(f"residual is {rtype}; float32 or bfloat16 is needed")
-        a.y = c.rows(y, "y", rows, width)
-        a.gate = c.rows(gate, "gate", rows, width)
-        a.residual = c.rows(residual, "residual", rows, width, rtype)
-        for name, t in (("after_weight", after_weight), ("after_bias", after_bias),
-                        ("scale", scale if isinstance(scale, torch.Tensor) else None),
-                        ("before_weight", before_weight), ("before_bias", before_bias)):
-            if t is not None:
-                setattr(a, name, _param(*c.dense(t, name, (width,))))
-        a.n_mutants = c.mutants
-        if residual_out is not False:
-            residual_out = c.output(residual_out, "residual_out", (rows, width), rtype)
-            a.residual_out = c.out_rows(residual_out)
-        else:
+        if rtype is not c.dtype and rtype is not torch.float32:
+            raise TypeError(f"residual is {rtype}; {c.dtype} or float32 is needed")
+        if before is None and out is not None:
+            raise ValueError("out needs a `before` norm")
+        py, pz = c.rows(y, "y", rows, width), c.rows(gate, "gate", rows, width)
+        pr, w = c.rows(residual, "residual", rows, width, rtype), (width,)
+        scaled = isinstance(scale, torch.Tensor)
+        params = (*c.dense(after_weight, "after_weight", w), *c.dense(after_bias, "after_bias", w),
+                  *c.dense(scale if scaled else None, "scale", w), *c.dense(before_weight, "before_weight", w),
+                  *c.dense(before_bias, "before_bias", w))
+        pro = po = _NONE_ROWS
+        if residual_out is False:
             residual_out = None
+        else:
+            residual_out = c.output(residual_out, "residual_out", (rows, width), rtype)
+            pro = c.out_rows(residual_out, "residual_out")
         if before is not None:
             out = c.output(out, "out", (rows, width))
-            a.out = c.out_rows(out)
-        elif out is not None:
-            raise ValueError("out needs a `before` norm")
-        c.run(self.lib.mure_seq_norm, self.ctx, a)
+            po = c.out_rows(out, "out")
+        c.run(self.lib.mure_seq_norm, self.ctx,
+              _NORM.pack(c.code, 0 if rtype is torch.float32 else 1, c.mutants, width, rows,
+                         0 if gate is None else _one_of(GATES, gate_at, "gate_at"),
+                         _one_of(ACTIVATIONS, gate_activation, "gate_activation"), _one_of(NORMS, after, "after"),
+                         _one_of(NORMS, before, "before"), eps, 1.0 if scaled else scale, *py, *pz, *pr, *params, *pro, *po))
         return residual_out, out

@@ -77,7 +77,7 @@ def scan(u, dt, A, B, C, lengths, skip=None, dt_bias=None, gate=None, use_softpl
         h = torch.zeros(M, D, N, dtype=torch.float64) if state is None else full(state)[:, i].clone()
         e = torch.zeros_like(h)                 # bound of h
         # a long sequence's decay over a chunk is one exponential of a sum of steps, at most 34 added in a row
-        summed = (5 if count <= 1024 else 40) * U
+        summed = (5 if count <= 512 else 40) * U
         for t in range(row, row + count):
             s = dt[:, t] + dt_bias
             step, rel = softplus(s) if use_softplus else (s, torch.zeros_like(s))

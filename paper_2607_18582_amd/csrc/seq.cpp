@@ -110,12 +110,11 @@ struct Span {
 
 Span span(const char* name, const void* p, int64_t esize, int64_t width, int64_t rows, int64_t row_stride, int64_t mutants,
           int64_t mutant_stride) {
-  const std::string n(name);
-  if (!p && rows > 0) invalid(n + " is NULL");
-  if (row_stride < 0 || mutant_stride < 0) invalid(n + ": a stride is negative");
+  if (!p && rows > 0) invalid(std::string(name) + " is NULL");
+  if (row_stride < 0 || mutant_stride < 0) invalid(std::string(name) + ": a stride is negative");
   Span s{name, static_cast<const char*>(p), esize, width, rows, rows > 1 ? row_stride : 0, mutants, mutants > 1 ? mutant_stride : 0};
-  if (s.extent() > MOST) invalid(n + ": its strides pass the address space");
-  if (reinterpret_cast<uintptr_t>(p) % esize) invalid(n + " is not aligned to its elements");
+  if (s.extent() > MOST) invalid(std::string(name) + ": its strides pass the address space");
+  if (reinterpret_cast<uintptr_t>(p) % esize) invalid(std::string(name) + " is not aligned to its elements");
   return s;
 }
 
@@ -150,8 +149,17 @@ bool same(const Span& a, const Span& b) {
          (a.mutants == 1 || a.mutant_stride > 0);
 }
 
+// The tensors of a call (a norm has the most, 10).
+struct Spans {
+  Span v[10];
+  int n = 0;
+  void push_back(const Span& s) { v[n++] = s; }
+  const Span* begin() const { return v; }
+  const Span* end() const { return v + n; }
+};
+
 // `out` may be one of `allowed`, element by element, and may meet nothing else.
-void check_apart(const Span& out, const std::vector<Span>& others, std::initializer_list<const Span*> allowed = {}) {
+void check_apart(const Span& out, const Spans& others, std::initializer_list<const Span*> allowed = {}) {
   for (const Span& o : others) {
     if (!meet(out, o)) continue;
     bool ok = false;
@@ -171,7 +179,7 @@ void check_range(int64_t v, int64_t lo, int64_t hi, const char* what) {
 }
 
 // An optional float32 parameter of n values a mutant.
-void add_param(std::vector<Span>& in, const char* name, const mure_seq_param& p, int64_t n, int64_t mutants) {
+void add_param(Spans& in, const char* name, const mure_seq_param& p, int64_t n, int64_t mutants) {
   if (p.p) in.push_back(span(name, p.p, 4, n, 1, 0, mutants, p.mutant_stride));
 }
 
@@ -272,7 +280,7 @@ void conv(mure_seq* s, const mure_seq_conv_args* args) {
   if (a.reserved) invalid("reserved must be 0");
   const int64_t M = a.n_mutants, C = a.channels, K = a.n_taps;
   if (K == 1) a.state = nullptr, a.state_out = nullptr;
-  std::vector<Span> in;
+  Spans in;
   in.push_back(span("x", a.x.p, es, C, s->tokens, a.x.row_stride, M, a.x.mutant_stride));
   in.push_back(span("taps", a.taps, es, C * K, 1, 0, M, a.taps_mutant_stride));
   add_param(in, "bias", a.bias, C, M);
@@ -289,7 +297,7 @@ void conv(mure_seq* s, const mure_seq_conv_args* args) {
     const Span so = span("state_out", a.state_out, es, held, 1, 0, M, a.state_out_mutant_stride);
     check_output(so);
     check_apart(so, in, {a.state ? &state : nullptr});
-    check_apart(so, {out});
+    if (meet(so, out)) invalid("state_out overlaps out");
   }
   check_device(s->device);
   // Long runs read fewer rows twice (at 4 taps 3 of 35, 19 and 7), short ones give more threads (of 16 bytes of
@@ -317,7 +325,7 @@ void scan(mure_seq* s, const mure_seq_scan_args* args) {
   check_range(a.softplus, 0, 1, "softplus");
   if (seq_scan_blocks(a) > SCAN_GRID) throw Fail{MURE_E_UNSUPPORTED, "too many channels times mutants for one scan"};
   const int64_t M = a.n_mutants, D = a.channels, N = a.states, T = s->tokens;
-  std::vector<Span> in;
+  Spans in;
   in.push_back(span("u", a.u.p, es, D, T, a.u.row_stride, M, a.u.mutant_stride));
   in.push_back(span("dt", a.dt.p, es, D, T, a.dt.row_stride, M, a.dt.mutant_stride));
   in.push_back(span("b", a.b.p, es, a.groups * N, T, a.b.row_stride, M, a.b.mutant_stride));
@@ -339,7 +347,7 @@ void scan(mure_seq* s, const mure_seq_scan_args* args) {
     const Span so = span("state_out", a.state_out, 4, held, 1, 0, M, a.state_out_mutant_stride);
     check_output(so);
     check_apart(so, in, {a.state ? &state : nullptr});
-    check_apart(so, {out});
+    if (meet(so, out)) invalid("state_out overlaps out");
   }
   check_device(s->device);
   k.n_slots = s->n_slots;
@@ -385,7 +393,7 @@ void norm(mure_ctx* ctx, const mure_seq_norm_args* args) {
   if (a.rows > 0 && !a.out.p && !a.residual_out.p) invalid("neither out nor residual_out is given");
   if (a.out.p && !a.before) invalid("out needs a `before`");
   const int64_t M = a.n_mutants, C = a.channels, R = a.rows;
-  std::vector<Span> in;
+  Spans in;
   const Span y = span("y", a.y.p, es, C, R, a.y.row_stride, M, a.y.mutant_stride);
   in.push_back(y);
   Span gate{}, res{};
@@ -396,17 +404,17 @@ void norm(mure_ctx* ctx, const mure_seq_norm_args* args) {
   add_param(in, "scale", a.scale, C, M);
   add_param(in, "before_weight", a.before_weight, C, M);
   add_param(in, "before_bias", a.before_bias, C, M);
-  std::vector<Span> outs;
+  Span ro{};
   if (a.residual_out.p) {
-    outs.push_back(span("residual_out", a.residual_out.p, rs, C, R, a.residual_out.row_stride, M, a.residual_out.mutant_stride));
-    check_output(outs.back());
-    check_apart(outs.back(), in, {a.residual.p ? &res : nullptr});
+    ro = span("residual_out", a.residual_out.p, rs, C, R, a.residual_out.row_stride, M, a.residual_out.mutant_stride);
+    check_output(ro);
+    check_apart(ro, in, {a.residual.p ? &res : nullptr});
   }
   if (a.out.p) {
     const Span o = span("out", a.out.p, es, C, R, a.out.row_stride, M, a.out.mutant_stride);
     check_output(o);
     check_apart(o, in, {&y, a.gate.p ? &gate : nullptr});
-    check_apart(o, outs);
+    if (a.residual_out.p && meet(o, ro)) invalid("out overlaps residual_out");
   }
   const CtxView cv = ctx_view(ctx);
   check_device(cv.device);

@@ -3,8 +3,9 @@
 a ``Sequences``, whose ``conv`` and ``scan`` run over them; ``Mure.block_norm``
 works row by row.
 
-Argument marshalling only, as in ``binding.py``.  Activations are CUDA tensors
-of packed rows, ``[tokens][channels]`` where all mutants share them or
+Argument marshalling only, as in ``binding.py``, the tensors' part of it in C++
+(``pyext/seq_args.cpp``).  Activations are CUDA tensors of packed rows,
+``[tokens][channels]`` where all mutants share them or
 ``[mutants][tokens][channels]``; parameters and states likewise have a leading
 mutant axis or none.  A size-1 or expanded (stride 0) mutant axis counts as
 shared.  Rows may be strided (slices of a projection's output); a row's
@@ -17,8 +18,6 @@ after the call.
 from __future__ import annotations
 
 import ctypes as C
-import struct
-import sys
 from typing import Optional, Sequence
 
 import numpy as np
@@ -30,38 +29,7 @@ ACTIVATIONS = {None: 0, "silu": 1, "sigmoid": 2}
 NORMS = {None: 0, "rms": 1, "layer": 2}
 GATES = {"before": 1, "after": 2}
 
-
-class _rows(C.Structure):                       # mure_seq_in, mure_seq_out
-    _fields_ = [("p", C.c_void_p), ("mutant_stride", C.c_int64), ("row_stride", C.c_int64)]
-
-
-class _param(C.Structure):                      # mure_seq_param
-    _fields_ = [("p", C.c_void_p), ("mutant_stride", C.c_int64)]
-
-
-class mure_seq_conv_args(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("n_mutants", C.c_int32), ("channels", C.c_int32), ("n_taps", C.c_int32),
-                ("activation", C.c_int32), ("reserved", C.c_int32), ("x", _rows), ("taps", C.c_void_p),
-                ("taps_mutant_stride", C.c_int64), ("bias", _param), ("state", C.c_void_p),
-                ("state_mutant_stride", C.c_int64), ("state_out", C.c_void_p),
-                ("state_out_mutant_stride", C.c_int64), ("out", _rows)]
-
-
-class mure_seq_scan_args(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("n_mutants", C.c_int32), ("channels", C.c_int32), ("states", C.c_int32),
-                ("groups", C.c_int32), ("softplus", C.c_int32), ("u", _rows), ("dt", _rows), ("b", _rows),
-                ("c", _rows), ("gate", _rows), ("a", _param), ("skip", _param), ("dt_bias", _param),
-                ("state", C.c_void_p), ("state_mutant_stride", C.c_int64), ("state_out", C.c_void_p),
-                ("state_out_mutant_stride", C.c_int64), ("out", _rows)]
-
-
-class mure_seq_norm_args(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("residual_dtype", C.c_int32), ("n_mutants", C.c_int32),
-                ("channels", C.c_int32), ("rows", C.c_int64), ("gate_at", C.c_int32), ("gate_activation", C.c_int32),
-                ("after", C.c_int32), ("before", C.c_int32), ("eps", C.c_float), ("scale_all", C.c_float),
-                ("y", _rows), ("gate", _rows), ("residual", _rows), ("after_weight", _param), ("after_bias", _param),
-                ("scale", _param), ("before_weight", _param), ("before_bias", _param), ("residual_out", _rows),
-                ("out", _rows)]
+_args = _raw_stream = None                      # the native marshalling; torch's current stream of a device
 
 
 def declare(lib: C.CDLL) -> None:
@@ -76,114 +44,38 @@ def declare(lib: C.CDLL) -> None:
         f.restype, f.argtypes = res, args
 
 
-# The argument blocks as they are filled here: one pack is several times as fast as a Structure's fields, and
-# a call on single tokens takes no longer on the GPU than its marshalling.
-_CONV = struct.Struct("=6i14q")
-_SCAN = struct.Struct("=6i28q")
-_NORM = struct.Struct("=4iq4i2f25q")
-assert (_CONV.size, _SCAN.size, _NORM.size) == tuple(map(C.sizeof, (mure_seq_conv_args, mure_seq_scan_args, mure_seq_norm_args)))
+def _native(lib: C.CDLL):
+    """The marshalling module, bound to the library; raises if it has not been built."""
+    global _args, _raw_stream
+    if _args is None:
+        import torch
+        try:
+            from . import _seq_args
+        except ImportError as e:
+            raise RuntimeError("_seq_args.so is missing or stale: build it first "
+                               "(python -m paper_2607_18582_amd.build)") from e
+        _seq_args.bind(*(C.cast(f, C.c_void_p).value for f in (lib.mure_seq_conv, lib.mure_seq_scan, lib.mure_seq_norm)))
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _args = _seq_args
+    return _args
 
-_NONE_ROWS, _NONE = (0, 0, 0), (0, 0)
 
-
-class _Call:
-    """The tensors of one call: their checks, the number of mutants, and the
-    order against torch's current stream."""
-
-    __slots__ = ("mure", "torch", "device", "dtype", "code", "mutants", "axis", "first")
-
-    def __init__(self, mure, first, what: str):
-        torch = self.torch = sys.modules["torch"]
-        if not isinstance(first, torch.Tensor):
-            raise TypeError(f"{what} must be a torch tensor")
-        self.mure, self.first, self.dtype, self.device = mure, first, first.dtype, first.get_device()
-        if self.device != mure.device:                 # -1: the CPU, or a planning-only context
-            raise ValueError(f"{what} is on {first.device}, the context on device {mure.device}")
-        if self.dtype is torch.bfloat16:
-            self.code = 1
-        elif self.dtype is torch.float32:
-            self.code = 0
-        else:
-            raise TypeError(f"{what} is {self.dtype}; float32 or bfloat16 is needed")
-        if not 2 <= first.dim() <= 3 or first.shape[-1] >= 1 << 31:
-            raise ValueError(f"{what} has shape {tuple(first.shape)}; [rows][channels] is needed, or that of each mutant")
-        self.mutants, self.axis = 1, False
-
-    def _check(self, t, what: str, dtype):
-        if not isinstance(t, self.torch.Tensor):
-            raise TypeError(f"{what} must be a torch tensor")
-        if t.dtype is not dtype or t.get_device() != self.device:
-            raise TypeError(f"{what} is {t.dtype} on {t.device}; {dtype} on {self.first.device} is needed")
-
-    def _mutant_axis(self, n: int, stride: int, what: str) -> int:
-        """The mutant stride of an axis of n mutants."""
-        self.axis = True
-        if n == 1:
-            return 0
-        if n == 0 or self.mutants not in (1, n):
-            raise ValueError(f"{what} has {n} mutants, another argument {self.mutants}")
-        self.mutants = n
-        return stride
-
-    def rows(self, t, what: str, rows: int, width: int, dtype=None):
-        """(address, mutant stride, row stride) of [rows][width] or that of each mutant"""
-        if t is None:
-            return _NONE_ROWS
-        self._check(t, what, dtype or self.dtype)
-        shape, stride = t.shape, t.stride()
-        if shape[-2:] != (rows, width) or len(shape) > 3:
-            raise ValueError(f"{what} has shape {tuple(shape)}; {(rows, width)} is needed, or that of each mutant")
-        if stride[-1] != 1 and width > 1:
-            raise ValueError(f"the last axis of {what} must be contiguous")
-        if len(shape) == 2:
-            return t.data_ptr(), 0, stride[0]
-        return t.data_ptr(), self._mutant_axis(shape[0], stride[0], what), stride[1]
-
-    def dense(self, t, what: str, shape: tuple, dtype=None):
-        """(address, mutant stride) of a tensor of `shape`, contiguous, or that of each mutant"""
-        if t is None:
-            return _NONE
-        self._check(t, what, dtype or self.torch.float32)
-        have, extra = t.shape, t.dim() - len(shape)
-        if not 0 <= extra <= 1 or have[extra:] != shape:
-            raise ValueError(f"{what} has shape {tuple(have)}; {shape} is needed, or that of each mutant")
-        if not t.is_contiguous() and not (extra and have[0] and t[0].is_contiguous()):
-            raise ValueError(f"{what} must be contiguous" + (" for each mutant" if extra else ""))
-        return t.data_ptr(), self._mutant_axis(have[0], t.stride(0), what) if extra else 0
-
-    def output(self, t, what: str, shape: tuple, dtype=None):
-        """t, checked, or a new tensor of the call's mutants."""
-        full = (self.mutants, *shape) if self.axis else shape
-        if t is None:
-            return self.first.new_empty(full, dtype=dtype or self.dtype)
-        self._check(t, what, dtype or self.dtype)
-        if t.shape != full:
-            raise ValueError(f"{what} has shape {tuple(t.shape)}; {full} is needed")
-        return t
-
-    def out_rows(self, t, what: str):
-        stride = t.stride()
-        if stride[-1] != 1 and t.shape[-1] > 1:
-            raise ValueError(f"the last axis of {what} must be contiguous")
-        return t.data_ptr(), stride[0] if self.axis else 0, stride[-2]
-
-    def out_dense(self, t, what: str):
-        if not t.is_contiguous() and not (self.axis and t[0].is_contiguous()):
-            raise ValueError(f"{what} must be contiguous" + (" for each mutant" if self.axis else ""))
-        return t.data_ptr(), t.stride(0) if self.axis else 0
-
-    def run(self, fn, handle, args: bytes) -> None:
-        mure, cuda = self.mure, self.torch.cuda
-        if mure.device < 0 or cuda.current_stream(self.device).cuda_stream == mure.stream:
-            status = fn(handle, args)
-        else:
-            current = cuda.current_stream(self.device)
-            own = cuda.ExternalStream(mure.stream, device=self.device) if mure.stream else cuda.default_stream(self.device)
-            own.wait_stream(current)
-            status = fn(handle, args)
-            current.wait_stream(own)
-        if status:
-            mure._check(status)
+def _call(mure, fn, *args):
+    """fn's two results, the call on the context's stream ordered with torch's current one."""
+    device = mure.device
+    if device < 0 or _raw_stream(device) == mure.stream:
+        status, a, b = fn(*args)
+    else:
+        from torch import cuda
+        current = cuda.current_stream(device)
+        own = cuda.ExternalStream(mure.stream, device=device) if mure.stream else cuda.default_stream(device)
+        own.wait_stream(current)
+        status, a, b = fn(*args)
+        current.wait_stream(own)
+    if status:
+        mure._check(status)
+    return a, b
 
 
 def _one_of(table: dict, key, what: str) -> int:
@@ -199,7 +91,7 @@ class Sequences:
     Made by ``Mure.sequences``."""
 
     def __init__(self, mure, lengths: Sequence[int]):
-        self.mure, self.handle = mure, C.c_void_p()
+        self.mure, self.handle, self.args = mure, C.c_void_p(), _native(mure.lib)
         given = np.asarray(lengths)
         if given.ndim != 1 or (given.size and given.dtype.kind not in "iu"):
             raise ValueError("lengths must be a list of whole numbers")
@@ -216,10 +108,10 @@ class Sequences:
 
     __del__ = close
 
-    def _call(self, first, what: str) -> _Call:
+    def _open(self) -> int:
         if not self.handle:
             raise ValueError("the batch is closed")
-        return _Call(self.mure, first, what)
+        return self.handle.value
 
     def conv(self, x, taps, bias=None, *, activation: Optional[str] = None, state=None, state_out=None, out=None):
         """Causal depthwise convolution along every sequence.
@@ -228,16 +120,8 @@ class Sequences:
         activation None or "silu"; state [sequences][K - 1][channels], the rows before the
         first token (zeros without it).  Returns (out, state_out), state_out being the last
         K - 1 rows of (state, x); both may be given, state_out as the state itself."""
-        c = self._call(x, "x")
-        width, K = x.shape[-1], taps.shape[-1]
-        held = (self.count, K - 1, width)
-        px, ptaps = c.rows(x, "x", self.tokens, width), c.dense(taps, "taps", (width, K), c.dtype)
-        pbias, pstate = c.dense(bias, "bias", (width,)), c.dense(state, "state", held, c.dtype)
-        out, state_out = c.output(out, "out", (self.tokens, width)), c.output(state_out, "state_out", held)
-        c.run(self.mure.lib.mure_seq_conv, self.handle,
-              _CONV.pack(c.code, c.mutants, width, K, _one_of(ACTIVATIONS, activation, "activation"), 0, *px, *ptaps, *pbias,
-                         *pstate, *c.out_dense(state_out, "state_out"), *c.out_rows(out, "out")))
-        return out, state_out
+        return _call(self.mure, self.args.conv, self._open(), self.mure.device, self.count, self.tokens, x, taps, bias,
+                     _one_of(ACTIVATIONS, activation, "activation"), state, state_out, out)
 
     def scan(self, u, dt, A, B, C_, *, skip=None, dt_bias=None, gate=None, softplus: bool = True, state=None,
              state_out=None, out=None):
@@ -247,21 +131,8 @@ class Sequences:
         [tokens][groups * states] in u's type; skip, dt_bias [channels] float32; state
         [sequences][channels][states] float32 (zeros without it).  Returns (out,
         state_out); both may be given, state_out as the state itself."""
-        c = self._call(u, "u")
-        width, N, cols, T = u.shape[-1], A.shape[-1], B.shape[-1], self.tokens
-        if N == 0 or cols % N:
-            raise ValueError(f"B has {cols} columns, no multiple of the {N} states of A")
-        held = (self.count, width, N)
-        pu, pdt, pb, pc = c.rows(u, "u", T, width), c.rows(dt, "dt", T, width), c.rows(B, "B", T, cols), c.rows(C_, "C_", T, cols)
-        pz, pa = c.rows(gate, "gate", T, width), c.dense(A, "A", (width, N))
-        pskip, pbias = c.dense(skip, "skip", (width,)), c.dense(dt_bias, "dt_bias", (width,))
-        pstate = c.dense(state, "state", held)
-        out = c.output(out, "out", (T, width))
-        state_out = c.output(state_out, "state_out", held, c.torch.float32)
-        c.run(self.mure.lib.mure_seq_scan, self.handle,
-              _SCAN.pack(c.code, c.mutants, width, N, cols // N, bool(softplus), *pu, *pdt, *pb, *pc, *pz, *pa, *pskip, *pbias,
-                         *pstate, *c.out_dense(state_out, "state_out"), *c.out_rows(out, "out")))
-        return out, state_out
+        return _call(self.mure, self.args.scan, self._open(), self.mure.device, self.count, self.tokens, u, dt, A, B, C_,
+                     skip, dt_bias, gate, bool(softplus), state, state_out, out)
 
 
 class SeqOps:
@@ -289,31 +160,7 @@ class SeqOps:
         float32 [channels] (scale may be a number).  Returns (r, before(r)), the second None
         without ``before``; residual_out = False leaves r out (None); residual_out may be the
         residual and out may be y or the gate."""
-        c = _Call(self, y, "y")
-        torch, (rows, width) = c.torch, y.shape[-2:]
-        rtype = c.dtype if residual is None else residual.dtype
-        if rtype is not c.dtype and rtype is not torch.float32:
-            raise TypeError(f"residual is {rtype}; {c.dtype} or float32 is needed")
-        if before is None and out is not None:
-            raise ValueError("out needs a `before` norm")
-        py, pz = c.rows(y, "y", rows, width), c.rows(gate, "gate", rows, width)
-        pr, w = c.rows(residual, "residual", rows, width, rtype), (width,)
-        scaled = isinstance(scale, torch.Tensor)
-        params = (*c.dense(after_weight, "after_weight", w), *c.dense(after_bias, "after_bias", w),
-                  *c.dense(scale if scaled else None, "scale", w), *c.dense(before_weight, "before_weight", w),
-                  *c.dense(before_bias, "before_bias", w))
-        pro = po = _NONE_ROWS
-        if residual_out is False:
-            residual_out = None
-        else:
-            residual_out = c.output(residual_out, "residual_out", (rows, width), rtype)
-            pro = c.out_rows(residual_out, "residual_out")
-        if before is not None:
-            out = c.output(out, "out", (rows, width))
-            po = c.out_rows(out, "out")
-        c.run(self.lib.mure_seq_norm, self.ctx,
-              _NORM.pack(c.code, 0 if rtype is torch.float32 else 1, c.mutants, width, rows,
-                         0 if gate is None else _one_of(GATES, gate_at, "gate_at"),
-                         _one_of(ACTIVATIONS, gate_activation, "gate_activation"), _one_of(NORMS, after, "after"),
-                         _one_of(NORMS, before, "before"), eps, 1.0 if scaled else scale, *py, *pz, *pr, *params, *pro, *po))
-        return residual_out, out
+        return _call(self, _native(self.lib).norm, self.ctx.value, self.device, y, residual, gate,
+                     _one_of(GATES, gate_at, "gate_at"), _one_of(ACTIVATIONS, gate_activation, "gate_activation"),
+                     _one_of(NORMS, after, "after"), after_weight, after_bias, scale, _one_of(NORMS, before, "before"),
+                     before_weight, before_bias, eps, residual_out, out)

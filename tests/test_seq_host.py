@@ -19,6 +19,41 @@ from paper_2607_18582_amd import seq as S
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
+# the argument blocks of mure_seq.h
+
+class Rows(C.Structure):                       # mure_seq_in, mure_seq_out
+    _fields_ = [("p", C.c_void_p), ("mutant_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class Param(C.Structure):                      # mure_seq_param
+    _fields_ = [("p", C.c_void_p), ("mutant_stride", C.c_int64)]
+
+
+class mure_seq_conv_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_mutants", C.c_int32), ("channels", C.c_int32), ("n_taps", C.c_int32),
+                ("activation", C.c_int32), ("reserved", C.c_int32), ("x", Rows), ("taps", C.c_void_p),
+                ("taps_mutant_stride", C.c_int64), ("bias", Param), ("state", C.c_void_p),
+                ("state_mutant_stride", C.c_int64), ("state_out", C.c_void_p),
+                ("state_out_mutant_stride", C.c_int64), ("out", Rows)]
+
+
+class mure_seq_scan_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_mutants", C.c_int32), ("channels", C.c_int32), ("states", C.c_int32),
+                ("groups", C.c_int32), ("softplus", C.c_int32), ("u", Rows), ("dt", Rows), ("b", Rows),
+                ("c", Rows), ("gate", Rows), ("a", Param), ("skip", Param), ("dt_bias", Param),
+                ("state", C.c_void_p), ("state_mutant_stride", C.c_int64), ("state_out", C.c_void_p),
+                ("state_out_mutant_stride", C.c_int64), ("out", Rows)]
+
+
+class mure_seq_norm_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("residual_dtype", C.c_int32), ("n_mutants", C.c_int32),
+                ("channels", C.c_int32), ("rows", C.c_int64), ("gate_at", C.c_int32), ("gate_activation", C.c_int32),
+                ("after", C.c_int32), ("before", C.c_int32), ("eps", C.c_float), ("scale_all", C.c_float),
+                ("y", Rows), ("gate", Rows), ("residual", Rows), ("after_weight", Param), ("after_bias", Param),
+                ("scale", Param), ("before_weight", Param), ("before_bias", Param), ("residual_out", Rows),
+                ("out", Rows)]
+
+
 @pytest.fixture()
 def mure():
     m = Mure(device=-1)
@@ -37,7 +72,7 @@ def test_library_exports_every_declared_symbol():
 
 
 def test_structures_match_the_header(tmp_path):
-    structs = [S.mure_seq_conv_args, S.mure_seq_scan_args, S.mure_seq_norm_args]
+    structs = [mure_seq_conv_args, mure_seq_scan_args, mure_seq_norm_args]
     lines, expected = [], []
     for t in structs:
         lines.append(f'printf("%zu\\n", sizeof({t.__name__}));')
@@ -67,9 +102,9 @@ def test_too_many_sequences(mure):
 
 def test_null_handles():
     lib = load_library()
-    a = S.mure_seq_conv_args()
+    a = mure_seq_conv_args()
     assert lib.mure_seq_conv(None, C.byref(a)) == MURE_E_INVALID
-    assert lib.mure_seq_norm(None, C.byref(S.mure_seq_norm_args())) == MURE_E_INVALID
+    assert lib.mure_seq_norm(None, C.byref(mure_seq_norm_args())) == MURE_E_INVALID
     out = C.c_void_p()
     lengths = (C.c_int64 * 1)(3)
     assert lib.mure_seq_create(None, 1, lengths, C.byref(out)) == MURE_E_INVALID
@@ -104,35 +139,35 @@ class Buffers:
 
 
 def conv_args(m):
-    a = S.mure_seq_conv_args(dtype=0, n_mutants=2, channels=CH, n_taps=3, activation=1)
-    a.x = S._rows(m(), 0, CH)
+    a = mure_seq_conv_args(dtype=0, n_mutants=2, channels=CH, n_taps=3, activation=1)
+    a.x = Rows(m(), 0, CH)
     a.taps = m()
-    a.bias = S._param(m(), CH)
+    a.bias = Param(m(), CH)
     a.state, a.state_mutant_stride = m(), 0
     a.state_out, a.state_out_mutant_stride = m(), 3 * 2 * CH
-    a.out = S._rows(m(), T * CH, CH)
+    a.out = Rows(m(), T * CH, CH)
     return a
 
 
 def scan_args(m):
-    a = S.mure_seq_scan_args(dtype=1, n_mutants=2, channels=CH, states=N, groups=2, softplus=1)
+    a = mure_seq_scan_args(dtype=1, n_mutants=2, channels=CH, states=N, groups=2, softplus=1)
     for name in ("u", "dt", "gate"):
-        setattr(a, name, S._rows(m(), 0, CH))
-    a.b = S._rows(m(), 0, 2 * N)
-    a.c = S._rows(m(), 0, 2 * N)
-    a.a, a.skip, a.dt_bias = (S._param(m(), 0) for _ in range(3))
+        setattr(a, name, Rows(m(), 0, CH))
+    a.b = Rows(m(), 0, 2 * N)
+    a.c = Rows(m(), 0, 2 * N)
+    a.a, a.skip, a.dt_bias = (Param(m(), 0) for _ in range(3))
     a.state_out, a.state_out_mutant_stride = m(), 3 * CH * N
-    a.out = S._rows(m(), T * CH, CH)
+    a.out = Rows(m(), T * CH, CH)
     return a
 
 
 def norm_args(m):
-    a = S.mure_seq_norm_args(dtype=1, residual_dtype=0, n_mutants=2, channels=CH, rows=T, gate_at=1, gate_activation=1, after=1,
+    a = mure_seq_norm_args(dtype=1, residual_dtype=0, n_mutants=2, channels=CH, rows=T, gate_at=1, gate_activation=1, after=1,
                              before=2, eps=1e-5, scale_all=1.0)
-    a.y, a.gate = S._rows(m(), T * CH, CH), S._rows(m(), 0, CH)
-    a.residual = S._rows(m(), 0, CH)
-    a.after_weight, a.before_bias = S._param(m(), 0), S._param(m(), CH)
-    a.residual_out, a.out = S._rows(m(), T * CH, CH), S._rows(m(), T * CH, CH)
+    a.y, a.gate = Rows(m(), T * CH, CH), Rows(m(), 0, CH)
+    a.residual = Rows(m(), 0, CH)
+    a.after_weight, a.before_bias = Param(m(), 0), Param(m(), CH)
+    a.residual_out, a.out = Rows(m(), T * CH, CH), Rows(m(), T * CH, CH)
     return a
 
 
@@ -286,8 +321,9 @@ def test_binding_refusals(mure):
     bad(ValueError, x, taps, out=torch.zeros(7, 9))
     bad(ValueError, x, torch.zeros(2, 8, 4), out=torch.zeros(7, 8))
     bad(ValueError, x, taps, state_out=torch.zeros(2, 8, 3).transpose(1, 2))
-    with pytest.raises(MureError, match="planning-only"):
-        seqs.conv(x, taps)
+    for K in (1, 4):                            # one tap: states without rows
+        with pytest.raises(MureError, match="planning-only"):
+            seqs.conv(x, torch.zeros(8, K))
     with pytest.raises(MureError, match="n_taps"):
         seqs.conv(x, torch.zeros(8, 9))
     u, b = torch.zeros(7, 8), torch.zeros(7, 6)

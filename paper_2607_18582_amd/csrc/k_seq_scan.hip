@@ -53,6 +53,20 @@ __device__ __forceinline__ float quad_xor2(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4e, 0xf, 0xf, true));
 }
 
+// Lane j of each quad receives the quad's sum of its p[j].
+__device__ __forceinline__ float quad_sums(float p0, float p1, float p2, float p3, int q) {
+  const bool odd = q & 1, high = q & 2;
+  const float a = (odd ? p1 : p0) + quad_xor1(odd ? p0 : p1);
+  const float b = (odd ? p3 : p2) + quad_xor1(odd ? p2 : p3);
+  return (high ? b : a) + quad_xor2(high ? a : b);
+}
+
+// The decay of a state over tokens whose steps sum to d.  Not below the
+// smallest positive float: an infinite state stays infinite, as it does when
+// it decays token by token.
+__device__ __forceinline__ float no_zero(float p) { return p < 1.4012985e-45f ? 1.4012985e-45f : p; }
+__device__ __forceinline__ float decay(float al, float d) { return no_zero(__builtin_amdgcn_exp2f(al * d)); }
+
 // Q: states per lane (4 Q in all); PAD: some of them are past N.
 // KIND: RUNS; ENDS, only the state that a run reaches from zero; STEPS, runs of
 // fewer than four tokens all, which need no LDS and half the registers.
@@ -148,7 +162,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
 
   float sum_d = 0.f;                                   // of this lane's tokens
   // token J of the quad's four, with D in dv's lane J and D u in du's
-  auto step = [&](auto jc, float dv, float du, vq bv, vq cv, float& yq) {
+  auto step = [&](auto jc, float dv, float du, vq bv, vq cv) {
     constexpr int J = decltype(jc)::value;
     const float dj = quad_bcast<J>(dv), duj = quad_bcast<J>(du);
     float p = 0.f;
@@ -157,11 +171,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
       h[i] = fmaf(__builtin_amdgcn_exp2f(dj * al[i]), h[i], duj * bv[i]);
       if (!ENDS) p = fmaf(cv[i], PAD && q * Q + i >= N ? 0.f : h[i], p);
     }
-    if (!ENDS) {
-      p += quad_xor1(p);
-      p += quad_xor2(p);
-      yq = q == J ? p : yq;
-    }
+    return p;
   };
   auto prepare = [&](float dv, float uv, float& du) {
     dv += bias;
@@ -184,13 +194,15 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
   // the run's last one to three tokens, with their rows of b and c
   auto last = [&](int t0, int left, T fu, T fd, T fz, auto brow, auto crow) {
     const float uv = to_f<T>(fu);
-    float du, yq = 0.f;
+    float du;
     const float dv = prepare(to_f<T>(fd), uv, du);
     const vq b0 = brow(0), c0 = ENDS ? b0 : crow(0), b1 = brow(min(1, left - 1)), c1 = ENDS ? b1 : crow(min(1, left - 1)),
              b2 = brow(left - 1), c2 = ENDS ? b2 : crow(left - 1);
-    step(J0(), dv, du, b0, c0, yq);
-    if (left > 1) step(J1(), dv, du, b1, c1, yq);
-    if (left > 2) step(J2(), dv, du, b2, c2, yq);
+    const float p0 = step(J0(), dv, du, b0, c0);
+    float p1 = 0.f, p2 = 0.f;
+    if (left > 1) p1 = step(J1(), dv, du, b1, c1);
+    if (left > 2) p2 = step(J2(), dv, du, b2, c2);
+    const float yq = ENDS ? 0.f : quad_sums(p0, p1, p2, 0.f, q);
     if (q >= left) return;
     if (ENDS) sum_d += dv;
     else store_row(t0, finish(yq, uv, to_f<T>(fz)));
@@ -212,13 +224,14 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
       for (int g = 0; g < GROUPS; ++g) {
         if (4 * g + 4 > count) break;
         const float uv = to_f<T>(ru[g]), zv = gated ? to_f<T>(rz[g]) : 0.f;
-        float du, yq = 0.f;
+        float du;
         const float dv = prepare(to_f<T>(rd[g]), uv, du);
         fetch_group(t1, more, g);
-        step(J0(), dv, du, row(bt, 4 * g), row(ct, 4 * g), yq);
-        step(J1(), dv, du, row(bt, 4 * g + 1), row(ct, 4 * g + 1), yq);
-        step(J2(), dv, du, row(bt, 4 * g + 2), row(ct, 4 * g + 2), yq);
-        step(J3(), dv, du, row(bt, 4 * g + 3), row(ct, 4 * g + 3), yq);
+        const float p0 = step(J0(), dv, du, row(bt, 4 * g), row(ct, 4 * g));
+        const float p1 = step(J1(), dv, du, row(bt, 4 * g + 1), row(ct, 4 * g + 1));
+        const float p2 = step(J2(), dv, du, row(bt, 4 * g + 2), row(ct, 4 * g + 2));
+        const float p3 = step(J3(), dv, du, row(bt, 4 * g + 3), row(ct, 4 * g + 3));
+        const float yq = ENDS ? 0.f : quad_sums(p0, p1, p2, p3, q);
         if (ENDS) sum_d += dv;
         else store_row(t0 + 4 * g, finish(yq, uv, zv));
       }
@@ -285,13 +298,13 @@ __global__ __launch_bounds__(256) void seq_scan_join_kernel(SeqScanArgs k, DivU3
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         ws[(j + i) * DN] = h;
-        h = fmaf(__builtin_amdgcn_exp2f(s[i] * al), h, end[i]);
+        h = fmaf(decay(al, s[i]), h, end[i]);
       }
     }
     for (; j + 1 < ch.n; ++j) {
       const float end = ws[j * DN];
       ws[j * DN] = h;
-      h = fmaf(__builtin_amdgcn_exp2f(sd[(int64_t)j * D] * al), h, end);
+      h = fmaf(decay(al, sd[(int64_t)j * D]), h, end);
     }
     ws[j * DN] = h;
   }

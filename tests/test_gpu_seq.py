@@ -434,3 +434,56 @@ def test_drawn_sizes(mure, seed):
     ey, el = R.conv(x, taps, b, lengths, "silu", st)
     R.close(y, ey, "conv")
     assert torch.equal(last.cpu().double(), el[0])
+
+
+@pytest.mark.parametrize("dtype,lengths,D,N,G,state", [
+    ("f32", [513, 1030, 3], 2048, 16, 1, True), ("bf16", [700, 512, 0, 1500], 1024, 16, 1, False),
+    ("bf16", [1024, 2048], 2052, 5, 4, True), ("f32", [530], 1100, 3, 1, True), ("f32", [600], 2050, 20, 1, True)])
+def test_scan_of_wide_layers(mure, dtype, lengths, D, N, G, state):
+    """Long sequences of wide layers; a few channels are compared."""
+    say(f"[scan wide] {dtype} {lengths} D={D} N={N}")
+    p = scan_inputs(20, lengths, D, N, TYPES[dtype], G, state=state)
+    p["A"][0, 1] = float("-inf")
+    y, last = run_scan(mure.sequences(lengths), p)
+    # per group: the first channels, some in the middle and the last
+    width = D // G
+    some = torch.tensor(sorted({g * width + c for g in range(G) for c in (0, 1, 2, 63, 64, width // 2, width - 2, width - 1)}))
+    cut = lambda v, axis: None if v is None else v.index_select(axis, some)  # noqa: E731
+    gid = some // width
+    spread = lambda v: v.view(1, -1, G, N)[:, :, gid].reshape(1, -1, len(some) * N)  # noqa: E731
+    ey, el = R.scan(cut(p["u"], 2), cut(p["dt"], 2), cut(p["A"], 1), spread(p["B"]), spread(p["C"]), lengths, cut(p["skip"], 1),
+                    cut(p["dt_bias"], 1), cut(p["gate"], 2), True, cut(p["state"], 2))
+    say("   worst:", R.close(y[:, :, some.cuda()], ey, "out"), R.close(last[:, :, some.cuda()], el, "state"))
+
+
+def test_wide_layers_do_not_depend_on_the_batch(mure):
+    say("[scan wide batch]")
+    lengths, D, N, M = [520, 20, 1300], 2048, 16, 2
+    p = scan_inputs(21, lengths, D, N, torch.bfloat16, M=M, own=True, mutated=True, state=True)
+    q = {k: None if v is None else v.cuda() for k, v in p.items()}
+    y, last = run_scan(mure.sequences(lengths), p)
+    row = 0
+    for i, n in enumerate(lengths):
+        cut, m = slice(row, row + n), (i + 1) % M
+        held = q["state"][m, i:i + 1].clone()
+        ys, ls = mure.sequences([n]).scan(q["u"][m, cut], q["dt"][m, cut], q["A"][m], q["B"][m, cut], q["C"][m, cut], skip=q["skip"][m],
+                                          dt_bias=q["dt_bias"][m], gate=q["gate"][m, cut], state=held, state_out=held)
+        assert torch.equal(ys, y[m, cut]) and torch.equal(ls[0], last[m, i])
+        row += n
+
+
+@pytest.mark.parametrize("D", [16, 1024, 2048])
+def test_infinite_states_of_long_sequences(mure, D):
+    """An infinite state stays infinite over spans in which any finite one decays to nothing, as token by token."""
+    say(f"[scan inf long] D={D}")
+    lengths, N = [1300], 16
+    p = scan_inputs(22, lengths, D, N, torch.float32)
+    p["B"], p["C"], p["skip"], p["gate"] = p["B"].abs() + 0.1, p["C"].abs() + 0.1, p["skip"].abs(), None
+    p["dt"][0, :, 3] += 8                       # steps of some 5: a decay of e^-80 a token for the last state
+    p["u"][0, 100, 3] = float("inf")
+    p["u"][0, 700, 5] = float("nan")
+    y, last = run_scan(mure.sequences(lengths), p)
+    assert bool(torch.isposinf(y[0, 100:, 3]).all()) and bool(torch.isposinf(last[0, 0, 3]).all())
+    assert bool(torch.isnan(y[0, 700:, 5]).all()) and bool(torch.isfinite(y[0, :700, 5]).all())
+    rest = [c for c in range(D) if c not in (3, 5)]
+    assert bool(torch.isfinite(y[0][:, rest]).all()) and bool(torch.isfinite(last[0, 0][rest]).all())

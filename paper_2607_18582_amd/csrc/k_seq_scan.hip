@@ -30,16 +30,14 @@ namespace mure {
 constexpr int TILE = 16;                               // tokens whose b and c stand in LDS
 constexpr float LOG2E = 1.44269504088896340736f;
 
-// log(1 + e^s) = max(s, 0) + log1p(e^-|s|), and with e = e^-|s| and w = 1 + e
-// rounded, log1p(e) = log(w) e / (w - 1), or e where w = 1 (D. Goldberg, "What
-// every computer scientist should know about floating-point arithmetic", ACM
-// Computing Surveys 23 (1991), Theorem 4): the error in w cancels.  The
-// hardware's logarithm and reciprocal are within a unit or two.
+// log(1 + e^s) = max(s, 0) + log(1 + e) with e = e^-|s|.  Of a small e the sum
+// w = 1 + e keeps only some bits; what it loses is r = e - (w - 1), exactly,
+// and log(1 + e) = log(w) + log(1 + r / w) = log(w) + r to the float's
+// precision: r is below 2^-24, and w is near 1 wherever r counts.
 __device__ __forceinline__ float softplus(float s) {
   const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(s));
-  const float w = 1.f + e, d = w - 1.f;
-  const float p = __builtin_amdgcn_logf(w) * ((1.f / LOG2E) * e) * __builtin_amdgcn_rcpf(d);
-  return fmaxf(s, 0.f) + (d == 0.f ? e : p);
+  const float w = 1.f + e, r = e - (w - 1.f);
+  return __builtin_amdgcn_fmed3f(s, 0.f, __builtin_inff()) + fmaf(1.f / LOG2E, __builtin_amdgcn_logf(w), r);
 }
 
 // Lane j's value of every quad, in all its lanes.
@@ -277,10 +275,12 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
   }
 }
 
+constexpr int JOIN = 64;                               // one wave a block: a long prompt of 2048 channels has 512 of them
+
 // The chunks' first states from their states from zero, in place.
-__global__ __launch_bounds__(256) void seq_scan_join_kernel(SeqScanArgs k, DivU32 dn) {
+__global__ __launch_bounds__(JOIN) void seq_scan_join_kernel(SeqScanArgs k, DivU32 dn) {
   const mure_seq_scan_args& a = k.a;
-  const uint32_t e = blockIdx.x * 256u + threadIdx.x;
+  const uint32_t e = blockIdx.x * (unsigned)JOIN + threadIdx.x;
   const int D = a.channels, N = a.states;
   if (e >= (uint32_t)D * (uint32_t)N) return;
   const int64_t m = blockIdx.z, d = divu(dn, e), DN = (int64_t)D * N;
@@ -290,23 +290,34 @@ __global__ __launch_bounds__(256) void seq_scan_join_kernel(SeqScanArgs k, DivU3
     float h = a.state ? a.state[m * a.state_mutant_stride + ch.seq * DN + e] : 0.f;
     float* ws = k.ws_h + (m * k.n_slots + ch.slot0) * DN + e;
     const float* sd = k.ws_d + (m * k.n_slots + ch.slot0) * D + d;
-    int j = 0;
-    for (; j + 8 < ch.n; j += 8) {                     // eight chunks' loads at a time
-      float end[8], s[8];
+    // AHEAD chunks are loaded at a time, ahead of those being joined.  The last chunk has no state from zero, and none
+    // is used.
+    constexpr int AHEAD = 8;
+    float end[AHEAD], s[AHEAD];
+    const float* at = ws;
+    auto load = [&](int n) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) end[i] = ws[(j + i) * DN], s[i] = sd[(int64_t)(j + i) * D];
+      for (int i = 0; i < AHEAD; ++i)
+        if (i < n) end[i] = at[i * DN], s[i] = sd[i * (int64_t)D];
+      at += AHEAD * DN;
+      sd += AHEAD * (int64_t)D;
+    };
+    auto join = [&](int n, int more) {                 // n chunks, and the loads of `more` after them
+      float e[AHEAD], f[AHEAD];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        ws[(j + i) * DN] = h;
-        h = fmaf(decay(al, s[i]), h, end[i]);
+      for (int i = 0; i < AHEAD; ++i) e[i] = end[i], f[i] = decay(al, s[i]);
+      load(more);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        if (i < n) ws[i * DN] = h;
+        h = fmaf(f[i], h, e[i]);
       }
-    }
-    for (; j + 1 < ch.n; ++j) {
-      const float end = ws[j * DN];
-      ws[j * DN] = h;
-      h = fmaf(decay(al, sd[(int64_t)j * D]), h, end);
-    }
-    ws[j * DN] = h;
+      ws += AHEAD * DN;
+    };
+    int left = ch.n;
+    load(min(AHEAD, left - 1));
+    for (; left > 2 * AHEAD; left -= AHEAD) join(AHEAD, AHEAD);
+    for (; left > 0; left -= AHEAD) join(left, left - AHEAD - 1);
   }
 }
 
@@ -353,7 +364,7 @@ hipError_t launch_seq_scan_ends(const SeqScanArgs& k, hipStream_t s) { return sc
 
 hipError_t launch_seq_scan_join(const SeqScanArgs& k, hipStream_t s) {
   const int64_t DN = (int64_t)k.a.channels * k.a.states;
-  seq_scan_join_kernel<<<dim3((unsigned)((DN + 255) / 256), (unsigned)std::min(k.n_chunked, 65535), (unsigned)k.a.n_mutants), 256, 0,
+  seq_scan_join_kernel<<<dim3((unsigned)((DN + JOIN - 1) / JOIN), (unsigned)std::min(k.n_chunked, 65535), (unsigned)k.a.n_mutants), JOIN, 0,
                          s>>>(k, make_divu32((uint32_t)k.a.states));
   return hipGetLastError();
 }

@@ -190,6 +190,14 @@ void check_device(int device) {
 
 // ---- batches
 
+// Sequence i's runs of at most `run` tokens, its chunks in the workspace from
+// `slot` on (or -1); a sequence without tokens has one empty run.
+void add_runs(std::vector<SeqItem>& to, int32_t i, int64_t row, int64_t length, int64_t run, int64_t slot) {
+  for (int64_t t = 0; t == 0 || t < length; t += run)
+    to.push_back({i, (int32_t)(row + t), (int32_t)std::min(run, length - t), (int32_t)t, (int32_t)length,
+                  slot < 0 ? -1 : (int32_t)(slot + t / run)});
+}
+
 void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out) {
   if (!out) invalid("out is NULL");
   *out = nullptr;
@@ -213,24 +221,23 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
   int64_t row = 0, slots = 0;
   for (int32_t i = 0; i < (int32_t)n_seq; ++i) {
     const int64_t L = lengths[i];
-    // runs of at most `run` tokens; a sequence without tokens has one empty run
-    auto runs = [&](std::vector<SeqItem>& v, int64_t run, int64_t slot) {
-      for (int64_t t = 0; t == 0 || t < L; t += run)
-        v.push_back({i, (int32_t)(row + t), (int32_t)std::min(run, L - t), (int32_t)t, (int32_t)L,
-                     slot < 0 ? -1 : (int32_t)(slot + t / run)});
-    };
-    for (int k = 0; k < N_RUNS; ++k) runs(conv[k], CONV_RUNS[k], -1);
     if (L <= MURE_SEQ_SPLIT_TOKENS) {
-      runs(scan, MURE_SEQ_SPLIT_TOKENS, -1);
+      add_runs(scan, i, row, L, MURE_SEQ_SPLIT_TOKENS, -1);
     } else {
       const int64_t n = (L + SCAN_CHUNK - 1) / SCAN_CHUNK;
       const size_t first = scan.size();
-      runs(scan, SCAN_CHUNK, slots);
+      add_runs(scan, i, row, L, SCAN_CHUNK, slots);
       ends.insert(ends.end(), scan.begin() + first, scan.end() - 1);
       chunked.push_back({i, (int32_t)slots, (int32_t)n});
       slots += n;
     }
     row += L;
+  }
+  // the convolution's runs: shorter ones only where a layer may take them (mure_seq_conv)
+  for (int k = 0; k < N_RUNS; ++k) {
+    if (k && conv[k - 1].size() >= (k == 1 ? 1u << 17 : 1u << 15)) break;
+    row = 0;
+    for (int32_t i = 0; i < (int32_t)n_seq; row += lengths[i++]) add_runs(conv[k], i, row, lengths[i], CONV_RUNS[k], -1);
   }
   // the longest first, so that a launch does not end with one long run
   std::stable_sort(scan.begin(), scan.end(), [](const SeqItem& a, const SeqItem& b) { return a.len > b.len; });
@@ -305,7 +312,11 @@ void conv(mure_seq* s, const mure_seq_conv_args* args) {
   // and 1536 bfloat16 channels take 24.4 us in runs of 16 (230 thousand threads) and 27 in runs of 32 or 8; 65536
   // tokens of 4096 channels 204 us in runs of 32 and 209 in runs of 16.
   const int64_t vecs = (C * es + 15) / 16 * M;
-  const int w = s->n_conv[0] * vecs >= 1 << 17 ? 0 : s->n_conv[1] * vecs >= 1 << 15 ? 1 : 2;
+  // A run reads the state for rows before the sequence, and the sequence's first run may overwrite it: every other
+  // run starts n_taps - 1 rows in, or later.
+  static_assert(CONV_RUNS[1] >= MURE_SEQ_MAX_TAPS - 1, "");
+  const bool shortest = s->n_conv[2] && s->n_conv[1] * vecs < 1 << 15 && CONV_RUNS[2] >= K - 1;
+  const int w = !s->n_conv[1] || s->n_conv[0] * vecs >= 1 << 17 ? 0 : shortest ? 2 : 1;
   k.items = s->conv[w];
   k.n_items = s->n_conv[w];
   check(launch_seq_conv(k, s->stream), "mure_seq_conv");
@@ -356,8 +367,8 @@ void scan(mure_seq* s, const mure_seq_scan_args* args) {
     const wide need = (wide)M * s->n_slots * D * (N + 1) * 4;
     if (need > MOST) throw Fail{MURE_E_NOMEM, "sequence workspace"};
     if (s->work.empty() || s->work.back().bytes < (size_t)need) {
-      Mem m;
-      m.alloc((size_t)need);
+      Mem m;                                   // twice the last: those that stay are no more than the largest
+      m.alloc(std::max((size_t)need, s->work.empty() ? 0 : 2 * s->work.back().bytes));
       s->work.push_back(std::move(m));
     }
     k.ws_h = static_cast<float*>(s->work.back().p);

@@ -5,6 +5,7 @@
 //
 // The library stays free of torch: its entry points come in as addresses
 // (bind), and only this module, used by seq.py, knows tensors.
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -36,7 +37,10 @@ std::string type_and_place(const at::Tensor& t) { return std::string(c10::toStri
 
 const at::Tensor& tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) raise(PyExc_TypeError, std::string(what) + " must be a torch tensor");
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && at::GradMode::is_enabled())
+    raise(PyExc_ValueError, std::string(what) + " requires a gradient, which no operator here has: call under torch.no_grad()");
+  return t;
 }
 
 int64_t whole(PyObject* o) {

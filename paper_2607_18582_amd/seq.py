@@ -10,6 +10,8 @@ Argument marshalling only, as in ``binding.py``, the tensors' part of it in C++
 mutant axis or none.  A size-1 or expanded (stride 0) mutant axis counts as
 shared.  Rows may be strided (slices of a projection's output); a row's
 channels are contiguous.  Results have a mutant axis when any argument has.
+There are no gradients: a tensor that requires one is refused outside
+``torch.no_grad()``.
 
 The library enqueues on its context's stream.  Where another stream is
 current in torch, the call is ordered after that stream's work and that stream
@@ -160,6 +162,8 @@ class SeqOps:
         float32 [channels] (scale may be a number).  Returns (r, before(r)), the second None
         without ``before``; residual_out = False leaves r out (None); residual_out may be the
         residual and out may be y or the gate."""
+        if not self.ctx:
+            raise ValueError("the context is closed")
         return _call(self, _native(self.lib).norm, self.ctx.value, self.device, y, residual, gate,
                      _one_of(GATES, gate_at, "gate_at"), _one_of(ACTIVATIONS, gate_activation, "gate_activation"),
                      _one_of(NORMS, after, "after"), after_weight, after_bias, scale, _one_of(NORMS, before, "before"),

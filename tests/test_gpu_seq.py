@@ -85,6 +85,21 @@ def test_conv_resumed_is_the_whole(mure, dtype):
     assert torch.equal(state, last)
 
 
+@pytest.mark.parametrize("K", range(2, 9))
+def test_conv_updates_states_in_place(mure, K):
+    """Short sequences of every number of taps: every run has read the old state before it is overwritten."""
+    say(f"[conv in place] K={K}")
+    lengths, C = [11, 1, 8, 0, 3, 40, 4, 5], 24
+    x, taps, b, st = conv_inputs(K, lengths, C, K, torch.bfloat16, state=True)
+    seqs = mure.sequences(lengths)
+    y, last = seqs.conv(*cuda(x, taps, b), state=st.cuda())
+    R.close(y, R.conv(x, taps, b, lengths, None, st)[0], "out")
+    for _ in range(20):
+        held = st.cuda()
+        y2, same = seqs.conv(*cuda(x, taps, b), state=held, state_out=held)
+        assert same is held and torch.equal(y2, y) and torch.equal(held, last)
+
+
 def test_conv_strided_views(mure):
     """Rows that are slices of wider ones, at odd addresses, in and out, and an expanded mutant axis."""
     say("[conv strided]")

@@ -119,6 +119,8 @@ def test_batches_close_with_their_context():
     s.close()
     with pytest.raises(ValueError, match="closed"):
         s.conv(torch.zeros(7, 4), torch.zeros(4, 2))
+    with pytest.raises(ValueError, match="closed"):
+        m.block_norm(torch.zeros(7, 4), before="rms")
 
 
 # ---- the C interface's own checks
@@ -321,6 +323,9 @@ def test_binding_refusals(mure):
     bad(ValueError, x, taps, out=torch.zeros(7, 9))
     bad(ValueError, x, torch.zeros(2, 8, 4), out=torch.zeros(7, 8))
     bad(ValueError, x, taps, state_out=torch.zeros(2, 8, 3).transpose(1, 2))
+    bad(ValueError, x, taps.clone().requires_grad_())
+    with torch.no_grad(), pytest.raises(MureError, match="planning-only"):
+        seqs.conv(x, taps.clone().requires_grad_())
     for K in (1, 4):                            # one tap: states without rows
         with pytest.raises(MureError, match="planning-only"):
             seqs.conv(x, torch.zeros(8, K))

@@ -1,13 +1,18 @@
 // Causal depthwise convolution along the sequences of a batch:
 //   y[t][c] = act(b[c] + sum_k w[c][k] x[t - K + 1 + k][c]).
 //
-// 2 K operations for 2 elements moved: bound by HBM.  A thread owns 16 bytes
+// 2 K operations for 2 elements moved: bound by HBM (65536 x 4096 bfloat16, 4
+// taps: 203 us, 5.3 TB/s; a copy of as much takes 200).  A thread owns 16 bytes
 // of channels (8 bfloat16, 4 float32) of one run of consecutive tokens; the
 // last K - 1 rows stay in its registers, so that a row is read once, but for
 // the K - 1 rows before the run, which the run before reads too.  Rows are
-// loaded ROWS at a time, ahead of their use, to keep several loads in flight.
+// taken ROWS at a time: three keep 3 waves a SIMD at 4 taps of bfloat16, with
+// four the float32 kernel waits longer (250 sequences of 16 mutants 24.7 us,
+// now 21.3).  The activation and odd widths are instances of their own: as
+// branches in the row they cost a quarter of the smallest calls' time.
 // Widths that fill no whole vector: the last vector of a row starts early (its
-// first `dup` channels are the neighbour's and are not stored).
+// first `dup` channels are the neighbour's and are not stored); vectors then
+// stand at any address, which costs up to a fifth of the bandwidth.
 #include <algorithm>
 
 #include "seq_dev.hpp"
@@ -35,9 +40,10 @@ template <typename T> struct Bits<T, 1> {
   static __device__ __forceinline__ void store_from(T* p, one v, int) { *p = v; }
 };
 
-template <typename T, int K, int N>
+// SILU: the activation; ODD: the last vector of a row starts early
+template <typename T, int K, int N, bool SILU, bool ODD>
 __global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dvec, uint32_t total) {
-  constexpr int ROWS = 4, H = K - 1;
+  constexpr int ROWS = 3, H = K - 1;
   const mure_seq_conv_args& a = k.a;
   const uint32_t id = blockIdx.x * 256u + threadIdx.x;
   if (id >= total) return;
@@ -47,7 +53,7 @@ __global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dve
   const int64_t m = blockIdx.y;
   const int C = a.channels;
   int c = v * N, dup = 0;
-  if (c + N > C) dup = c + N - C, c = C - N;           // N == 1 where C < the vector
+  if (ODD && c + N > C) dup = c + N - C, c = C - N;    // N == 1 where C < the vector
   const T* x = static_cast<const T*>(a.x.p) + m * a.x.mutant_stride + (int64_t)it.row0 * a.x.row_stride + c;
   T* y = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (int64_t)it.row0 * a.out.row_stride + c;
   const int64_t held = (int64_t)it.seq * H * C + c;    // of this sequence's state
@@ -89,49 +95,64 @@ __global__ __launch_bounds__(256) void seq_conv_kernel(SeqConvArgs k, DivU32 dve
       if (pos >= 0) keep[j] = Bits<T, N>::load(x + (int64_t)pos * a.x.row_stride);
       else if (st) keep[j] = Bits<T, N>::load(st + (int64_t)(H + pos) * C);
     }
-  for (int t = 0; t < it.len; t += ROWS) {
+  auto rows = [&](int t, auto whole) {                 // ROWS of them, or what is left
+    constexpr bool WHOLE = decltype(whole)::value;
+    const T* from = x + (int64_t)t * a.x.row_stride;
 #pragma unroll
-    for (int u = 0; u < ROWS; ++u)                     // rows past the run repeat its last one; they are not stored
-      load_n<T, N>(x + (int64_t)min(t + u, it.len - 1) * a.x.row_stride, r[H + u]);
+    for (int u = 0; u < ROWS; ++u)
+      if (WHOLE || t + u < it.len) load_n<T, N>(from + u * a.x.row_stride, r[H + u]);
+    T* to = y + (int64_t)t * a.out.row_stride;
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
+      if (!WHOLE && t + u >= it.len) break;
       float s[N];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         s[j] = b[j];
 #pragma unroll
         for (int i = 0; i < K; ++i) s[j] = fmaf(w[i][j], r[u + i][j], s[j]);
-        if (a.activation == MURE_SEQ_SILU) s[j] = seq_silu(s[j]);
+        if (SILU) s[j] = seq_silu(s[j]);
       }
-      if (t + u < it.len) store_from<T, N>(y + (int64_t)(t + u) * a.out.row_stride, s, dup);
+      store_from<T, N>(to + u * a.out.row_stride, s, ODD ? dup : 0);
     }
 #pragma unroll
     for (int i = 0; i < H; ++i)
 #pragma unroll
       for (int j = 0; j < N; ++j) r[i][j] = r[ROWS + i][j];
-  }
+  };
+  int t = 0;
+  for (; t + ROWS <= it.len; t += ROWS) rows(t, std::true_type());
+  if (t < it.len) rows(t, std::false_type());
   if (carry) {
     T* so = static_cast<T*>(a.state_out) + m * a.state_out_mutant_stride + held;
 #pragma unroll
-    for (int j = 0; j < H; ++j) Bits<T, N>::store_from(so + (int64_t)j * C, keep[j], dup);
+    for (int j = 0; j < H; ++j) Bits<T, N>::store_from(so + (int64_t)j * C, keep[j], ODD ? dup : 0);
   }
 }
 
-template <typename T, int K, int N>
+template <typename T, int K, int N, bool SILU, bool ODD>
 static hipError_t conv_n(SeqConvArgs k, hipStream_t s) {
   const int vecs = (k.a.channels + N - 1) / N;
   const int most = (1 << 30) / vecs;                   // items of a launch: its grid has fewer than 2^32 threads
   for (int left = k.n_items; left > 0; left -= most, k.item0 += most) {
     const uint32_t total = (uint32_t)std::min(left, most) * (uint32_t)vecs;
-    seq_conv_kernel<T, K, N><<<dim3((total + 255) / 256, (unsigned)k.a.n_mutants), 256, 0, s>>>(k, make_divu32((uint32_t)vecs), total);
+    seq_conv_kernel<T, K, N, SILU, ODD><<<dim3((total + 255) / 256, (unsigned)k.a.n_mutants), 256, 0, s>>>(
+        k, make_divu32((uint32_t)vecs), total);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
+template <typename T, int K, bool SILU>
+static hipError_t conv_v(const SeqConvArgs& k, hipStream_t s) {
+  constexpr int N = Vec<T>::N;
+  if (k.a.channels < N) return conv_n<T, K, 1, SILU, false>(k, s);
+  return k.a.channels % N ? conv_n<T, K, N, SILU, true>(k, s) : conv_n<T, K, N, SILU, false>(k, s);
+}
+
 template <typename T, int K>
 static hipError_t conv_k(const SeqConvArgs& k, hipStream_t s) {
-  return k.a.channels >= Vec<T>::N ? conv_n<T, K, Vec<T>::N>(k, s) : conv_n<T, K, 1>(k, s);
+  return k.a.activation == MURE_SEQ_SILU ? conv_v<T, K, true>(k, s) : conv_v<T, K, false>(k, s);
 }
 
 template <typename T>

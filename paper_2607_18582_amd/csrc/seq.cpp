@@ -233,7 +233,7 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
     }
     row += L;
   }
-  // the convolution's runs: shorter ones only where a layer may take them (mure_seq_conv)
+  // the convolution's runs: shorter ones only where a layer may take them (conv below)
   for (int k = 0; k < N_RUNS; ++k) {
     if (k && conv[k - 1].size() >= (k == 1 ? 1u << 17 : 1u << 15)) break;
     row = 0;
@@ -307,10 +307,10 @@ void conv(mure_seq* s, const mure_seq_conv_args* args) {
     if (meet(so, out)) invalid("state_out overlaps out");
   }
   check_device(s->device);
-  // Long runs read fewer rows twice (at 4 taps 3 of 35, 19 and 7), short ones give more threads (of 16 bytes of
+  // Long runs read fewer rows twice (at 4 taps 3 of 36, 15 and 6), short ones give more threads (of 16 bytes of
   // channels): the longest is taken that fills the chip, or the next that comes near it.  24 prompts of 18865 tokens
-  // and 1536 bfloat16 channels take 24.4 us in runs of 16 (230 thousand threads) and 27 in runs of 32 or 8; 65536
-  // tokens of 4096 channels 204 us in runs of 32 and 209 in runs of 16.
+  // and 1536 bfloat16 channels take 25.0 us in runs of 12 and 26.9 in runs of 32; 65536 tokens of 4096 channels 203 us
+  // in runs of 33 and 209 in runs of 16.
   const int64_t vecs = (C * es + 15) / 16 * M;
   // A run reads the state for rows before the sequence, and the sequence's first run may overwrite it: every other
   // run starts n_taps - 1 rows in, or later.

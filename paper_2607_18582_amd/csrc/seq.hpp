@@ -29,7 +29,7 @@ struct SeqChunks {
 };
 
 constexpr int SCAN_CHUNK = 128;                // tokens of a chunk
-constexpr int CONV_RUNS[] = {32, 16, 4};       // tokens of a convolution's runs
+constexpr int CONV_RUNS[] = {33, 12, 3};       // tokens of a convolution's runs
 constexpr int N_RUNS = 3;
 
 struct SeqConvArgs {

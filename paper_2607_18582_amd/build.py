@@ -45,7 +45,8 @@ def hipcc() -> str:
 
 
 def sources(d: str = CSRC):
-    return sorted(os.path.join(d, f) for f in os.listdir(d)
+    """The compiled sources of d and its subfolders; their names differ."""
+    return sorted(os.path.join(at, f) for at, _, files in os.walk(d) for f in files
                   if f.endswith((".hip", ".cpp")))
 
 

@@ -20,7 +20,7 @@
 #include "kernels.hpp"
 #include "plan.hpp"
 #include "run.hpp"
-#include "seq.hpp"
+#include "seq/seq.hpp"
 
 using namespace mure;
 

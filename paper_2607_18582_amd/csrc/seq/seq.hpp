@@ -6,8 +6,8 @@
 #include <cstdint>
 #include <string>
 
-#include "../../include/mure_seq.h"
-#include "kernels.hpp"
+#include "../../../include/mure_seq.h"
+#include "../kernels.hpp"
 
 namespace mure {
 

@@ -2,7 +2,7 @@
 // alignment, activations.
 #pragma once
 
-#include "dev.hpp"
+#include "../dev.hpp"
 #include "seq.hpp"
 
 namespace mure {

@@ -21,6 +21,11 @@
 // computes the chunks' states from zero and their sums of D (seq_scan_kernel,
 // ENDS), one walks the chunks of every channel and state (seq_scan_join_kernel)
 // and one computes the outputs from the chunks' first states.
+//
+// 32768 tokens of 2048 channels and 16 states, bfloat16: 197, 21 and 270 us.
+// The two scans keep the vector ALU busy all the time: of the second one's 122
+// instructions per quad and four tokens 80 are the recurrence, and the 20
+// transcendental ones take two slots.
 #include <algorithm>
 
 #include "seq_dev.hpp"
@@ -277,7 +282,8 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
 
 constexpr int JOIN = 64;                               // one wave a block: a long prompt of 2048 channels has 512 of them
 
-// The chunks' first states from their states from zero, in place.
+// The chunks' first states from their states from zero, in place: of 256 chunks of 2048 x 16 states 69 MB in 21 us,
+// bound by the chains' loads (32768 threads have 16 each in flight).
 __global__ __launch_bounds__(JOIN) void seq_scan_join_kernel(SeqScanArgs k, DivU32 dn) {
   const mure_seq_scan_args& a = k.a;
   const uint32_t e = blockIdx.x * (unsigned)JOIN + threadIdx.x;

@@ -83,7 +83,7 @@ def _pyext(verbose: bool) -> None:
     tmp = PYEXT_LIB + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-isystem", inc, "-isystem",
            os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"], PYEXT_SRC,
-           "-o", tmp, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+           "-o", tmp, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")

@@ -5,8 +5,9 @@
 //
 // The library stays free of torch: its entry points come in as addresses
 // (bind), and only this module, used by seq.py, knows tensors.
+#include <ATen/EmptyTensor.h>
 #include <ATen/core/grad_mode.h>
-#include <ATen/ops/empty.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -139,12 +140,14 @@ struct Call {
     return {static_cast<const float*>(p.first), p.second};
   }
 
-  // The result given, checked, or a new one of `shape` for every mutant.
+  // The result given, checked, or a new one of `shape` for every mutant: from the device's allocator, ahead of the
+  // dispatcher, which would add a tenth to a call on single tokens (two results each).
   at::Tensor result(PyObject* o, const char* what, c10::IntArrayRef shape, at::ScalarType dtype) const {
     c10::SmallVector<int64_t, 4> full;
     if (axis) full.push_back(mutants);
     full.append(shape.begin(), shape.end());
-    if (o == Py_None) return at::empty(full, first.options().dtype(dtype));
+    if (o == Py_None)
+      return at::Tensor(first.is_cuda() ? at::detail::empty_cuda(full, dtype, first.device(), std::nullopt) : at::detail::empty_cpu(full, dtype));
     const at::Tensor& t = same_place(o, what, dtype);
     if (t.sizes() != c10::IntArrayRef(full))
       raise(PyExc_ValueError, std::string(what) + " has shape " + text(t.sizes()) + "; " + text(full) + " is needed");

@@ -42,7 +42,9 @@ constexpr float LOG2E = 1.44269504088896340736f;
 __device__ __forceinline__ float softplus(float s) {
   const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(s));
   const float w = 1.f + e, r = e - (w - 1.f);
-  return __builtin_amdgcn_fmed3f(s, 0.f, __builtin_inff()) + fmaf(1.f / LOG2E, __builtin_amdgcn_logf(w), r);
+  float m;                                             // of fmaxf the compiler makes two instructions; of a NaN e is one
+  asm("v_max_f32 %0, 0, %1" : "=v"(m) : "v"(s));
+  return m + fmaf(1.f / LOG2E, __builtin_amdgcn_logf(w), r);
 }
 
 // Lane j's value of every quad, in all its lanes.
@@ -70,6 +72,26 @@ __device__ __forceinline__ float quad_sums(float p0, float p1, float p2, float p
 __device__ __forceinline__ float no_zero(float p) { return p < 1.4012985e-45f ? 1.4012985e-45f : p; }
 __device__ __forceinline__ float decay(float al, float d) { return no_zero(__builtin_amdgcn_exp2f(al * d)); }
 
+// An element `off` bytes past p, which is the same in all lanes: with 32 bits through a buffer at p, whose loads and
+// stores take p from scalar registers and need no 64-bit addition in every lane.
+template <typename T> __device__ __forceinline__ T lane_load(const T* p, uint64_t off) {
+  return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(p) + off);
+}
+template <typename T> __device__ __forceinline__ void lane_store(T* p, uint64_t off, T v) {
+  *reinterpret_cast<T*>(reinterpret_cast<char*>(p) + off) = v;
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, -1, 0x00027000);       // raw, 2^32 - 1 bytes
+}
+template <typename T> __device__ __forceinline__ T lane_load(const T* p, uint32_t off) {
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(buffer_at(p), off, 0, 0);
+  else return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer_at(p), off, 0, 0));
+}
+template <typename T> __device__ __forceinline__ void lane_store(T* p, uint32_t off, T v) {
+  if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(v, buffer_at(p), off, 0, 0);
+  else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), buffer_at(p), off, 0, 0);
+}
+
 // Q: states per lane (4 Q in all); PAD: some of them are past N.
 // KIND: RUNS; ENDS, only the state that a run reaches from zero; STEPS, runs of
 // fewer than four tokens all, which need no LDS and half the registers.
@@ -92,27 +114,35 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
   const int64_t m = mi;
   const int D = a.channels, N = a.states, width = D / a.groups;
   const int dg = tile * 64 + (tid >> 2);               // in the group
-  const bool live = dg < width;
-  const int d = group * width + min(dg, width - 1);
+  const bool live = dg < width;                        // else the last channel again, not stored
+  const bool wave_live = tile * 64 + 16 * __builtin_amdgcn_readfirstlane(tid >> 6) < width;
+  const int d0 = group * width + tile * 64, d = group * width + min(dg, width - 1);
   const int64_t su = a.u.row_stride, sd = a.dt.row_stride, sz = a.gate.row_stride, sy = a.out.row_stride;
-  const T* u = static_cast<const T*>(a.u.p) + m * a.u.mutant_stride + it.row0 * su + d;
-  const T* dt = static_cast<const T*>(a.dt.p) + m * a.dt.mutant_stride + it.row0 * sd + d;
-  const T* z = static_cast<const T*>(a.gate.p) + m * a.gate.mutant_stride + it.row0 * sz + d;
+  // The next rows to be loaded, and stored: the same address in all lanes, and a lane's distance from it.
+  const bool gated = !ENDS && a.gate.p;
+  const T* u = static_cast<const T*>(a.u.p) + m * a.u.mutant_stride + it.row0 * su + d0;
+  const T* dt = static_cast<const T*>(a.dt.p) + m * a.dt.mutant_stride + it.row0 * sd + d0;
+  const T* z = static_cast<const T*>(a.gate.p) + m * a.gate.mutant_stride + it.row0 * sz + d0;
+  using Off = std::conditional_t<PAD, uint64_t, uint32_t>;
+  auto lane_off = [&](int64_t stride) { return Off((q * stride + (d - d0)) * sizeof(T)); };
+  const Off ou = lane_off(su), od = lane_off(sd), oz = lane_off(sz), oy = lane_off(sy);
   const T* b = static_cast<const T*>(a.b.p) + m * a.b.mutant_stride + it.row0 * a.b.row_stride + group * N;
   const T* c = static_cast<const T*>(a.c.p) + m * a.c.mutant_stride + it.row0 * a.c.row_stride + group * N;
-  T* y = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * sy + d;
-  const bool gated = !ENDS && a.gate.p;
+  T* y = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * sy + d0;
 
   // A tile's inputs, as they come from memory: b and c; u, dt and gate of its whole groups of four tokens, and of
   // the one to three tokens after them, where the run ends.
-  T bc[PER], ru[GROUPS + 1], rd[GROUPS + 1], rz[GROUPS + 1];
-  // Row t + lane_t of them, t the same in all lanes: kept opaque, or the compiler holds an address for every group
-  // of a tile in registers (156 of them for 16 states, and now 90).
-  auto fetch_row = [&](int t, int lane_t, T& fu, T& fd, T& fz) {
-    asm("" : "+s"(t));
-    fu = (u + t * su)[lane_t * su];
-    fd = (dt + t * sd)[lane_t * sd];
-    if (gated) fz = (z + t * sz)[lane_t * sz];
+  T bc[PER], ru[GROUPS + 1], rd[GROUPS + 1], rz[GROUPS + 1] = {};
+  auto fetch_rows = [&](T& fu, T& fd, T& fz) {         // four tokens
+    fu = lane_load(u, ou);
+    fd = lane_load(dt, od);
+    if (gated) fz = lane_load(z, oz);
+    u += 4 * su, dt += 4 * sd, z += 4 * sz;
+  };
+  auto fetch_last = [&](int left, T& fu, T& fd, T& fz) {       // one to three tokens
+    const int64_t t = min(q, left - 1), c = d - d0;
+    fu = u[t * su + c], fd = dt[t * sd + c];
+    if (gated) fz = z[t * sz + c];
   };
   auto fetch_bc = [&](int t0, int count) {
 #pragma unroll
@@ -123,18 +153,18 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
       if ((BC % 256 == 0 || e < BC) && (!PAD || n < N)) bc[i] = r < TILE ? b[t * a.b.row_stride + n] : c[t * a.c.row_stride + n];
     }
   };
-  auto fetch_group = [&](int t0, int count, int g) {   // g = GROUPS: the tokens after the whole groups
-    if (g < GROUPS && 4 * g + 4 <= count) fetch_row(t0 + 4 * g, q, ru[g], rd[g], rz[g]);
-    if (g == GROUPS && count % 4) fetch_row(t0 + count / 4 * 4, min(q, count % 4 - 1), ru[g], rd[g], rz[g]);
+  auto fetch_group = [&](int count, int g) {           // of a tile of `count` tokens; g = GROUPS: after the whole groups
+    if (g < GROUPS && 4 * g + 4 <= count) fetch_rows(ru[g], rd[g], rz[g]);
+    if (g == GROUPS && count % 4) fetch_last(count % 4, ru[g], rd[g], rz[g]);
   };
   const bool tiled = KIND != STEPS && it.len >= 4;
   if (tiled) {
     const int count = min(TILE, it.len);
     fetch_bc(0, count);
 #pragma unroll
-    for (int g = 0; g <= GROUPS; ++g) fetch_group(0, count, g);
+    for (int g = 0; g <= GROUPS; ++g) fetch_group(count, g);
   } else if (it.len) {
-    fetch_row(0, min(q, it.len - 1), ru[GROUPS], rd[GROUPS], rz[GROUPS]);
+    fetch_last(it.len, ru[GROUPS], rd[GROUPS], rz[GROUPS]);
   }
 
   float al[Q], h[Q];                                   // a log2(e): exp(D a) is one hardware exp2
@@ -172,7 +202,8 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
 #pragma unroll
     for (int i = 0; i < Q; ++i) {
       h[i] = fmaf(__builtin_amdgcn_exp2f(dj * al[i]), h[i], duj * bv[i]);
-      if (!ENDS) p = fmaf(cv[i], PAD && q * Q + i >= N ? 0.f : h[i], p);
+      const float hi = PAD && q * Q + i >= N ? 0.f : h[i];
+      if (!ENDS) p = i ? fmaf(cv[i], hi, p) : cv[i] * hi;
     }
     return p;
   };
@@ -186,16 +217,12 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
     const float v = fmaf(skip, uv, yq);
     return gated ? v * seq_silu(zv) : v;
   };
-  auto store_row = [&](int t, float v) {
-    asm("" : "+s"(t));
-    (y + t * sy)[q * sy] = from_f<T>(v);
-  };
   using J0 = std::integral_constant<int, 0>;
   using J1 = std::integral_constant<int, 1>;
   using J2 = std::integral_constant<int, 2>;
   using J3 = std::integral_constant<int, 3>;
   // the run's last one to three tokens, with their rows of b and c
-  auto last = [&](int t0, int left, T fu, T fd, T fz, auto brow, auto crow) {
+  auto last = [&](int left, T fu, T fd, T fz, auto brow, auto crow) {
     const float uv = to_f<T>(fu);
     float du;
     const float dv = prepare(to_f<T>(fd), uv, du);
@@ -208,7 +235,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
     const float yq = ENDS ? 0.f : quad_sums(p0, p1, p2, 0.f, q);
     if (q >= left) return;
     if (ENDS) sum_d += dv;
-    else store_row(t0, finish(yq, uv, to_f<T>(fz)));
+    else if (live) lane_store(y, oy, from_f<T>(finish(yq, uv, to_f<T>(fz))));
   };
   if (tiled) {
     for (int t0 = 0, i = 0; t0 < it.len; t0 += TILE, i ^= 1) {
@@ -220,30 +247,31 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
       __syncthreads();                                 // this tile is there, and the one before last is read
       const int t1 = t0 + TILE, more = min(TILE, it.len - t1);     // the next tile: its inputs take the registers of
       if (more > 0) fetch_bc(t1, more);                            // this one's as they are used
-      if (!live) continue;
+      if (!wave_live) continue;
       const float *bt = now + q * Q, *ct = ENDS ? bt : bt + TILE * NP;
       auto row = [&](const float* p, int t) { return *reinterpret_cast<const vq*>(p + t * NP); };
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g) {
         if (4 * g + 4 > count) break;
-        const float uv = to_f<T>(ru[g]), zv = gated ? to_f<T>(rz[g]) : 0.f;
-        float du;
+        float uv = to_f<T>(ru[g]), zv = to_f<T>(rz[g]), du;
+        asm("" : "+v"(uv), "+v"(zv));                  // converted here: the registers are free for the next tile's
         const float dv = prepare(to_f<T>(rd[g]), uv, du);
-        fetch_group(t1, more, g);
+        fetch_group(more, g);
         const float p0 = step(J0(), dv, du, row(bt, 4 * g), row(ct, 4 * g));
         const float p1 = step(J1(), dv, du, row(bt, 4 * g + 1), row(ct, 4 * g + 1));
         const float p2 = step(J2(), dv, du, row(bt, 4 * g + 2), row(ct, 4 * g + 2));
         const float p3 = step(J3(), dv, du, row(bt, 4 * g + 3), row(ct, 4 * g + 3));
         const float yq = ENDS ? 0.f : quad_sums(p0, p1, p2, p3, q);
         if (ENDS) sum_d += dv;
-        else store_row(t0 + 4 * g, finish(yq, uv, zv));
+        else if (live) lane_store(y, oy, from_f<T>(finish(yq, uv, zv)));
+        y += 4 * sy;
       }
       if (more <= 0 && count % 4) {
         const int done = count / 4 * 4;
-        last(t0 + done, count - done, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(bt, done + j); },
+        last(count - done, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(bt, done + j); },
              [&](int j) { return row(ct, done + j); });
       }
-      fetch_group(t1, more, GROUPS);
+      fetch_group(more, GROUPS);
     }
     if (!live) return;
   } else {
@@ -255,7 +283,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
       return v;
     };
     if (it.len)
-      last(0, it.len, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(b, j * a.b.row_stride); },
+      last(it.len, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(b, j * a.b.row_stride); },
            [&](int j) { return row(c, j * a.c.row_stride); });
   }
   float* to = nullptr;
@@ -346,7 +374,10 @@ static hipError_t scan_q(SeqScanArgs k, hipStream_t s) {
 
 template <typename T, int Q, int KIND>
 static hipError_t scan_p(const SeqScanArgs& k, hipStream_t s) {
-  return k.a.states == 4 * Q ? scan_q<T, Q, false, KIND>(k, s) : scan_q<T, Q, true, KIND>(k, s);
+  // A lane's distance from its rows' first element has 32 bits but in the instances with padding.
+  const int64_t most = ((int64_t)UINT32_MAX / (int64_t)sizeof(T) - 64) / 3;
+  const bool near = std::max({k.a.u.row_stride, k.a.dt.row_stride, k.a.gate.p ? k.a.gate.row_stride : 0, k.a.out.row_stride}) <= most;
+  return k.a.states == 4 * Q && near ? scan_q<T, Q, false, KIND>(k, s) : scan_q<T, Q, true, KIND>(k, s);
 }
 
 template <typename T, int KIND>

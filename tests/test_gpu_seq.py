@@ -502,3 +502,24 @@ def test_infinite_states_of_long_sequences(mure, D):
     assert bool(torch.isnan(y[0, 700:, 5]).all()) and bool(torch.isfinite(y[0, :700, 5]).all())
     rest = [c for c in range(D) if c not in (3, 5)]
     assert bool(torch.isfinite(y[0][:, rest]).all()) and bool(torch.isfinite(last[0, 0][rest]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scan_of_rows_far_apart(mure, dtype):
+    """Rows of which four span more than 2^32 bytes, read and written."""
+    say(f"[scan far rows] {dtype}")
+    T, D, N = 7, 70, 16
+    far = (1 << 32) // (3 * TYPES[dtype].itemsize) + 101
+    whole = torch.empty((T - 1) * far + D, dtype=TYPES[dtype], device="cuda")
+    rows = whole.as_strided((T, D), (far, 1))
+    p = scan_inputs(23, [T], D, N, TYPES[dtype])
+    q = {k: None if v is None else v.cuda()[0] for k, v in p.items()}
+    rest = dict(skip=q["skip"], dt_bias=q["dt_bias"], gate=q["gate"])
+    seqs = mure.sequences([T])
+    expected, last = seqs.scan(q["u"], q["dt"], q["A"], q["B"], q["C"], **rest)
+    R.close(expected[None], R.scan(p["u"], p["dt"], p["A"], p["B"], p["C"], [T], p["skip"], p["dt_bias"], p["gate"])[0], "near")
+    rows.copy_(q["u"])
+    y, state = seqs.scan(rows, q["dt"], q["A"], q["B"], q["C"], **rest)
+    assert torch.equal(y, expected) and torch.equal(state, last)
+    y, state = seqs.scan(q["u"], q["dt"], q["A"], q["B"], q["C"], out=rows, **rest)
+    assert y is rows and torch.equal(rows, expected) and torch.equal(state, last)

@@ -126,8 +126,9 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
   using Off = std::conditional_t<PAD, uint64_t, uint32_t>;
   auto lane_off = [&](int64_t stride) { return Off((q * stride + (d - d0)) * sizeof(T)); };
   const Off ou = lane_off(su), od = lane_off(sd), oz = lane_off(sz), oy = lane_off(sy);
-  const T* b = static_cast<const T*>(a.b.p) + m * a.b.mutant_stride + it.row0 * a.b.row_stride + group * N;
-  const T* c = static_cast<const T*>(a.c.p) + m * a.c.mutant_stride + it.row0 * a.c.row_stride + group * N;
+  const int64_t sb = a.b.row_stride, sc = a.c.row_stride;
+  const T* b = static_cast<const T*>(a.b.p) + m * a.b.mutant_stride + it.row0 * sb + group * N;
+  const T* c = static_cast<const T*>(a.c.p) + m * a.c.mutant_stride + it.row0 * sc + group * N;
   T* y = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * sy + d0;
 
   // A tile's inputs, as they come from memory: b and c; u, dt and gate of its whole groups of four tokens, and of
@@ -144,14 +145,26 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
     fu = u[t * su + c], fd = dt[t * sd + c];
     if (gated) fz = z[t * sz + c];
   };
-  auto fetch_bc = [&](int t0, int count) {
+  // Element tid + 256 i of a tile's b and c, of the next tile to be loaded: from 16 states on a block's threads take
+  // STEP whole rows at a time, of b and then of c; below that all of them at once.
+  constexpr bool ROWWISE = TILE * NP >= 256;
+  constexpr int STEP = 256 / NP, OF_B = ROWWISE ? TILE / STEP : 1;
+  const int br = tid / NP % TILE, bn = tid % NP;
+  const bool of_c = !ROWWISE && !ENDS && tid / NP >= TILE;
+  const int64_t s0 = of_c ? sc : sb;
+  const T *b0 = (of_c ? c : b) + br * s0 + bn, *c0 = c + br * sc + bn;
+  auto fetch_bc = [&](int count) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int e = tid + 256 * i, r = e / NP, n = e % NP;
-      const int64_t t = t0 + min(r % TILE, count - 1);  // rows past the run are not used
+      const bool is_c = i >= OF_B;
+      const int step = i % OF_B * STEP;                // rows on from this thread's first
+      const T* p = is_c ? c0 + step * sc : b0 + step * s0;
+      if (count < TILE) p += (min(br + step, count - 1) - br - step) * (is_c ? sc : s0);       // rows past the run are not used
       bc[i] = T(0);
-      if ((BC % 256 == 0 || e < BC) && (!PAD || n < N)) bc[i] = r < TILE ? b[t * a.b.row_stride + n] : c[t * a.c.row_stride + n];
+      if ((BC % 256 == 0 || tid + 256 * i < BC) && (!PAD || bn < N)) bc[i] = *p;
     }
+    b0 += TILE * s0;
+    if (ROWWISE && !ENDS) c0 += TILE * sc;
   };
   auto fetch_group = [&](int count, int g) {           // of a tile of `count` tokens; g = GROUPS: after the whole groups
     if (g < GROUPS && 4 * g + 4 <= count) fetch_rows(ru[g], rd[g], rz[g]);
@@ -160,7 +173,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
   const bool tiled = KIND != STEPS && it.len >= 4;
   if (tiled) {
     const int count = min(TILE, it.len);
-    fetch_bc(0, count);
+    fetch_bc(count);
 #pragma unroll
     for (int g = 0; g <= GROUPS; ++g) fetch_group(count, g);
   } else if (it.len) {
@@ -246,7 +259,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
         if (BC % 256 == 0 || tid + 256 * j < BC) now[tid + 256 * j] = to_f<T>(bc[j]);
       __syncthreads();                                 // this tile is there, and the one before last is read
       const int t1 = t0 + TILE, more = min(TILE, it.len - t1);     // the next tile: its inputs take the registers of
-      if (more > 0) fetch_bc(t1, more);                            // this one's as they are used
+      if (more > 0) fetch_bc(more);                                // this one's as they are used
       if (!wave_live) continue;
       const float *bt = now + q * Q, *ct = ENDS ? bt : bt + TILE * NP;
       auto row = [&](const float* p, int t) { return *reinterpret_cast<const vq*>(p + t * NP); };
@@ -283,8 +296,8 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
       return v;
     };
     if (it.len)
-      last(it.len, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(b, j * a.b.row_stride); },
-           [&](int j) { return row(c, j * a.c.row_stride); });
+      last(it.len, ru[GROUPS], rd[GROUPS], rz[GROUPS], [&](int j) { return row(b, j * sb); },
+           [&](int j) { return row(c, j * sc); });
   }
   float* to = nullptr;
   if (ENDS) {

@@ -22,10 +22,10 @@
 // ENDS), one walks the chunks of every channel and state (seq_scan_join_kernel)
 // and one computes the outputs from the chunks' first states.
 //
-// 32768 tokens of 2048 channels and 16 states, bfloat16: 197, 21 and 270 us.
-// The two scans keep the vector ALU busy all the time: of the second one's 122
-// instructions per quad and four tokens 80 are the recurrence, and the 20
-// transcendental ones take two slots.
+// 32768 tokens of 2048 channels and 16 states, bfloat16: 190, 20 and 255 us
+// at best, 424 to 436 us a call.  The two scans keep the vector ALU busy
+// all the time: of the second one's 113 instructions per quad and four tokens 80
+// are the recurrence, and the 20 transcendental ones take two slots.
 #include <algorithm>
 
 #include "seq_dev.hpp"

@@ -1,7 +1,7 @@
 // Argument marshalling of the sequence operators (include/mure_seq.h) for
 // Python: checks torch tensors, allocates outputs, fills the argument blocks
 // and makes the call.  A call on single tokens runs for some 5 us on the GPU;
-// the same work done by ctypes takes 14 us on the host, this 6.
+// the same work done by ctypes takes 14 us on the host, this 5.6.
 //
 // The library stays free of torch: its entry points come in as addresses
 // (bind), and only this module, used by seq.py, knows tensors.

@@ -121,6 +121,10 @@ mure_status mure_seq_conv(mure_seq* seq, const mure_seq_conv_args* args);
  *   h[n] = exp(D a[d][n]) h[n] + D u[t][d] b[t][g(d)][n]
  *   out[t][d] = (sum_n c[t][g(d)][n] h[n] + skip[d] u[t][d]) silu(gate[t][d])
  * from the sequence's state (or 0), whose last value goes to state_out.
+ * The rates a and the steps may have either sign.  A state past float32's
+ * range is infinite.  What is or becomes infinite goes on by the arithmetic of
+ * infinities: NaN after a decay that underflows to 0 or with an infinite term
+ * of the other sign (in a long sequence also one summed up over a chunk).
  * dtype: of u, dt, b, c, gate and out.  b, c: rows of groups * states.
  * a: float32 [channels][states]; skip, dt_bias, gate (p = NULL) optional.
  * state, state_out: float32 [n_seq][channels][states], dense for one mutant,

@@ -66,11 +66,12 @@ __device__ __forceinline__ float quad_sums(float p0, float p1, float p2, float p
   return (high ? b : a) + quad_xor2(high ? a : b);
 }
 
-// The decay of a state over tokens whose steps sum to d.  Not below the
-// smallest positive float: an infinite state stays infinite, as it does when
-// it decays token by token.
-__device__ __forceinline__ float no_zero(float p) { return p < 1.4012985e-45f ? 1.4012985e-45f : p; }
-__device__ __forceinline__ float decay(float al, float d) { return no_zero(__builtin_amdgcn_exp2f(al * d)); }
+// The state h after tokens that take a state of zero to `end`, and whose steps times the state's rate sum to
+// 2 half / log2(e): 2^(2 half) h + end.  In two products: the result may be in float's range where the factor is not.
+__device__ __forceinline__ float carried(float half, float h, float end) {
+  const float f = __builtin_amdgcn_exp2f(half);
+  return fmaf(f, f * h, end);
+}
 
 // An element `off` bytes past p, which is the same in all lanes: with 32 bits through a buffer at p, whose loads and
 // stores take p from scalar registers and need no 64-bit addition in every lane.
@@ -324,22 +325,51 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
 constexpr int JOIN = 64;                               // one wave a block: a long prompt of 2048 channels has 512 of them
 
 // The chunks' first states from their states from zero, in place: of 256 chunks of 2048 x 16 states 69 MB in 21 us,
-// bound by the chains' loads (32768 threads have 16 each in flight).
+// bound by the chains' loads (32768 threads have 16 each in flight).  Where a chunk takes a state out of float's range,
+// or an infinite one by decays that may be 0 (0 times infinity is NaN), the state goes through it token by token, with
+// the operations of seq_scan_kernel: two parts past float's range may add up to a number.
+template <typename T>
 __global__ __launch_bounds__(JOIN) void seq_scan_join_kernel(SeqScanArgs k, DivU32 dn) {
   const mure_seq_scan_args& a = k.a;
   const uint32_t e = blockIdx.x * (unsigned)JOIN + threadIdx.x;
   const int D = a.channels, N = a.states;
   if (e >= (uint32_t)D * (uint32_t)N) return;
   const int64_t m = blockIdx.z, d = divu(dn, e), DN = (int64_t)D * N;
-  const float al = a.a.p[m * a.a.mutant_stride + e] * LOG2E;
+  const float al = a.a.p[m * a.a.mutant_stride + e] * LOG2E, half_al = 0.5f * al;
   for (int i = blockIdx.y; i < k.n_chunked; i += gridDim.y) {
     const SeqChunks ch = k.chunks[i];
     float h = a.state ? a.state[m * a.state_mutant_stride + ch.seq * DN + e] : 0.f;
     float* ws = k.ws_h + (m * k.n_slots + ch.slot0) * DN + e;
     const float* sd = k.ws_d + (m * k.n_slots + ch.slot0) * D + d;
+    // the state after chunk j, token by token
+    auto walk = [&](int j, float h) {
+      const int64_t row = ch.row0 + (int64_t)j * SCAN_CHUNK, n = e - d * N + d / (D / a.groups) * N;
+      const T* u = static_cast<const T*>(a.u.p) + m * a.u.mutant_stride + row * a.u.row_stride + d;
+      const T* dt = static_cast<const T*>(a.dt.p) + m * a.dt.mutant_stride + row * a.dt.row_stride + d;
+      const T* b = static_cast<const T*>(a.b.p) + m * a.b.mutant_stride + row * a.b.row_stride + n;
+      const float bias = a.dt_bias.p ? a.dt_bias.p[m * a.dt_bias.mutant_stride + d] : 0.f;
+      for (int t0 = 0; t0 < SCAN_CHUNK; t0 += TILE) {
+        T ru[TILE], rd[TILE], rb[TILE];
+#pragma unroll
+        for (int t = 0; t < TILE; ++t) {
+          ru[t] = u[(t0 + t) * a.u.row_stride];
+          rd[t] = dt[(t0 + t) * a.dt.row_stride];
+          rb[t] = b[(t0 + t) * a.b.row_stride];
+        }
+#pragma unroll
+        for (int t = 0; t < TILE; ++t) {
+          float dv = to_f<T>(rd[t]) + bias;
+          if (a.softplus) dv = softplus(dv);
+          const float du = dv * to_f<T>(ru[t]);
+          h = fmaf(__builtin_amdgcn_exp2f(dv * al), h, du * to_f<T>(rb[t]));
+        }
+      }
+      return h;
+    };
     // AHEAD chunks are loaded at a time, ahead of those being joined.  The last chunk has no state from zero, and none
     // is used.
     constexpr int AHEAD = 8;
+    constexpr float LEAST = -62.f;                     // of half: with steps of one sign no token's decay is 0
     float end[AHEAD], s[AHEAD];
     const float* at = ws;
     auto load = [&](int n) {
@@ -349,22 +379,47 @@ __global__ __launch_bounds__(JOIN) void seq_scan_join_kernel(SeqScanArgs k, DivU
       at += AHEAD * DN;
       sd += AHEAD * (int64_t)D;
     };
-    auto join = [&](int n, int more) {                 // n chunks, and the loads of `more` after them
-      float e[AHEAD], f[AHEAD];
+    int left = ch.n;
+    // n chunks, `ended` of them with ends, and the loads of `more` after them; false: they have to be joined one by one
+    auto join = [&](int n, int ended, int more) {
+      float e[AHEAD], x[AHEAD], to[AHEAD];
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) e[i] = end[i], f[i] = decay(al, s[i]);
+      for (int i = 0; i < AHEAD; ++i) e[i] = end[i], x[i] = half_al * s[i];
       load(more);
+      float last = h;
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
-        if (i < n) ws[i * DN] = h;
-        h = fmaf(f[i], h, e[i]);
+        to[i] = last;
+        if (i < ended) last = carried(x[i], last, e[i]);
       }
-      ws += AHEAD * DN;
+      bool plain = isfinite(last) || isnan(h);         // an infinite state or a NaN on the way is one at the end
+      if (!plain && isinf(h)) {
+        plain = true;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (i < ended) plain = plain && x[i] >= LEAST;
+      }
+      if (!plain) return false;
+      h = last;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (i < n) ws[i * DN] = to[i];
+      return true;
     };
-    int left = ch.n;
     load(min(AHEAD, left - 1));
-    for (; left > 2 * AHEAD; left -= AHEAD) join(AHEAD, AHEAD);
-    for (; left > 0; left -= AHEAD) join(left, left - AHEAD - 1);
+    for (; left > 0; left -= AHEAD, ws += AHEAD * DN) {
+      if (left > 2 * AHEAD ? join(AHEAD, AHEAD, AHEAD) : join(left, left - 1, left - AHEAD - 1)) continue;
+      const int j0 = ch.n - left;
+      const float* sums = k.ws_d + (m * k.n_slots + ch.slot0 + j0) * D + d;
+#pragma unroll 1
+      for (int i = 0; i < min(AHEAD, left); ++i) {
+        const float end = ws[i * DN], sum = sums[i * (int64_t)D], x = half_al * sum;
+        ws[i * DN] = h;
+        if (i == left - 1 || isnan(h)) continue;
+        const float next = h == 0.f ? end : carried(x, h, end);
+        h = isfinite(sum) && (isfinite(h) ? isfinite(next) : x >= LEAST) ? next : walk(j0 + i, h);
+      }
+    }
   }
 }
 
@@ -414,7 +469,8 @@ hipError_t launch_seq_scan_ends(const SeqScanArgs& k, hipStream_t s) { return sc
 
 hipError_t launch_seq_scan_join(const SeqScanArgs& k, hipStream_t s) {
   const int64_t DN = (int64_t)k.a.channels * k.a.states;
-  seq_scan_join_kernel<<<dim3((unsigned)((DN + JOIN - 1) / JOIN), (unsigned)std::min(k.n_chunked, 65535), (unsigned)k.a.n_mutants), JOIN, 0,
+  const auto kernel = k.a.dtype == MURE_F32 ? seq_scan_join_kernel<float> : seq_scan_join_kernel<bf16_t>;
+  kernel<<<dim3((unsigned)((DN + JOIN - 1) / JOIN), (unsigned)std::min(k.n_chunked, 65535), (unsigned)k.a.n_mutants), JOIN, 0,
                          s>>>(k, make_divu32((uint32_t)k.a.states));
   return hipGetLastError();
 }

@@ -228,7 +228,7 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
       const size_t first = scan.size();
       add_runs(scan, i, row, L, SCAN_CHUNK, slots);
       ends.insert(ends.end(), scan.begin() + first, scan.end() - 1);
-      chunked.push_back({i, (int32_t)slots, (int32_t)n});
+      chunked.push_back({i, (int32_t)slots, (int32_t)n, (int32_t)row});
       slots += n;
     }
     row += L;

@@ -23,9 +23,9 @@ struct SeqItem {
 // one token each, which a decoding step need not wait for.
 __device__ __forceinline__ SeqItem seq_item(const SeqItem* items, int i) { return items ? items[i] : SeqItem{i, i, 1, 0, 1, -1}; }
 
-// A sequence scanned in chunks: its slots slot0 .. slot0 + n - 1.
+// A sequence scanned in chunks: its slots slot0 .. slot0 + n - 1, its first row.
 struct SeqChunks {
-  int32_t seq, slot0, n;
+  int32_t seq, slot0, n, row0;
 };
 
 constexpr int SCAN_CHUNK = 128;                // tokens of a chunk

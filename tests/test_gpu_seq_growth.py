@@ -1,0 +1,205 @@
+"""Scans of long sequences whose states grow, shrink or pass float32's range:
+the states carried over the chunks against the definition in float64 with its
+running bounds (``seq_reference``), and against the same sequence in parts of
+which none is split, where every state goes on token by token."""
+import pytest
+import torch
+
+import seq_reference as R
+from paper_2607_18582_amd import Mure
+
+pytestmark = pytest.mark.gpu
+
+MOST = torch.finfo(torch.float32).max
+CHUNK = 128
+
+
+@pytest.fixture(scope="module")
+def mure():
+    m = Mure(device=0)
+    yield m
+    m.close()
+
+
+def inputs(length, D, N, dtype=torch.float32, seed=0, rates=None, step=None, M=1):
+    """Without softplus and bias: the steps are dt.  rates [D][N], step [length][D] or a number."""
+    g = torch.Generator().manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    dt = torch.full((M, length, D), float(step)) if not isinstance(step, torch.Tensor) else step.expand(M, length, D).clone()
+    return dict(u=normal(M, length, D).to(dtype), dt=dt.to(dtype), A=rates.expand(1, D, N).clone(),
+                B=(normal(M, length, N).abs() + 0.1).to(dtype), C=(normal(M, length, N).abs() + 0.1).to(dtype), state=None)
+
+
+def scan(seqs, p, softplus=False, cut=slice(None), state=None, **more):
+    q = {k: v.cuda() for k, v in p.items() if v is not None}
+    held = q.get("state") if state is None else state
+    return seqs.scan(q["u"][:, cut], q["dt"][:, cut], q["A"], q["B"][:, cut], q["C"][:, cut], softplus=softplus, state=held, **more)
+
+
+def in_parts(mure, p, length, part, softplus=False):
+    """The same in parts that are one run each, the state carried on."""
+    ys, state = [], None
+    for at in range(0, length, part):
+        n = min(part, length - at)
+        y, state = scan(mure.sequences([n]), p, softplus, slice(at, at + n), state)
+        ys.append(y)
+    return torch.cat(ys, 1), state
+
+
+def check(mure, p, length, softplus=False):
+    y, last = scan(mure.sequences([length]), p, softplus)
+    ey, el = R.scan(p["u"], p["dt"], p["A"], p["B"], p["C"], [length], use_softplus=softplus, state=p["state"])
+    for (value, bound), got, what in ((ey, y, "out"), (el, last, "state")):
+        assert float((value + bound).abs().max()) < MOST, f"{what}: the case passes float32's range"
+        R.close(got, (value, bound), what)
+    return y, last
+
+
+def same_kind(a, b):
+    """NaN and infinities of both signs stand at the same places."""
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(a.isposinf(), b.isposinf()) and torch.equal(a.isneginf(), b.isneginf())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N", [1, 6, 16])
+def test_growing_states_that_begin_late(mure, dtype, N):
+    """Rates that grow by more than float32's range over one chunk; no input, and so no state, until the last tokens."""
+    print(f"[growth] late {dtype} N={N}", flush=True)
+    D, length = 5, 600
+    p = inputs(length, D, N, dtype, 1, torch.linspace(0.75, 1.5, D)[:, None] * torch.ones(N), 1.0)
+    p["u"][:, :length - 10] = 0
+    check(mure, p, length)
+    p["dt"] = torch.full_like(p["dt"], 0.625)   # a softplus of 1.05: factors of up to e^200 over a chunk
+    y, last = check(mure, p, length, True)
+    assert bool((y[:, :length - 10] == 0).all()) and float(last.abs().min()) > 0
+
+
+def test_growing_states_given_as_zero(mure):
+    print("[growth] zero state", flush=True)
+    D, N, length = 3, 16, 1300
+    p = inputs(length, D, N, seed=2, rates=torch.full((D, N), 1.0), step=1.0)
+    p["u"][:, :length - 7] = 0
+    p["state"] = torch.zeros(1, 1, D, N)
+    check(mure, p, length)
+
+
+def test_tiny_states_that_grow_and_shrink(mure):
+    """From 1e-30 by e^115 in one chunk and back in the next: the product is in range where the factor is not."""
+    print("[growth] tiny", flush=True)
+    D, N, length = 4, 16, 6 * CHUNK
+    step = torch.zeros(length, D)
+    for i in range(6):
+        step[i * CHUNK:(i + 1) * CHUNK] = (0.9, -0.9)[i % 2]
+    p = inputs(length, D, N, seed=3, rates=torch.ones(D, N), step=step)
+    p["u"][:] = 0
+    p["state"] = torch.linspace(1, 2, D * N).view(1, 1, D, N) * 1e-30
+    check(mure, p, length)
+
+
+def test_huge_states_that_decay(mure):
+    """From 1e30 down by e^-115 a chunk, and by far more: what is left counts as float32 holds it, and nothing is added."""
+    print("[growth] huge", flush=True)
+    D, N, length = 6, 16, 700
+    rates = torch.tensor([-0.45, -0.9, -1.1, -2.0, -5.0, -0.1])[:, None] * torch.ones(N)
+    p = inputs(length, D, N, seed=4, rates=rates, step=1.0)
+    p["u"][:] = 0
+    p["state"] = torch.full((1, 1, D, N), 1e30)
+    p["state"][0, 0, :, ::2] *= -1
+    y, last = check(mure, p, length)
+    assert bool((last[0, 0, 3:5] == 0).all()) and bool((y[0, 3 * CHUNK:, 3:5] == 0).all())
+    assert bool((last[0, 0, 5] != 0).all())
+
+
+@pytest.mark.parametrize("softplus", [False, True])
+def test_states_that_overflow(mure, softplus):
+    """A state past float32's range is infinite from there on, as in parts."""
+    print(f"[growth] overflow {softplus}", flush=True)
+    D, N, length = 6, 8, 1000
+    rates = torch.tensor([0.05, 0.2, 0.7, 1.0, 3.0, -0.5])[:, None] * torch.ones(N)
+    p = inputs(length, D, N, seed=5, rates=rates, step=0.9)
+    p["u"] = p["u"].abs() + 0.1
+    p["u"][:, :300, 2] = 0
+    p["u"][:, :, 3] *= -1
+    y, last = scan(mure.sequences([length]), p, softplus)
+    ey, el = in_parts(mure, p, length, 500, softplus)
+    assert same_kind(y, ey) and same_kind(last, el)
+    assert bool(last[0, 0, 1:3].isposinf().all()) and bool(last[0, 0, 3].isneginf().all()) and bool(last[0, 0, 5].isfinite().all())
+    assert not bool(y.isnan().any())
+
+
+def test_infinite_states_as_token_by_token(mure):
+    """An infinite state stays infinite while its decays are float32 numbers and is NaN after one that underflows to 0,
+    in every chunk alike."""
+    print("[growth] infinite", flush=True)
+    D, N, length = 4, 5, 1500
+    step = torch.full((length, D), 0.25)
+    step[900, 1] = 80.0                         # e^-80 ... e^-400: the fastest states' factor is 0
+    step[1400, 2] = 200.0
+    rates = -torch.arange(1, N + 1).float().expand(D, N)
+    p = inputs(length, D, N, seed=6, rates=rates, step=step)
+    p["u"][0, 200, :3] = torch.tensor([float("inf"), float("inf"), float("-inf")])
+    y, last = scan(mure.sequences([length]), p)
+    ey, el = in_parts(mure, p, length, 500)
+    assert same_kind(last, el) and same_kind(y, ey)
+    assert bool(last[0, 0, 0].isposinf().all()) and bool(last[0, 0, 1].isnan().any()) and bool(last[0, 0, 1].isposinf().any())
+    assert bool(last[0, 0, 3].isfinite().all())
+    # an infinite state that is given, and one of each sign that meet
+    p["state"] = torch.zeros(1, 1, D, N)
+    p["state"][0, 0, 3, 1], p["state"][0, 0, 3, 2] = float("inf"), float("-inf")
+    p["u"][0, 1200, 0] = float("-inf")
+    y, last = scan(mure.sequences([length]), p)
+    ey, state = [], p["state"].cuda()
+    for at in range(0, length, 500):
+        part, state = scan(mure.sequences([500]), p, cut=slice(at, at + 500), state=state)
+        ey.append(part)
+    assert same_kind(last, state) and same_kind(y, torch.cat(ey, 1))
+    assert bool(last[0, 0, 0].isnan().all())
+
+
+def test_opposite_overflows_of_a_chunk(mure):
+    """A state that its next input nearly cancels grows on from what is left: the two parts alone pass float32's
+    range, with opposite signs."""
+    print("[growth] opposite", flush=True)
+    D, N, length = 2, 4, 640
+    p = inputs(length, D, N, seed=7, rates=torch.ones(D, N), step=0.0)
+    p["u"][:] = 0
+    p["B"][:] = 1
+    p["dt"][0, 130:256] = 0.72                  # e^90.7 over the second chunk
+    p["dt"][0, 129], p["u"][0, 129] = 2.0 ** -10, -1024 * 1.0009765625
+    p["state"] = torch.ones(1, 1, D, N)
+    y, last = scan(mure.sequences([length]), p)
+    ey, state = [], p["state"].cuda()
+    for at in range(0, length, 320):
+        part, state = scan(mure.sequences([320]), p, cut=slice(at, at + 320), state=state)
+        ey.append(part)
+    assert bool(state.isfinite().all()) and float(state.abs().max()) > 0
+    assert torch.equal(last, state) and torch.equal(y, torch.cat(ey, 1))
+
+
+def test_steps_whose_sum_overflows(mure):
+    """Finite steps of a chunk with an infinite sum: a rate of 0 still keeps the state."""
+    print("[growth] sum of steps", flush=True)
+    D, N, length = 2, 4, 600
+    rates = torch.tensor([0.0, -1.0])[:, None] * torch.ones(N)
+    p = inputs(length, D, N, seed=8, rates=rates, step=1e37)
+    p["u"][:] = 0
+    p["state"] = torch.ones(1, 1, D, N)
+    y, last = check(mure, p, length)
+    assert bool((last[0, 0, 0] == 1).all()) and bool((last[0, 0, 1] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("softplus", [False, True])
+def test_mixed_rates_of_many_mutants(mure, dtype, softplus):
+    """Rates and steps of both signs, moderate over the whole sequence, several sequences and mutants."""
+    print(f"[growth] mixed {dtype} {softplus}", flush=True)
+    D, N, M, lengths = 9, 12, 2, [700, 40, 1025]
+    T = sum(lengths)
+    g = torch.Generator().manual_seed(9)
+    rates = torch.randn(D, N, generator=g) * 0.03
+    p = inputs(T, D, N, dtype, 10, rates, torch.randn(T, D, generator=g) * (1 if softplus else 3), M)
+    p["state"] = torch.randn(M, len(lengths), D, N, generator=g)
+    y, last = scan(mure.sequences(lengths), p, softplus)
+    ey, el = R.scan(p["u"], p["dt"], p["A"], p["B"], p["C"], lengths, use_softplus=softplus, state=p["state"])
+    R.close(y, ey, "out")
+    R.close(last, el, "state")

@@ -136,9 +136,10 @@ static hipError_t conv_n(SeqConvArgs k, hipStream_t s) {
   const int most = (1 << 30) / vecs;                   // items of a launch: its grid has fewer than 2^32 threads
   for (int left = k.n_items; left > 0; left -= most, k.item0 += most) {
     const uint32_t total = (uint32_t)std::min(left, most) * (uint32_t)vecs;
-    seq_conv_kernel<T, K, N, SILU, ODD><<<dim3((total + 255) / 256, (unsigned)k.a.n_mutants), 256, 0, s>>>(
-        k, make_divu32((uint32_t)vecs), total);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (hipError_t e = launch(seq_conv_kernel<T, K, N, SILU, ODD>, dim3((total + 255) / 256, (unsigned)k.a.n_mutants), 256, s, k,
+                              make_divu32((uint32_t)vecs), total);
+        e != hipSuccess)
+      return e;
   }
   return hipSuccess;
 }

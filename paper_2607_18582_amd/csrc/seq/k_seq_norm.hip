@@ -226,8 +226,7 @@ static hipError_t norm_l(const mure_seq_norm_args& a, hipStream_t s) {
   constexpr int FULL = (V * N == 16 ? 768 : 1024) * 256 / BLOCK;
   const int64_t most = std::max<int64_t>(1, FULL / a.n_mutants);
   const int64_t blocks = std::min<int64_t>((a.rows + PER - 1) / PER, most);
-  seq_norm_kernel<T, R, L, V, N><<<dim3((unsigned)blocks, (unsigned)a.n_mutants), BLOCK, 0, s>>>(a, vecs);
-  return hipGetLastError();
+  return launch(seq_norm_kernel<T, R, L, V, N>, dim3((unsigned)blocks, (unsigned)a.n_mutants), BLOCK, s, a, vecs);
 }
 
 // Lanes and vectors by the width alone: the order of the sums is part of the

@@ -433,9 +433,11 @@ static hipError_t scan_q(SeqScanArgs k, hipStream_t s) {
   const int64_t blocks = seq_scan_blocks(k.a);         // of an item: at most SCAN_GRID (checked by the caller)
   const int most = (int)(SCAN_GRID / blocks);
   for (int left = k.n_items; left > 0; left -= most, k.item0 += most) {
-    seq_scan_kernel<T, Q, PAD, KIND><<<(unsigned)(blocks * std::min(left, most)), 256, 0, s>>>(
-        k, make_divu32((uint32_t)(tiles * k.a.groups)), make_divu32((uint32_t)k.a.n_mutants), make_divu32((uint32_t)tiles));
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (hipError_t e = launch(seq_scan_kernel<T, Q, PAD, KIND>, dim3((unsigned)(blocks * std::min(left, most))), 256, s, k,
+                              make_divu32((uint32_t)(tiles * k.a.groups)), make_divu32((uint32_t)k.a.n_mutants),
+                              make_divu32((uint32_t)tiles));
+        e != hipSuccess)
+      return e;
   }
   return hipSuccess;
 }
@@ -470,9 +472,8 @@ hipError_t launch_seq_scan_ends(const SeqScanArgs& k, hipStream_t s) { return sc
 hipError_t launch_seq_scan_join(const SeqScanArgs& k, hipStream_t s) {
   const int64_t DN = (int64_t)k.a.channels * k.a.states;
   const auto kernel = k.a.dtype == MURE_F32 ? seq_scan_join_kernel<float> : seq_scan_join_kernel<bf16_t>;
-  kernel<<<dim3((unsigned)((DN + JOIN - 1) / JOIN), (unsigned)std::min(k.n_chunked, 65535), (unsigned)k.a.n_mutants), JOIN, 0,
-                         s>>>(k, make_divu32((uint32_t)k.a.states));
-  return hipGetLastError();
+  return launch(kernel, dim3((unsigned)((DN + JOIN - 1) / JOIN), (unsigned)std::min(k.n_chunked, 65535), (unsigned)k.a.n_mutants), JOIN,
+                s, k, make_divu32((uint32_t)k.a.states));
 }
 
 }  // namespace mure

@@ -24,6 +24,7 @@ struct Fail {
 
 void check(hipError_t e, const char* what) {
   if (e == hipSuccess) return;
+  (void)hipGetLastError();                     // reported here: not again by a later launch
   throw Fail{e == hipErrorOutOfMemory ? MURE_E_NOMEM : MURE_E_DEVICE, std::string(what) + ": " + hipGetErrorString(e)};
 }
 

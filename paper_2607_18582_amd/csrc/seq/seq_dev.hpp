@@ -2,10 +2,26 @@
 // alignment, activations.
 #pragma once
 
+#include <tuple>
+#include <utility>
+
 #include "../dev.hpp"
 #include "seq.hpp"
 
 namespace mure {
+
+// Enqueues a kernel and returns the launch's own status: hipGetLastError would report what another call of this thread
+// has left there.
+template <typename... P, typename... A>
+hipError_t launch(void (*kernel)(P...), dim3 grid, unsigned block, hipStream_t s, A&&... a) {
+  std::tuple<P...> params(std::forward<A>(a)...);
+  return std::apply(
+      [&](auto&... p) {
+        void* at[] = {&p...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(block), at, 0, s);
+      },
+      params);
+}
 
 // 16 bytes of elements of T at the alignment of T: the GPU's global loads and
 // stores take any address (a vector that crosses a cache line costs both).

@@ -1,6 +1,7 @@
 // C ABI of the sequence operators (mure_seq.h): batches, checks of arguments,
 // workspaces and launches.
 #include "seq.hpp"
+#include "workspace.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -28,22 +29,15 @@ void check(hipError_t e, const char* what) {
   throw Fail{e == hipErrorOutOfMemory ? MURE_E_NOMEM : MURE_E_DEVICE, std::string(what) + ": " + hipGetErrorString(e)};
 }
 
-// Device memory held until it is destroyed.
-struct Mem {
-  void* p = nullptr;
-  size_t bytes = 0;
-  Mem() = default;
-  Mem(Mem&& o) noexcept : p(o.p), bytes(o.bytes) { o.p = nullptr; }
-  Mem(const Mem&) = delete;
-  Mem& operator=(const Mem&) = delete;
-  ~Mem() {
-    if (p) (void)hipFree(p);
+struct Api {
+  static hipError_t alloc(void** p, size_t n) {
+    const hipError_t e = hipMalloc(p, n);
+    if (e != hipSuccess) (void)hipGetLastError();        // less may be asked for next
+    return e;
   }
-  void alloc(size_t n) {
-    check(hipMalloc(&p, n), "sequence workspace");
-    bytes = n;
-  }
+  static void free(void* p) { (void)hipFree(p); }
 };
+using Mem = SeqMem<Api>;
 
 }  // namespace
 
@@ -63,9 +57,7 @@ struct mure_seq {
   const SeqChunks* chunked = nullptr;
   int n_chunked = 0;
   int64_t n_slots = 0;
-  // Workspaces of the chunks' states; the last is the largest.  Smaller ones
-  // stay: a captured graph may hold them.
-  std::vector<Mem> work;
+  SeqWorkspace<Api> work;                      // the chunks' states
 };
 
 namespace {
@@ -260,7 +252,7 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
   s->n_chunked = (int)chunked.size();
   if (s->device >= 0) {
     check_device(s->device);
-    s->lists.alloc(host.size());
+    check(s->lists.alloc(host.size()), "work lists");
     check(hipMemcpyAsync(s->lists.p, host.data(), host.size(), hipMemcpyHostToDevice, s->stream), "upload of the work lists");
     check(hipStreamSynchronize(s->stream), "upload of the work lists");
     const char* d = static_cast<const char*>(s->lists.p);
@@ -367,12 +359,9 @@ void scan(mure_seq* s, const mure_seq_scan_args* args) {
   if (s->n_chunked) {
     const wide need = (wide)M * s->n_slots * D * (N + 1) * 4;
     if (need > MOST) throw Fail{MURE_E_NOMEM, "sequence workspace"};
-    if (s->work.empty() || s->work.back().bytes < (size_t)need) {
-      Mem m;                                   // twice the last: those that stay are no more than the largest
-      m.alloc(std::max((size_t)need, s->work.empty() ? 0 : 2 * s->work.back().bytes));
-      s->work.push_back(std::move(m));
-    }
-    k.ws_h = static_cast<float*>(s->work.back().p);
+    void* work = nullptr;
+    check(s->work.get((size_t)need, &work), "sequence workspace");
+    k.ws_h = static_cast<float*>(work);
     k.ws_d = k.ws_h + M * s->n_slots * D * N;
     k.chunks = s->chunked;
     k.n_chunked = s->n_chunked;

@@ -36,9 +36,12 @@
  *     nor another output, but where a call says so.
  *   - On a planning-only context the calls check their arguments and return
  *     MURE_E_UNSUPPORTED where they would launch.
- *   - Only mure_seq_create and the first mure_seq_scan of a size allocate;
- *     every other call may be captured into a HIP graph, which holds until
- *     the batch is destroyed.
+ *   - Every call but mure_seq_create may be captured into a HIP graph, which
+ *     holds until the batch is destroyed.  Scans of sequences of more than
+ *     MURE_SEQ_SPLIT_TOKENS tokens need a workspace: a batch has one for the
+ *     calls made directly, which grows with them, and one for each capture, kept
+ *     until the batch is destroyed.  So graphs may be replayed beside each other
+ *     and beside other calls, as far as their tensors allow it.
  */
 #ifndef MURE_SEQ_H
 #define MURE_SEQ_H

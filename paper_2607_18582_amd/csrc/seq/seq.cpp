@@ -29,13 +29,32 @@ void check(hipError_t e, const char* what) {
   throw Fail{e == hipErrorOutOfMemory ? MURE_E_NOMEM : MURE_E_DEVICE, std::string(what) + ": " + hipGetErrorString(e)};
 }
 
+// Allocations and frees are no part of a capture, of this stream or another one.
+struct Relaxed {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  Relaxed() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+  ~Relaxed() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+};
+
 struct Api {
   static hipError_t alloc(void** p, size_t n) {
+    Relaxed relaxed;
     const hipError_t e = hipMalloc(p, n);
     if (e != hipSuccess) (void)hipGetLastError();        // less may be asked for next
     return e;
   }
-  static void free(void* p) { (void)hipFree(p); }
+  static void free(void* p) {
+    Relaxed relaxed;
+    (void)hipFree(p);
+  }
+  static hipError_t synchronize(hipStream_t s) { return hipStreamSynchronize(s); }
+  static hipError_t capture(hipStream_t s, bool* on, unsigned long long* id) {
+    if (!s) return hipSuccess;                 // the null stream cannot be captured
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamGetCaptureInfo(s, &status, id);
+    *on = status != hipStreamCaptureStatusNone;
+    return e;
+  }
 };
 using Mem = SeqMem<Api>;
 
@@ -360,7 +379,7 @@ void scan(mure_seq* s, const mure_seq_scan_args* args) {
     const wide need = (wide)M * s->n_slots * D * (N + 1) * 4;
     if (need > MOST) throw Fail{MURE_E_NOMEM, "sequence workspace"};
     void* work = nullptr;
-    check(s->work.get((size_t)need, &work), "sequence workspace");
+    check(s->work.get(s->stream, (size_t)need, &work), "sequence workspace");
     k.ws_h = static_cast<float*>(work);
     k.ws_d = k.ws_h + M * s->n_slots * D * N;
     k.chunks = s->chunked;

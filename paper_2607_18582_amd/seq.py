@@ -90,7 +90,8 @@ def _one_of(table: dict, key, what: str) -> int:
 
 class Sequences:
     """A batch of sequences of ``lengths`` tokens, packed one after the other.
-    Made by ``Mure.sequences``."""
+    Made by ``Mure.sequences``.  It has to outlive the graphs that captured its
+    calls; each of them keeps a workspace of its own here."""
 
     def __init__(self, mure, lengths: Sequence[int]):
         self.mure, self.handle, self.args = mure, C.c_void_p(), _native(mure.lib)

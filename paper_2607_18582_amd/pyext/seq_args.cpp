@@ -8,6 +8,7 @@
 #include <ATen/EmptyTensor.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -41,6 +42,10 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
   const at::Tensor& t = THPVariable_Unpack(o);
   if (t.requires_grad() && at::GradMode::is_enabled())
     raise(PyExc_ValueError, std::string(what) + " requires a gradient, which no operator here has: call under torch.no_grad()");
+  if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(/*level=*/0).defined())
+    raise(PyExc_ValueError, std::string(what) + " has a forward tangent, which no operator here carries on");
+  if (t.is_neg()) raise(PyExc_ValueError, std::string(what) + " has the negative bit, its memory the other sign: call its resolve_neg()");
+  if (t._is_zerotensor()) raise(PyExc_ValueError, std::string(what) + " has no memory (a tensor of zeros of autograd)");
   return t;
 }
 

@@ -11,7 +11,7 @@ mutant axis or none.  A size-1 or expanded (stride 0) mutant axis counts as
 shared.  Rows may be strided (slices of a projection's output); a row's
 channels are contiguous.  Results have a mutant axis when any argument has.
 There are no gradients: a tensor that requires one is refused outside
-``torch.no_grad()``.
+``torch.no_grad()``, and so is one with a forward tangent.
 
 The library enqueues on its context's stream.  Where another stream is
 current in torch, the call is ordered after that stream's work and that stream

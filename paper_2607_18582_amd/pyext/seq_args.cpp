@@ -176,6 +176,11 @@ template <typename F> mure_status without_gil(F&& f) {
   Py_END_ALLOW_THREADS return st;
 }
 
+// A result's tensor that the caller gave counts as changed, where it keeps count.
+void written(mure_status st, PyObject* given, const at::Tensor& t) {
+  if (st == MURE_OK && THPVariable_Check(given) && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // (status, the first result, the second)
 PyObject* answer(mure_status st, PyObject* a, PyObject* b) {
   PyObject* r = Py_BuildValue("(iNN)", (int)st, a, b);
@@ -233,6 +238,8 @@ PyObject* conv(PyObject* const* p) {
   a.channels = (int32_t)c.width;
   a.n_taps = (int32_t)K;
   const mure_status st = without_gil([&] { return g_conv(seq, &a); });
+  written(st, p[10], out);
+  written(st, p[9], state);
   return answer(st, THPVariable_Wrap(out), THPVariable_Wrap(state));
 }
 
@@ -271,6 +278,8 @@ PyObject* scan(PyObject* const* p) {
   a.states = (int32_t)N;
   a.groups = (int32_t)(cols / N);
   const mure_status st = without_gil([&] { return g_scan(seq, &a); });
+  written(st, p[15], out);
+  written(st, p[14], state);
   return answer(st, THPVariable_Wrap(out), THPVariable_Wrap(state));
 }
 
@@ -318,6 +327,8 @@ PyObject* norm(PyObject* const* p) {
   a.channels = (int32_t)c.width;
   a.rows = c.rows;
   const mure_status st = without_gil([&] { return g_norm(ctx, &a); });
+  written(st, p[16], out);
+  written(st, p[15], res);
   return answer(st, res.defined() ? THPVariable_Wrap(res) : none(), out.defined() ? THPVariable_Wrap(out) : none());
 }
 

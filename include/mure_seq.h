@@ -173,7 +173,8 @@ typedef struct {
 } mure_seq_norm_args;
 mure_status mure_seq_norm(mure_ctx* ctx, const mure_seq_norm_args* args);
 
-/* Release the batch.  NULL is ignored.  Synchronises the context's stream. */
+/* Release the batch.  NULL is ignored.  Waits for the context's stream; one that
+ * is being captured stays so. */
 void mure_seq_destroy(mure_seq* seq);
 
 int32_t mure_seq_version(void);

@@ -473,7 +473,10 @@ void mure_seq_destroy(mure_seq* seq) {
   if (!seq) return;
   if (seq->device >= 0) {
     (void)hipSetDevice(seq->device);
-    (void)hipStreamSynchronize(seq->stream);
+    bool on = false;
+    unsigned long long id = 0;
+    // A wait would end a capture of the stream; what it had before is waited for by the frees.
+    if (Api::capture(seq->stream, &on, &id) != hipSuccess || !on) (void)hipStreamSynchronize(seq->stream);
   }
   delete seq;
 }

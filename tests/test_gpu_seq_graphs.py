@@ -82,3 +82,31 @@ def test_graphs_beside_each_other(own):
         torch.cuda.synchronize()
         for got, e in zip(out1 + out2 + (direct,), expected + [expected[2]]):
             assert torch.equal(got[0], e[0]) and torch.equal(got[1], e[1]), i
+
+
+def test_a_batch_closed_during_a_capture(own):
+    """A batch that is closed, or found by the garbage collector, while its context's stream is captured."""
+    print("[graphs] close", flush=True)
+    m, side = own
+    x, taps = torch.ones(604, 16, device="cuda"), torch.ones(16, 4, device="cuda")
+    seqs, other = m.sequences([600, 4]), m.sequences([5000, 5])
+    with torch.cuda.stream(side):
+        many = torch.randn(5005, 512, device="cuda")
+        expected = other.conv(many, torch.ones(512, 4, device="cuda"))[0]
+        side.synchronize()
+        taken = other.conv(many, torch.ones(512, 4, device="cuda"))[0]      # still running when the batch is closed
+
+    def call():
+        y, _ = seqs.conv(x, taps)
+        other.close()
+        return seqs.conv(y, taps)
+
+    graph, (y, _) = capture(side, call)
+    torch.cuda.synchronize()
+    assert torch.equal(taken, expected)
+    for i in range(3):
+        y.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float(y[3, 0]) == 1 + 2 + 3 + 4 and float(y[599, 5]) == 16, i

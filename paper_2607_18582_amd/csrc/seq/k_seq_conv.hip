@@ -2,7 +2,7 @@
 //   y[t][c] = act(b[c] + sum_k w[c][k] x[t - K + 1 + k][c]).
 //
 // 2 K operations for 2 elements moved: bound by HBM (65536 x 4096 bfloat16, 4
-// taps: 203 us, 5.3 TB/s; a copy of as much takes 200).  A thread owns 16 bytes
+// taps: 203 us, 5.3 TB/s; a copy of as much takes 181).  A thread owns 16 bytes
 // of channels (8 bfloat16, 4 float32) of one run of consecutive tokens; the
 // last K - 1 rows stay in its registers, so that a row is read once, but for
 // the K - 1 rows before the run, which the run before reads too.  Rows are

@@ -2,9 +2,11 @@
 //   v = after(y act(gate)),  r = residual + scale v,  out = before(r).
 //
 // A few operations per element moved: bound by HBM (65536 rows of 4096, gate,
-// bfloat16: 517 us, 5.2 TB/s, a copy of as much takes 507).  L lanes own a row (16 to
+// bfloat16: 517 us, 5.2 TB/s, a copy of as much takes 465).  L lanes own a row (16 to
 // a whole wave up to 2 vectors a lane, a block above) and keep it in registers
-// through both norms, so that every tensor is read or written once; means are
+// through both norms, so that every tensor is read or written once (above 8192
+// channels 92 to 132 bytes a lane are in scratch: 4096 rows of 16384 run at 2.8
+// to 4.6 TB/s); means are
 // taken over the lanes by cross-lane adds, over waves through LDS.  A block
 // goes from row to row and keeps the weights in registers; a row's inputs are
 // loaded before the row before it is computed, so that the loads are in flight
@@ -221,8 +223,10 @@ template <typename T, typename R, int L, int V, int N>
 static hipError_t norm_l(const mure_seq_norm_args& a, hipStream_t s) {
   constexpr int BLOCK = L > 256 ? L : 256, PER = BLOCK / L;
   const int vecs = (a.channels + N - 1) / N;
-  // Blocks that the chip holds at once (3 waves a SIMD where a lane has 16 channels, else 4), shared out over the
-  // mutants: 65536 rows of 4096 bfloat16 take 536 us with 768 blocks and 558 with 2048.
+  // Blocks that the chip holds at once where a SIMD has 3 waves (a lane of 16 channels) or 4, shared out over the
+  // mutants.  Times of 65536 rows of 4096 bfloat16 with 512, 768, 1024 and 2048 blocks: 511, 516, 546 and 532 us; with
+  // a float32 residual, of which a SIMD has 2 waves: 751, 771, 758 and 787; 16384 channels of which with 128, 192, 256
+  // and 512 blocks, one of them a CU, 4096 rows: 369, 292, 243 and 249.
   constexpr int FULL = (V * N == 16 ? 768 : 1024) * 256 / BLOCK;
   const int64_t most = std::max<int64_t>(1, FULL / a.n_mutants);
   const int64_t blocks = std::min<int64_t>((a.rows + PER - 1) / PER, most);

@@ -22,8 +22,9 @@
 // ENDS), one walks the chunks of every channel and state (seq_scan_join_kernel)
 // and one computes the outputs from the chunks' first states.
 //
-// 32768 tokens of 2048 channels and 16 states, bfloat16: 190, 20 and 255 us
-// at best, 424 to 436 us a call.  The two scans keep the vector ALU busy
+// 32768 tokens of 2048 channels and 16 states, bfloat16: 427 to 435 us a call
+// (its launches one by one under the profiler 193, 22 and 261, more than they
+// take in a call).  The two scans keep the vector ALU busy
 // all the time: of the second one's 113 instructions per quad and four tokens 80
 // are the recurrence, and the 20 transcendental ones take two slots.
 #include <algorithm>
@@ -324,10 +325,11 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs k, DivU32 dcb
 
 constexpr int JOIN = 64;                               // one wave a block: a long prompt of 2048 channels has 512 of them
 
-// The chunks' first states from their states from zero, in place: of 256 chunks of 2048 x 16 states 69 MB in 21 us,
+// The chunks' first states from their states from zero, in place: of 256 chunks of 2048 x 16 states 69 MB in 22 us,
 // bound by the chains' loads (32768 threads have 16 each in flight).  Where a chunk takes a state out of float's range,
 // or an infinite one by decays that may be 0 (0 times infinity is NaN), the state goes through it token by token, with
-// the operations of seq_scan_kernel: two parts past float's range may add up to a number.
+// the operations of seq_scan_kernel: two parts past float's range may add up to a number.  Rates that make every state
+// overflow take 0.7 ms.
 template <typename T>
 __global__ __launch_bounds__(JOIN) void seq_scan_join_kernel(SeqScanArgs k, DivU32 dn) {
   const mure_seq_scan_args& a = k.a;

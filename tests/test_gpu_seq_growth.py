@@ -203,3 +203,68 @@ def test_mixed_rates_of_many_mutants(mure, dtype, softplus):
     ey, el = R.scan(p["u"], p["dt"], p["A"], p["B"], p["C"], lengths, use_softplus=softplus, state=p["state"])
     R.close(y, ey, "out")
     R.close(last, el, "state")
+
+
+@pytest.mark.parametrize("dtype,more", [(torch.float32, 0.0), (torch.float32, 2.0 ** -14), (torch.bfloat16, 0.0)])
+def test_opposite_overflows_of_groups_and_mutants(mure, dtype, more):
+    """The same with groups, a bias of the steps, several mutants and sequences: each state goes through its own
+    group's and mutant's tokens, at its sequence's rows.  more: what the input exceeds the state by (0: it cancels
+    to a rounding, or to nothing)."""
+    print(f"[growth] opposite, groups {dtype} {more}", flush=True)
+    D, N, G, M, lengths = 6, 3, 3, 2, [20, 640, 530]
+    T = sum(lengths)
+    factor = torch.tensor([1.0, 2.0, 4.0])      # B of the groups, and the states that it cancels
+    p = dict(u=torch.zeros(M, T, D), dt=torch.full((M, T, D), -0.25), A=torch.ones(M, D, N), C=torch.ones(1, T, G * N),
+             B=factor.repeat_interleave(N).expand(1, T, G * N).clone(), skip=torch.ones(M, D), dt_bias=torch.full((1, D), 0.25),
+             state=factor.repeat_interleave(D // G)[:, None].expand(M, 3, D, N).clone())
+    p["A"][1] = 0.984375
+    for start, n in ((20, 640), (660, 530)):
+        p["dt"][:, start + 130:start + 256] = 0.5               # e^94.5 over the second chunk, of the second mutant e^93
+        p["dt"][:, start + 129] = -0.125                        # a step of 1/8
+        for m in range(M):
+            p["u"][m, start + 129] = -8 * torch.exp(torch.tensor(0.125) * p["A"][m, 0, 0]) * (1 + more)
+    p = {k: v.to(dtype) if k in ("u", "dt", "B", "C") else v for k, v in p.items()}
+    q = {k: v.cuda() for k, v in p.items()}
+
+    def run(seqs, rows, state):
+        return seqs.scan(q["u"][:, rows], q["dt"][:, rows], q["A"], q["B"][:, rows].expand(M, -1, -1), q["C"][:, rows], skip=q["skip"],
+                         dt_bias=q["dt_bias"], softplus=False, state=state)
+
+    y, last = run(mure.sequences(lengths), slice(0, T), q["state"])
+    start = 0
+    for i, n in enumerate(lengths):
+        state, parts = q["state"][:, i:i + 1].contiguous(), []
+        for at in range(0, n, 320):
+            count = min(320, n - at)
+            part, state = run(mure.sequences([count]), slice(start + at, start + at + count), state)
+            parts.append(part)
+        assert bool(state.isfinite().all()) and (i == 0 or not more or float(state.abs().min()) > 1e30)
+        assert torch.equal(last[:, i:i + 1], state) and torch.equal(y[:, start:start + n], torch.cat(parts, 1)), i
+        start += n
+
+
+def test_states_that_overflow_in_many_forms(mure):
+    """Softplus and bias, groups, mutated rates, sequences beside short ones: infinities where they are in parts."""
+    print("[growth] overflow forms", flush=True)
+    D, N, G, M, lengths = 10, 5, 2, 3, [600, 7, 1400, 512]
+    T, g = sum(lengths), torch.Generator().manual_seed(11)
+    normal = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    A = normal(M, D, N) * 0.6
+    B, C = normal(M, T, G * N).abs() + 0.1, normal(M, T, G * N)
+    u, dt, bias, state = normal(M, T, D).abs() + 0.1, normal(M, T, D) * 0.5 + 0.3, normal(1, D) * 0.2, normal(M, 4, D, N).abs()
+    q = [v.cuda() for v in (u, dt, A, B, C, bias, state)]
+
+    def run(seqs, rows, held):
+        return seqs.scan(q[0][:, rows], q[1][:, rows], q[2], q[3][:, rows], q[4][:, rows], dt_bias=q[5], state=held)
+
+    y, last = run(mure.sequences(lengths), slice(0, T), q[6])
+    row = 0
+    for i, n in enumerate(lengths):
+        held, parts = q[6][:, i:i + 1].contiguous(), []
+        for at in range(0, n, 400):
+            count = min(400, n - at)
+            part, held = run(mure.sequences([count]), slice(row + at, row + at + count), held)
+            parts.append(part)
+        assert same_kind(last[:, i:i + 1], held) and same_kind(y[:, row:row + n], torch.cat(parts, 1)), i
+        assert n < 500 or (bool(held.isinf().any()) and bool(held.isfinite().any()))
+        row += n

@@ -16,7 +16,7 @@ from typing import Dict, Optional, Sequence
 
 import numpy as np
 
-from . import seq as _seq
+from . import attn as _attn, seq as _seq
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmure.so")
@@ -153,6 +153,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         f.restype = res
         f.argtypes = args
     _seq.declare(lib)
+    _attn.declare(lib)
     _lib = lib
     return lib
 
@@ -182,7 +183,7 @@ def layer_descriptors(nodes) -> "C.Array":
     return arr
 
 
-class Mure(_seq.SeqOps):
+class Mure(_seq.SeqOps, _attn.AttnOps):
     """One library context on a GPU (``device`` >= 0) or a planning-only
     context (``device`` = -1)."""
 

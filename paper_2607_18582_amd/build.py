@@ -1,7 +1,7 @@
 """Build libmure.so (the C-ABI library) and libmure_peaks.so (the measured
 copy and MFMA ceilings, ``include/mure_peaks.h``) for gfx950 with hipcc, and
 _seq_args.so (the binding's marshalling of torch tensors for
-``include/mure_seq.h``, host code) with g++, in-tree.
+``include/mure_seq.h`` and ``include/mure_attn.h``, host code) with g++, in-tree.
 
     python -m paper_2607_18582_amd.build        # or build() from Python
 
@@ -27,7 +27,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libmure.so")
 PEAKS = os.path.join(HERE, "peaks")
 PEAKS_LIB = os.path.join(HERE, "libmure_peaks.so")
-PYEXT_SRC = os.path.join(HERE, "pyext", "seq_args.cpp")
+PYEXT_SRC = [os.path.join(HERE, "pyext", f) for f in ("seq_args.cpp", "attn_args.cpp")]
 PYEXT_LIB = os.path.join(HERE, "_seq_args.so")
 ARCH = "gfx950"
 
@@ -82,7 +82,7 @@ def _pyext(verbose: bool) -> None:
     inc = os.path.join(torch, "include")
     tmp = PYEXT_LIB + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-isystem", inc, "-isystem",
-           os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"], PYEXT_SRC,
+           os.path.join(inc, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"], *PYEXT_SRC,
            "-o", tmp, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

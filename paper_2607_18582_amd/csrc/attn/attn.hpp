@@ -1,0 +1,41 @@
+// Operators of an attention block (mure_attn.h): argument blocks and launchers
+// of their kernels.
+#pragma once
+
+#include "../../../include/mure_attn.h"
+#include "../seq/seq.hpp"
+
+namespace mure {
+
+struct AttnRotateArgs {
+  mure_attn_rotate_args a;
+  const SeqItem* items = nullptr;              // runs of tokens
+  int n_items = 0, item0 = 0, longest = 0;     // longest: tokens of a run
+  int64_t tokens = 0;
+};
+
+constexpr int ATTN_KEYS_SHORT = 512, ATTN_KEYS_MID = 1024;     // keys of a part, where they are worked on side by side
+
+struct AttnArgs {
+  mure_attn_attend_args a;
+  const SeqItem* items = nullptr;
+  int n_items = 0, item0 = 0;
+  int rows_each = 0;                           // rows of the workspace that an item has
+  int parts = 1;                               // of the keys
+  float* ws_o = nullptr;                       // [mutants][items][rows_each][heads][parts][head_dim], before the division
+  float* ws_ml = nullptr;                      // ... [2]: the largest exponent (of 2), the sum
+  bool fast = false;                           // rows of k, v and the caches are whole aligned 16-byte pieces
+};
+
+// launchers (return the launch status)
+hipError_t launch_attn_rotate(const AttnRotateArgs& a, hipStream_t s);
+// sequences of at most ATTN_SHORT tokens, runs of ATTN_ROWS tokens, and the results of parts of `keys` keys
+hipError_t attn_short_f32(const AttnArgs& a, hipStream_t s);
+hipError_t attn_short_bf16(const AttnArgs& a, hipStream_t s);
+hipError_t attn_runs_f32(const AttnArgs& a, hipStream_t s);
+hipError_t attn_runs_bf16(const AttnArgs& a, hipStream_t s);
+hipError_t attn_join_f32(const AttnArgs& a, int keys, hipStream_t s);
+hipError_t attn_join_bf16(const AttnArgs& a, int keys, hipStream_t s);
+hipError_t launch_attn_gated(const mure_attn_gated_args& a, bool fast, hipStream_t s);     // fast: as above, of x, gate and up
+
+}  // namespace mure

@@ -1,0 +1,352 @@
+// Kernels of attention (mure_attn_attend) and their launches, for one type of
+// tensors (compiled in a source of its own each).
+#pragma once
+
+#include "attn_dev.hpp"
+
+#include <algorithm>
+
+namespace mure {
+
+// One sequence's rows of keys and values of a head of one mutant.
+template <typename T> struct Source {
+  Rows<T> k, v;
+  int past, total;
+  bool bad;                                    // its past does not fit the cache
+  __device__ __forceinline__ Source(const AttnArgs& k_, const SeqItem& it, int m, int g) {
+    const mure_attn_attend_args& a = k_.a;
+    const bool held = a.k_cache.p;
+    past = held && a.past ? a.past[it.seq] : 0;
+    bad = held && (past < 0 || past > a.capacity - it.total);
+    total = past + it.total;
+    const int64_t row = it.row0 - it.pos0, c = (int64_t)g * a.head_dim;
+    k.past = v.past = past;
+    k.own = static_cast<const T*>(a.k.p) + m * a.k.mutant_stride + row * a.k.row_stride + c;
+    v.own = static_cast<const T*>(a.v.p) + m * a.v.mutant_stride + row * a.v.row_stride + c;
+    k.own_stride = a.k.row_stride;
+    v.own_stride = a.v.row_stride;
+    k.held = static_cast<const T*>(a.k_cache.p) + m * a.k_cache.mutant_stride + it.seq * a.k_cache.seq_stride + c;
+    v.held = static_cast<const T*>(a.v_cache.p) + m * a.v_cache.mutant_stride + it.seq * a.v_cache.seq_stride + c;
+    k.held_stride = a.k_cache.row_stride;
+    v.held_stride = a.v_cache.row_stride;
+  }
+  // The run's own keys and values into the cache; the call reads them from where they come from.
+  __device__ __forceinline__ void keep(const mure_attn_attend_args& a, const SeqItem& it, int m, int tid, int threads) const {
+    if (m && !a.k_cache.mutant_stride && !a.v_cache.mutant_stride) return;
+    const bool keep_k = !m || a.k_cache.mutant_stride, keep_v = !m || a.v_cache.mutant_stride;
+    constexpr int E = 16 / sizeof(T);
+    const int per = (a.head_dim + E - 1) / E;
+    for (int i = tid; i < it.len * per; i += threads) {
+      const int t = i / per, e = i % per * E, j = past + it.pos0 + t;
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        if (!(which ? keep_v : keep_k)) continue;
+        const Rows<T>& r = which ? v : k;
+        const T* from = r.at(j);
+        T* to = const_cast<T*>(r.held) + j * r.held_stride;
+        if (e + E <= a.head_dim) {
+          *reinterpret_cast<v4u_any*>(to + e) = *reinterpret_cast<const v4u_any*>(from + e);
+        } else {
+          for (int x = e; x < a.head_dim; ++x) to[x] = from[x];
+        }
+      }
+    }
+  }
+};
+
+// Head and mutant number i of n: neighbouring blocks go to the chip's eight dies in turn, so each die gets neighbouring
+// heads, which share keys and values in its L2.
+__device__ __forceinline__ int spread(int i, int n) { return n % 8 ? i : i % 8 * (n / 8) + i / 8; }
+
+// ---- runs of tokens: one head, 128 tokens, 32 of them a wave; tiles of keys and values in LDS, two at a time
+
+template <typename T, int DB> struct Run {
+  using H = Head<T, DB>;
+  static constexpr int KT = H::ROW <= 256 ? 64 : 32;           // keys of a tile
+  static constexpr int TILE = KT * H::ROW;
+  static constexpr int LDS = 4 * TILE;
+};
+
+template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <= 4 ? 2 : 1) void run_kernel(AttnArgs k) {
+  using R = Run<T, DB>;
+  constexpr int KT = R::KT, KB = KT / 32;
+  extern __shared__ char lds[];
+  const mure_attn_attend_args& a = k.a;
+  const int n = a.heads * a.n_mutants, hm = spread(blockIdx.x % n, n), m = hm / a.heads, h = hm % a.heads, group = a.heads / a.kv_heads, g = h / group;
+  const int at = blockIdx.x / n, part = at % k.parts, i = k.item0 + at / k.parts;
+  const SeqItem it = seq_item(k.items, i);
+  const Source<T> src(k, it, m, g);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5;
+  T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * a.out.row_stride + (int64_t)h * a.head_dim;
+  if (src.bad) {
+    if (part == 0)
+      for (int x = tid; x < it.len * a.head_dim; x += 256) out[x / a.head_dim * a.out.row_stride + x % a.head_dim] = from_f<T>(__builtin_nanf(""));
+    return;
+  }
+  if (a.k_cache.p && part == 0 && h % group == 0) src.keep(a, it, m, tid, 256);
+  // keys that any row of the block sees, in this part
+  const int first = src.past + it.pos0, last = first + it.len - 1;
+  int from, to, none;
+  sees(a, first, src.total, from, none);
+  sees(a, last, src.total, none, to);
+  if (k.parts > 1) {
+    from = max(from, part * ATTN_KEYS_MID);
+    to = (int)min((int64_t)to, (int64_t)(part + 1) * ATTN_KEYS_MID);
+    if (from >= to) return;
+  }
+  const int row = wave * 32 + (lane & 31), pos = min(first + row, last);
+  int lo, hi;
+  sees(a, pos, src.total, lo, hi);
+  // ... that all rows of the wave see, and that any of them sees
+  const int wave_first = min(first + wave * 32, last), wave_last = min(first + wave * 32 + 31, last);
+  int all_lo, all_hi, any_lo, any_hi;
+  sees(a, wave_first, src.total, any_lo, all_hi);
+  sees(a, wave_last, src.total, all_lo, any_hi);
+  const bool idle = wave * 32 >= it.len;
+  Query<T, DB> q;
+  load_query<T, DB>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)(pos - first)) * a.q.row_stride + (int64_t)h * a.head_dim,
+                    a.head_dim, half, a.scale);
+  const float c = factor(a.scale);
+  Running<DB> run;
+  run.start();
+  auto load = [&](int t, int buffer) {
+    char* tile = lds + buffer * 2 * R::TILE;
+    fetch<T, DB, KT, false, FAST>(tile, src.k, t, src.total, a.head_dim, wave, 4, lane);
+    fetch<T, DB, KT, true, FAST>(tile + R::TILE, src.v, t, src.total, a.head_dim, wave, 4, lane);
+  };
+  int t = from / KT * KT, buffer = 0;
+  load(t, 0);
+  for (; t < to; t += KT, buffer ^= 1) {
+    wait_copies();
+    __syncthreads();                           // the tile is there, and the last one has been used
+    if (t + KT < to) load(t + KT, buffer ^ 1);
+    if (idle || t >= any_hi || t + KT <= any_lo) continue;
+    const char* tile = lds + buffer * 2 * R::TILE;
+    v16f s[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) s[b] = scores<T, DB>(tile, 32 * b, lane, q);
+    // a tile that starts before the part's keys or ends behind them is cut to them
+    const int first_key = max(lo, from), end_key = min(hi, to);
+    if (t >= max(all_lo, from) && t + KT <= min(all_hi, to)) take<T, DB, KB, false>(run, s, tile + R::TILE, 0, 0, c, lane);
+    else take<T, DB, KB, true>(run, s, tile + R::TILE, first_key - t, end_key - t, c, lane);
+  }
+  if (row >= it.len) return;
+  const float l = run.l + other_half(run.l);
+  if (k.parts > 1) {
+    const int64_t at_row = (((int64_t)m * k.n_items + i) * k.rows_each + row) * a.heads + h, slot = at_row * k.parts + part;
+    store_row<float, DB>(k.ws_o + slot * a.head_dim, a.head_dim, run.o, 1.f, half);
+    if (!half) k.ws_ml[2 * slot] = run.m, k.ws_ml[2 * slot + 1] = l;
+  } else {
+    store_row<T, DB>(out + row * a.out.row_stride, a.head_dim, run.o, 1.f / l, half);
+  }
+}
+
+// ---- short sequences: 32 rows (token, head of a group) a block, the keys spread over its waves
+
+template <typename T, int DB> struct Short {
+  using H = Head<T, DB>;
+  static constexpr int KT = 32;
+  static constexpr int TILE = KT * H::ROW;
+  static constexpr int WAVES = 4;
+  static constexpr int PER = ATTN_KEYS_SHORT / WAVES;          // keys of a wave
+  static constexpr int TILES = 2 * WAVES * TILE <= 160 << 10 ? 2 : 1;    // of a wave: keys and values in one another's place where both do not fit
+  static constexpr int SUMS = 32 * 32 * DB * 4;
+  static constexpr int LDS = TILES * WAVES * TILE > SUMS + 1024 ? TILES * WAVES * TILE : SUMS + 1024;
+};
+
+template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <= 4 ? 2 : 1) void short_kernel(AttnArgs k, int units) {
+  using S = Short<T, DB>;
+  extern __shared__ char lds[];
+  const mure_attn_attend_args& a = k.a;
+  const int n = a.kv_heads * a.n_mutants, gm = spread(blockIdx.x % n, n), m = gm / a.kv_heads, g = gm % a.kv_heads, group = a.heads / a.kv_heads;
+  const int at = blockIdx.x / n, unit = at % units, part = at / units % k.parts, i = k.item0 + at / units / k.parts;
+  const SeqItem it = seq_item(k.items, i);
+  if (unit * 32 >= it.len * group) return;
+  const Source<T> src(k, it, m, g);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5;
+  // row r of the unit: token r / group, head g group + r % group
+  const int rows = min(32, it.len * group - unit * 32), r = min(unit * 32 + (lane & 31), it.len * group - 1), token = r / group, h = g * group + r % group;
+  T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * a.out.row_stride;
+  if (src.bad) {
+    if (part == 0)
+      for (int x = tid; x < rows * a.head_dim; x += 256) {
+        const int y = unit * 32 + x / a.head_dim;
+        out[y / group * a.out.row_stride + (int64_t)(g * group + y % group) * a.head_dim + x % a.head_dim] = from_f<T>(__builtin_nanf(""));
+      }
+    return;
+  }
+  if (a.k_cache.p && part == 0 && unit == 0) src.keep(a, it, m, tid, 256);
+  int lo, hi, from, to, none;
+  sees(a, src.past + token, src.total, lo, hi);
+  sees(a, src.past, src.total, from, none);
+  sees(a, src.total - 1, src.total, none, to);
+  const int64_t part0 = (int64_t)part * ATTN_KEYS_SHORT;
+  if (max((int64_t)from, part0) >= min((int64_t)to, part0 + ATTN_KEYS_SHORT)) return;
+  from = (int)max((int64_t)from, part0 + wave * S::PER);
+  to = (int)min((int64_t)to, part0 + (wave + 1) * S::PER);
+  Query<T, DB> q;
+  load_query<T, DB>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)token) * a.q.row_stride + (int64_t)h * a.head_dim, a.head_dim,
+                    half, a.scale);
+  const float c = factor(a.scale);
+  Running<DB> run;
+  run.start();
+  char* tile = lds + wave * S::TILES * S::TILE;
+  char* vtile = tile + (S::TILES - 1) * S::TILE;
+  auto landed = [] {                           // the wave's own copies
+    wait_copies();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  for (int t = from / S::KT * S::KT; t < to; t += S::KT) {
+    __builtin_amdgcn_wave_barrier();
+    fetch<T, DB, S::KT, false, FAST>(tile, src.k, t, src.total, a.head_dim, 0, 1, lane);
+    if constexpr (S::TILES == 2) fetch<T, DB, S::KT, true, FAST>(vtile, src.v, t, src.total, a.head_dim, 0, 1, lane);
+    landed();
+    v16f s[1] = {scores<T, DB>(tile, 0, lane, q)};
+    if constexpr (S::TILES == 1) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      fetch<T, DB, S::KT, true, FAST>(vtile, src.v, t, src.total, a.head_dim, 0, 1, lane);
+      landed();
+    }
+    take<T, DB, 1, true>(run, s, vtile, max(lo, from) - t, min(hi, to) - t, c, lane);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  // the waves' sums, added in order
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(lds);
+  float* ml = reinterpret_cast<float*>(lds + S::SUMS);         // [4][32][2]
+  const float l = run.l + other_half(run.l);
+  if (!half) ml[(wave * 32 + lane) * 2] = run.m, ml[(wave * 32 + lane) * 2 + 1] = l;
+  __syncthreads();
+  float m_all = ml[(lane & 31) * 2];
+  for (int w = 1; w < S::WAVES; ++w) m_all = fmaxf(m_all, ml[(w * 32 + (lane & 31)) * 2]);
+  const float base = m_all == -__builtin_inff() ? 0.f : m_all;
+  float l_all = 0.f;
+  for (int w = 0; w < S::WAVES; ++w) l_all += ml[(w * 32 + (lane & 31)) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * 32 + (lane & 31)) * 2] - base);
+  const float f = __builtin_amdgcn_exp2f(run.m - base);
+  for (int w = 0; w < S::WAVES; ++w) {
+    if (w == wave && from < to)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          float* p = sums + (32 * d + 8 * (x / 4) + 4 * half + x % 4) * 32 + (lane & 31);
+          *p = (w ? *p : 0.f) + run.o[d][x] * f;
+        }
+    else if (w == 0 && wave == 0)
+      for (int x = lane; x < 1024 * DB; x += 64) sums[x] = 0.f;
+    __syncthreads();
+  }
+  if (wave == 0 && !half) ml[lane * 2] = m_all, ml[lane * 2 + 1] = l_all;
+  __syncthreads();
+  for (int x = tid; x < rows * a.head_dim; x += 256) {
+    const int y = x / a.head_dim, e = x % a.head_dim, all = unit * 32 + y, tk = all / group, hd = g * group + all % group;
+    const float v = sums[e * 32 + y];
+    if (k.parts > 1) {
+      const int64_t slot = ((((int64_t)m * k.n_items + i) * k.rows_each + tk) * a.heads + hd) * k.parts + part;
+      k.ws_o[slot * a.head_dim + e] = v;
+      if (e < 2) k.ws_ml[2 * slot + e] = ml[2 * y + e];
+      if (e == 0 && a.head_dim == 1) k.ws_ml[2 * slot + 1] = ml[2 * y + 1];
+    } else {
+      out[tk * a.out.row_stride + (int64_t)hd * a.head_dim + e] = from_f<T>(v * (1.f / ml[2 * y + 1]));
+    }
+  }
+}
+
+// ---- the parts' results of one token and head, added in order
+
+template <typename T> __global__ __launch_bounds__(256) void join_kernel(AttnArgs k, int keys, int64_t total_rows) {
+  const mure_attn_attend_args& a = k.a;
+  const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (x >= total_rows) return;
+  const int h = x % a.heads, row = x / a.heads % k.rows_each;
+  const int64_t im = x / a.heads / k.rows_each;
+  const int i = im % k.n_items, m = im / k.n_items;
+  const SeqItem it = seq_item(k.items, i);
+  if (row >= it.len) return;
+  const int past = a.past ? a.past[it.seq] : 0;
+  if (past < 0 || past > a.capacity - it.total) return;        // NaN already
+  int lo, hi, none, block_lo, block_hi;
+  sees(a, past + it.pos0 + row, past + it.total, lo, hi);
+  // parts that the kernel worked on: those with keys of any of the item's rows
+  sees(a, past + it.pos0, past + it.total, block_lo, none);
+  sees(a, past + it.pos0 + it.len - 1, past + it.total, none, block_hi);
+  const int p0 = lo / keys, p1 = (hi - 1) / keys;
+  const int64_t slot = x * k.parts;
+  float mx = -__builtin_inff();
+  for (int p = p0; p <= p1; ++p) mx = fmaxf(mx, k.ws_ml[2 * (slot + p)]);
+  const float base = mx == -__builtin_inff() ? 0.f : mx;
+  float l = 0.f, o[4] = {};
+  for (int p = p0; p <= p1; ++p) {
+    const float f = __builtin_amdgcn_exp2f(k.ws_ml[2 * (slot + p)] - base);
+    l += k.ws_ml[2 * (slot + p) + 1] * f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (lane + 64 * j < a.head_dim) o[j] += k.ws_o[(slot + p) * a.head_dim + lane + 64 * j] * f;
+  }
+  T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (it.row0 + (int64_t)row) * a.out.row_stride + (int64_t)h * a.head_dim;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (lane + 64 * j < a.head_dim) out[lane + 64 * j] = from_f<T>(o[j] * (1.f / l));
+}
+
+// ---- launches
+
+constexpr int64_t BLOCKS = (1 << 24) - 1;
+
+// `each` blocks an item, as many items a launch as fit
+template <typename F> hipError_t over_items(AttnArgs& k, int64_t each, F&& f) {
+  const int n = k.n_items;
+  const int most = (int)std::min<int64_t>(n, BLOCKS / each);
+  for (k.item0 = 0; k.item0 < n; k.item0 += most)
+    if (const hipError_t e = f((unsigned)(each * std::min(most, n - k.item0))); e != hipSuccess) return e;
+  return hipSuccess;
+}
+
+template <typename... P, typename... A> hipError_t launch_lds(void (*kernel)(P...), unsigned grid, unsigned lds, hipStream_t s, A&&... a) {
+  if (lds > 65536)                             // more than the default limit has to be asked for
+    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
+  std::tuple<P...> params(std::forward<A>(a)...);
+  return std::apply(
+      [&](auto&... p) {
+        void* at[] = {&p...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(256), at, lds, s);
+      },
+      params);
+}
+
+template <typename T, int DB, bool FAST> hipError_t short_f(AttnArgs k, hipStream_t s) {
+  const int units = (k.rows_each * (k.a.heads / k.a.kv_heads) + 31) / 32;
+  return over_items(k, (int64_t)k.a.kv_heads * k.a.n_mutants * units * k.parts,
+                    [&](unsigned grid) { return launch_lds(short_kernel<T, DB, FAST>, grid, Short<T, DB>::LDS, s, k, units); });
+}
+
+template <typename T, int DB, bool FAST> hipError_t runs_f(AttnArgs k, hipStream_t s) {
+  return over_items(k, (int64_t)k.a.heads * k.a.n_mutants * k.parts,
+                    [&](unsigned grid) { return launch_lds(run_kernel<T, DB, FAST>, grid, Run<T, DB>::LDS, s, k); });
+}
+
+template <typename T, int DB> hipError_t with_speed(const AttnArgs& k, bool brief, hipStream_t s) {
+  if (brief) return k.fast ? short_f<T, DB, true>(k, s) : short_f<T, DB, false>(k, s);
+  return k.fast ? runs_f<T, DB, true>(k, s) : runs_f<T, DB, false>(k, s);
+}
+
+template <typename T> hipError_t with_head(const AttnArgs& k, bool brief, hipStream_t s) {
+  const int d = k.a.head_dim;
+  if (d <= 32) return with_speed<T, 1>(k, brief, s);
+  if (d <= 64) return with_speed<T, 2>(k, brief, s);
+  if (d <= 96) return with_speed<T, 3>(k, brief, s);
+  if (d <= 128) return with_speed<T, 4>(k, brief, s);
+  if (d <= 192) return with_speed<T, 6>(k, brief, s);
+  return with_speed<T, 8>(k, brief, s);
+}
+
+template <typename T> hipError_t join(const AttnArgs& k, int keys, hipStream_t s) {
+  const int64_t rows = (int64_t)k.a.n_mutants * k.n_items * k.rows_each * k.a.heads, blocks = (rows + 3) / 4;
+  if (blocks > BLOCKS) return hipErrorInvalidConfiguration;
+  return launch(join_kernel<T>, dim3((unsigned)blocks), 256, s, k, keys, rows);
+}
+
+}  // namespace mure

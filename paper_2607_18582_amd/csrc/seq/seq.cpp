@@ -1,204 +1,15 @@
-// C ABI of the sequence operators (mure_seq.h): batches, checks of arguments,
-// workspaces and launches.
-#include "seq.hpp"
-#include "workspace.hpp"
+// C ABI of the sequence operators (mure_seq.h): batches, checks of a call's
+// arguments, and launches.
+#include "batch.hpp"
 
 #include <algorithm>
 #include <cmath>
-#include <exception>
 #include <memory>
-#include <new>
 #include <vector>
 
 using namespace mure;
 
 namespace {
-
-typedef __int128 wide;
-
-struct Fail {
-  mure_status st;
-  std::string msg;
-};
-
-[[noreturn]] void invalid(const std::string& m) { throw Fail{MURE_E_INVALID, m}; }
-
-void check(hipError_t e, const char* what) {
-  if (e == hipSuccess) return;
-  (void)hipGetLastError();                     // reported here: not again by a later launch
-  throw Fail{e == hipErrorOutOfMemory ? MURE_E_NOMEM : MURE_E_DEVICE, std::string(what) + ": " + hipGetErrorString(e)};
-}
-
-// Allocations and frees are no part of a capture, of this stream or another one.
-struct Relaxed {
-  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
-  Relaxed() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
-  ~Relaxed() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
-};
-
-struct Api {
-  static hipError_t alloc(void** p, size_t n) {
-    Relaxed relaxed;
-    const hipError_t e = hipMalloc(p, n);
-    if (e != hipSuccess) (void)hipGetLastError();        // less may be asked for next
-    return e;
-  }
-  static void free(void* p) {
-    Relaxed relaxed;
-    (void)hipFree(p);
-  }
-  static hipError_t synchronize(hipStream_t s) { return hipStreamSynchronize(s); }
-  static hipError_t capture(hipStream_t s, bool* on, unsigned long long* id) {
-    if (!s) return hipSuccess;                 // the null stream cannot be captured
-    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    const hipError_t e = hipStreamGetCaptureInfo(s, &status, id);
-    *on = status != hipStreamCaptureStatusNone;
-    return e;
-  }
-};
-using Mem = SeqMem<Api>;
-
-}  // namespace
-
-struct mure_seq {
-  mure_ctx* ctx = nullptr;
-  int device = -1;
-  hipStream_t stream = nullptr;
-  int64_t n_seq = 0, tokens = 0, longest = 0;
-  // work lists, in device memory
-  Mem lists;
-  const SeqItem* conv[N_RUNS] = {};            // runs of at most CONV_RUNS tokens
-  int n_conv[N_RUNS] = {};
-  const SeqItem* scan = nullptr;               // whole sequences and chunks, longest first
-  int n_scan = 0;
-  const SeqItem* ends = nullptr;               // the chunks but each sequence's last
-  int n_ends = 0;
-  const SeqChunks* chunked = nullptr;
-  int n_chunked = 0;
-  int64_t n_slots = 0;
-  SeqWorkspace<Api> work;                      // the chunks' states
-};
-
-namespace {
-
-template <typename F>
-mure_status guarded(mure_ctx* ctx, F&& f) noexcept {
-  mure_status st = MURE_E_INVALID;
-  try {
-    std::string msg;
-    try {
-      f();
-      return MURE_OK;
-    } catch (const Fail& e) {
-      st = e.st;
-      msg = e.msg;
-    } catch (const std::bad_alloc&) {
-      st = MURE_E_NOMEM;
-      msg = "host memory exhausted";
-    } catch (const std::exception& e) {
-      msg = e.what();
-    }
-    if (ctx) *ctx_view(ctx).err = msg;
-  } catch (...) {
-  }
-  return st;
-}
-
-// ---- checks of arguments
-
-constexpr wide MOST = (wide)1 << 60;           // elements of a tensor, from its first to its last
-
-// The elements that an output writes or an input reads: rows of `width`
-// elements, `rows` of them `row_stride` apart, `mutants` times.
-struct Span {
-  const char* name;
-  const char* p;
-  int64_t esize, width, rows, row_stride, mutants, mutant_stride;
-  wide extent() const {                        // bytes from the first element past the last
-    if (rows == 0 || width == 0) return 0;
-    return ((wide)(mutants - 1) * mutant_stride + (wide)(rows - 1) * row_stride + width) * esize;
-  }
-};
-
-Span span(const char* name, const void* p, int64_t esize, int64_t width, int64_t rows, int64_t row_stride, int64_t mutants,
-          int64_t mutant_stride) {
-  if (!p && rows > 0) invalid(std::string(name) + " is NULL");
-  if (row_stride < 0 || mutant_stride < 0) invalid(std::string(name) + ": a stride is negative");
-  Span s{name, static_cast<const char*>(p), esize, width, rows, rows > 1 ? row_stride : 0, mutants, mutants > 1 ? mutant_stride : 0};
-  if (s.extent() > MOST) invalid(std::string(name) + ": its strides pass the address space");
-  if (reinterpret_cast<uintptr_t>(p) % esize) invalid(std::string(name) + " is not aligned to its elements");
-  return s;
-}
-
-// An output's elements are apart from each other.
-void check_output(const Span& s) {
-  if (s.extent() == 0) return;
-  const wide rows = (wide)(s.rows - 1) * s.row_stride + s.width, muts = (wide)(s.mutants - 1) * s.mutant_stride + s.width;
-  const bool rows_inside = (s.rows == 1 || s.row_stride >= s.width) && (s.mutants == 1 || s.mutant_stride >= rows);
-  const bool muts_inside = (s.mutants == 1 || s.mutant_stride >= s.width) && (s.rows == 1 || s.row_stride >= muts);
-  if (!rows_inside && !muts_inside) invalid(std::string(s.name) + ": its rows overlap");
-}
-
-// Whether two tensors may share memory.  Rows side by side in one buffer (the
-// same pitch, at different columns) do not.
-bool meet(const Span& a, const Span& b) {
-  if (a.extent() == 0 || b.extent() == 0) return false;
-  const wide pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
-  if (pa + a.extent() <= pb || pb + b.extent() <= pa) return false;
-  // The pitch in bytes of a tensor of several rows, and of one with one row
-  // per mutant, or none.
-  auto pitch = [](const Span& s) { return (s.rows > 1 ? s.row_stride : s.mutant_stride) * (wide)s.esize; };
-  const wide q = pitch(a);
-  if (q == 0 || pitch(b) != q) return true;
-  for (const Span* s : {&a, &b})
-    if ((wide)s->mutant_stride * s->esize % q || (wide)s->width * s->esize > q) return true;
-  const wide d = ((pb - pa) % q + q) % q;      // b's first column, as a's rows see it
-  return d < (wide)a.width * a.esize || d + (wide)b.width * b.esize > q;
-}
-
-bool same(const Span& a, const Span& b) {
-  return a.p == b.p && a.esize == b.esize && a.row_stride == b.row_stride && a.mutant_stride == b.mutant_stride &&
-         (a.mutants == 1 || a.mutant_stride > 0);
-}
-
-// The tensors of a call (a norm has the most, 10).
-struct Spans {
-  Span v[10];
-  int n = 0;
-  void push_back(const Span& s) { v[n++] = s; }
-  const Span* begin() const { return v; }
-  const Span* end() const { return v + n; }
-};
-
-// `out` may be one of `allowed`, element by element, and may meet nothing else.
-void check_apart(const Span& out, const Spans& others, std::initializer_list<const Span*> allowed = {}) {
-  for (const Span& o : others) {
-    if (!meet(out, o)) continue;
-    bool ok = false;
-    for (const Span* s : allowed) ok = ok || (s && s->p == o.p && s->name == o.name && same(out, o));
-    if (!ok) invalid(std::string(out.name) + " overlaps " + o.name);
-  }
-}
-
-int64_t esize_of(int32_t dtype, const char* what) {
-  if (dtype != MURE_F32 && dtype != MURE_BF16) invalid(std::string(what) + ": unknown type");
-  return dtype == MURE_F32 ? 4 : 2;
-}
-
-void check_range(int64_t v, int64_t lo, int64_t hi, const char* what) {
-  if (v < lo || v > hi)
-    invalid(std::string(what) + " is " + std::to_string(v) + ", outside " + std::to_string(lo) + " ... " + std::to_string(hi));
-}
-
-// An optional float32 parameter of n values a mutant.
-void add_param(Spans& in, const char* name, const mure_seq_param& p, int64_t n, int64_t mutants) {
-  if (p.p) in.push_back(span(name, p.p, 4, n, 1, 0, mutants, p.mutant_stride));
-}
-
-void check_device(int device) {
-  if (device < 0) throw Fail{MURE_E_UNSUPPORTED, "planning-only context"};
-  check(hipSetDevice(device), "hipSetDevice");
-}
 
 // ---- batches
 
@@ -254,8 +65,31 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
   // the longest first, so that a launch does not end with one long run
   std::stable_sort(scan.begin(), scan.end(), [](const SeqItem& a, const SeqItem& b) { return a.len > b.len; });
   s->n_slots = slots;
+  std::vector<SeqItem> brief, runs;
+  row = 0;
+  for (int32_t i = 0; i < (int32_t)n_seq; row += lengths[i++]) {
+    const int64_t L = lengths[i];
+    if (L == 0) continue;
+    if (L <= ATTN_SHORT) {
+      add_runs(brief, i, row, L, L, -1);
+      s->longest_brief = std::max(s->longest_brief, (int)L);
+      s->brief_tokens += L;
+    } else {
+      add_runs(runs, i, row, L, ATTN_ROWS, -1);
+      if (L <= ATTN_MID) s->mid_tokens += L;
+      else s->n_long_runs += (int)((L + ATTN_ROWS - 1) / ATTN_ROWS);
+    }
+  }
+  std::stable_sort(brief.begin(), brief.end(), [](const SeqItem& a, const SeqItem& b) { return a.len > b.len; });
+  // a causal run's work is that of the tokens up to its end
+  std::stable_sort(runs.begin(), runs.end(), [](const SeqItem& a, const SeqItem& b) {
+    const bool la = a.total > ATTN_MID, lb = b.total > ATTN_MID;
+    return la != lb ? la : a.pos0 + a.len > b.pos0 + b.len;
+  });
+  s->n_brief = (int)brief.size();
+  s->n_runs = (int)runs.size();
   std::vector<char> host;
-  size_t at[N_RUNS + 3];
+  size_t at[N_RUNS + 5];
   int k = 0;
   auto put = [&](const void* p, size_t bytes) {
     at[k++] = host.size();
@@ -265,6 +99,7 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
   for (const auto& v : conv) put(v.data(), v.size() * sizeof(SeqItem));
   for (const auto* v : {&scan, &ends}) put(v->data(), v->size() * sizeof(SeqItem));
   put(chunked.data(), chunked.size() * sizeof(SeqChunks));
+  for (const auto* v : {&brief, &runs}) put(v->data(), v->size() * sizeof(SeqItem));
   for (int i = 0; i < N_RUNS; ++i) s->n_conv[i] = (int)conv[i].size();
   s->n_scan = (int)scan.size();
   s->n_ends = (int)ends.size();
@@ -280,6 +115,8 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
     if (!ones) s->scan = reinterpret_cast<const SeqItem*>(d + at[N_RUNS]);
     s->ends = reinterpret_cast<const SeqItem*>(d + at[N_RUNS + 1]);
     s->chunked = reinterpret_cast<const SeqChunks*>(d + at[N_RUNS + 2]);
+    if (!ones) s->brief = reinterpret_cast<const SeqItem*>(d + at[N_RUNS + 3]);
+    s->runs = reinterpret_cast<const SeqItem*>(d + at[N_RUNS + 4]);
   }
   *out = s.release();
 }
@@ -476,7 +313,7 @@ void mure_seq_destroy(mure_seq* seq) {
     bool on = false;
     unsigned long long id = 0;
     // A wait would end a capture of the stream; what it had before is waited for by the frees.
-    if (Api::capture(seq->stream, &on, &id) != hipSuccess || !on) (void)hipStreamSynchronize(seq->stream);
+    if (SeqApi::capture(seq->stream, &on, &id) != hipSuccess || !on) (void)hipStreamSynchronize(seq->stream);
   }
   delete seq;
 }

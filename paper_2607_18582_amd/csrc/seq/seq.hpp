@@ -31,6 +31,8 @@ struct SeqChunks {
 constexpr int SCAN_CHUNK = 128;                // tokens of a chunk
 constexpr int CONV_RUNS[] = {33, 12, 3};       // tokens of a convolution's runs
 constexpr int N_RUNS = 3;
+constexpr int ATTN_SHORT = 16, ATTN_MID = 512; // tokens of sequences that attention takes in other ways
+constexpr int ATTN_ROWS = 128;                 // tokens of a run of the others
 
 struct SeqConvArgs {
   mure_seq_conv_args a;

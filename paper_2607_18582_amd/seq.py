@@ -1,7 +1,7 @@
 """The operators of a selective state space block (``include/mure_seq.h``):
 ``Mure.sequences`` registers the lengths of a test set's sequences and returns
-a ``Sequences``, whose ``conv`` and ``scan`` run over them; ``Mure.block_norm``
-works row by row.
+a ``Sequences``, whose ``conv`` and ``scan`` run over them (and the operators of
+``attn.py``); ``Mure.block_norm`` works row by row.
 
 Argument marshalling only, as in ``binding.py``, the tensors' part of it in C++
 (``pyext/seq_args.cpp``).  Activations are CUDA tensors of packed rows,
@@ -24,14 +24,15 @@ from typing import Optional, Sequence
 
 import numpy as np
 
+from .attn import AttnBatch
+from .calls import call as _call, native as _native, one_of as _one_of
+
 SEQ_EXPORTED = ["mure_seq_version", "mure_seq_create", "mure_seq_destroy", "mure_seq_conv", "mure_seq_scan",
                 "mure_seq_norm"]
 SEQ_VERSION = 1
 ACTIVATIONS = {None: 0, "silu": 1, "sigmoid": 2}
 NORMS = {None: 0, "rms": 1, "layer": 2}
 GATES = {"before": 1, "after": 2}
-
-_args = _raw_stream = None                      # the native marshalling; torch's current stream of a device
 
 
 def declare(lib: C.CDLL) -> None:
@@ -46,49 +47,7 @@ def declare(lib: C.CDLL) -> None:
         f.restype, f.argtypes = res, args
 
 
-def _native(lib: C.CDLL):
-    """The marshalling module, bound to the library; raises if it has not been built."""
-    global _args, _raw_stream
-    if _args is None:
-        import torch
-        try:
-            from . import _seq_args
-        except ImportError as e:
-            raise RuntimeError("_seq_args.so is missing or stale: build it first "
-                               "(python -m paper_2607_18582_amd.build)") from e
-        _seq_args.bind(*(C.cast(f, C.c_void_p).value for f in (lib.mure_seq_conv, lib.mure_seq_scan, lib.mure_seq_norm)))
-        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
-            (lambda device: torch.cuda.current_stream(device).cuda_stream)
-        _args = _seq_args
-    return _args
-
-
-def _call(mure, fn, *args):
-    """fn's two results, the call on the context's stream ordered with torch's current one."""
-    device = mure.device
-    if device < 0 or _raw_stream(device) == mure.stream:
-        status, a, b = fn(*args)
-    else:
-        from torch import cuda
-        current = cuda.current_stream(device)
-        own = cuda.ExternalStream(mure.stream, device=device) if mure.stream else cuda.default_stream(device)
-        own.wait_stream(current)
-        status, a, b = fn(*args)
-        current.wait_stream(own)
-    if status:
-        mure._check(status)
-    return a, b
-
-
-def _one_of(table: dict, key, what: str) -> int:
-    if key is None or isinstance(key, str):
-        code = table.get(key)
-        if code is not None:
-            return code
-    raise ValueError(f"{what} is {key!r}; one of {', '.join(map(repr, table))} is needed")
-
-
-class Sequences:
+class Sequences(AttnBatch):
     """A batch of sequences of ``lengths`` tokens, packed one after the other.
     Made by ``Mure.sequences``.  It has to outlive the graphs that captured its
     calls; each of them keeps a workspace of its own here."""

@@ -1,0 +1,204 @@
+"""The operators of an attention block on the GPU, against their definitions in
+float64 with rounding bounds (``attn_reference``)."""
+import pytest
+import torch
+
+import attn_reference as R
+from paper_2607_18582_amd import Mure
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+RAGGED = [5, 0, 1, 33, 17, 64, 3, 130, 16, 0]
+
+
+@pytest.fixture(scope="module")
+def mure():
+    m = Mure(device=0)
+    yield m
+    m.close()
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def normal(g, *shape, dtype=torch.float32, mean=0.0, std=1.0):
+    """On the CPU, already rounded to dtype."""
+    return (torch.randn(*shape, generator=g) * std + mean).to(dtype)
+
+
+def cuda(*tensors):
+    return [None if t is None else t.cuda() for t in tensors]
+
+
+# ---------------------------------------------------------------- norm and rotation
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,pairs,H,G,norm,interleaved,M,own", [
+    (128, 64, 4, 2, "rms", False, 1, True), (64, 32, 3, 1, "layer", True, 3, True), (32, 8, 5, 5, None, False, 2, False),
+    (80, 20, 2, 1, "rms", False, 1, True), (17, 8, 3, 2, "layer", False, 2, True), (256, 128, 1, 1, "rms", True, 1, True),
+    (255, 127, 2, 1, "rms", False, 1, True), (1, 0, 4, 4, "rms", False, 2, True), (2, 1, 4, 2, None, True, 1, True),
+    (96, 0, 2, 2, "layer", False, 1, True), (130, 60, 2, 1, "rms", True, 1, True), (20, 10, 40, 8, "rms", False, 1, True)])
+def test_rotate(mure, dtype, dim, pairs, H, G, norm, interleaved, M, own):
+    say(f"[rotate] {dtype} dim={dim} pairs={pairs} H={H} G={G} {norm} M={M}")
+    g = torch.Generator().manual_seed(dim + pairs)
+    T, dt = sum(RAGGED), TYPES[dtype]
+    q, k = normal(g, M, T, H * dim, dtype=dt, mean=0.2), normal(g, M if own else 1, T, G * dim, dtype=dt)
+    f = torch.rand(M, pairs, generator=g) * 2
+    wq, wk = (normal(g, M, dim, mean=1, std=0.2), normal(g, 1, dim, mean=1, std=0.2)) if norm else (None, None)
+    past = torch.randint(0, 5000, (len(RAGGED),), generator=g, dtype=torch.int32)
+    seqs = mure.sequences(RAGGED)
+    for p in (None, past):
+        gq, gk = seqs.rotate(*cuda(q, k, f), head_dim=dim, norm=norm, q_weight=cuda(wq)[0], k_weight=cuda(wk)[0], eps=1e-5, past=cuda(p)[0],
+                             interleaved=interleaved)
+        R.close(gq, R.rotate(q, f, RAGGED, dim, norm, wq, 1e-5, p, interleaved=interleaved), "q")
+        R.close(gk, R.rotate(k, f, RAGGED, dim, norm, wk, 1e-5, p, interleaved=interleaved), "k")
+
+
+def test_rotate_positions_of_several_axes(mure):
+    say("[rotate axes]")
+    g = torch.Generator().manual_seed(3)
+    lengths, dim, sections = [40, 0, 7], 48, [10, 7, 7]
+    q, f = normal(g, 1, 47, 2 * dim), torch.rand(1, 24, generator=g)
+    at = torch.randint(-1000, 1000, (3, 47), generator=g, dtype=torch.int32)
+    seqs = mure.sequences(lengths)
+    y, none = seqs.rotate(q[0].cuda(), None, f[0].cuda(), head_dim=dim, positions=at.cuda(), sections=sections)
+    assert none is None and y.shape == (47, 2 * dim)
+    R.close(y[None], R.rotate(q, f, lengths, dim, positions=at, sections=sections), "q")
+    one, _ = seqs.rotate(q[0].cuda(), None, f[0].cuda(), head_dim=dim, positions=at[:1].contiguous().cuda())
+    R.close(one[None], R.rotate(q, f, lengths, dim, positions=at[:1], sections=[24]), "q, one axis")
+    skip, _ = seqs.rotate(q[0].cuda(), None, f[0].cuda(), head_dim=dim, positions=at.cuda(), sections=[0, 24, 0])
+    R.close(skip[None], R.rotate(q, f, lengths, dim, positions=at[1:2], sections=[24]), "q, an axis of three")
+
+
+@pytest.mark.parametrize("at", [0, 1, 131071, 1 << 24, (1 << 31) - 5])
+def test_rotate_far_positions(mure, at):
+    """A float32 product of position and frequency would be off by whole turns."""
+    say(f"[rotate far] {at}")
+    g = torch.Generator().manual_seed(4)
+    q, f = normal(g, 1, 3, 64), (10000.0 ** (-torch.arange(16).double() / 16)).float()[None]
+    past = torch.tensor([at], dtype=torch.int32)
+    y, _ = mure.sequences([3]).rotate(*cuda(q), None, *cuda(f), head_dim=32, past=past.cuda())
+    R.close(y, R.rotate(q, f, [3], 32, past=past), "q")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rotate_in_place_and_strided(mure, dtype):
+    say(f"[rotate in place] {dtype}")
+    g = torch.Generator().manual_seed(5)
+    dt, lengths, dim, H, G = TYPES[dtype], [9, 30], 24, 3, 1
+    rows = normal(g, 39, (H + 2 * G) * dim + 3, dtype=dt)
+    f = torch.rand(12, generator=g)
+    seqs = mure.sequences(lengths)
+    wide = rows.cuda()
+    q, k = wide[:, 1:1 + H * dim], wide[:, 1 + H * dim:1 + (H + G) * dim]
+    fresh = seqs.rotate(q, k, f.cuda(), head_dim=dim, norm="rms")
+    same = seqs.rotate(q, k, f.cuda(), head_dim=dim, norm="rms", q_out=q, k_out=k)
+    assert same[0].data_ptr() == q.data_ptr()
+    assert torch.equal(wide[:, 1:1 + H * dim], fresh[0]) and torch.equal(wide[:, 1 + H * dim:1 + (H + G) * dim], fresh[1])
+    assert torch.equal(wide[:, 0].cpu(), rows[:, 0]) and torch.equal(wide[:, 1 + (H + G) * dim:].cpu(), rows[:, 1 + (H + G) * dim:])
+    R.close(fresh[0][None], R.rotate(rows[None, :, 1:1 + H * dim], f[None], lengths, dim, "rms"), "q")
+
+
+# ---------------------------------------------------------------- attention
+
+def qkv(seed, lengths, H, G, dim, dtype, M=1, own=True):
+    g = torch.Generator().manual_seed(seed)
+    T = sum(lengths)
+    return normal(g, M, T, H * dim, dtype=dtype), normal(g, M if own else 1, T, G * dim, dtype=dtype), normal(g, M if own else 1, T, G * dim, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,H,G,causal,window,M,own", [
+    (128, 4, 2, True, None, 1, True), (64, 6, 2, False, None, 2, True), (32, 3, 3, True, 7, 1, True), (80, 4, 1, True, None, 2, False),
+    (1, 2, 1, True, None, 1, True), (7, 5, 5, False, 3, 1, True), (17, 2, 2, True, 1, 1, True), (96, 3, 1, False, 40, 1, True),
+    (100, 8, 8, True, None, 1, True), (192, 2, 1, True, None, 1, True), (256, 4, 2, False, None, 1, True), (200, 1, 1, True, 20, 1, True),
+    (33, 9, 1, True, None, 1, True), (64, 40, 1, True, None, 1, True)])
+def test_attend(mure, dtype, dim, H, G, causal, window, M, own):
+    say(f"[attend] {dtype} dim={dim} H={H} G={G} causal={causal} window={window} M={M}")
+    q, k, v = qkv(dim + H, RAGGED, H, G, dim, TYPES[dtype], M, own)
+    out = mure.sequences(RAGGED).attend(*cuda(q, k, v), head_dim=dim, causal=causal, window=window)
+    R.close(out, R.attend(q, k, v, RAGGED, dim, causal=causal, window=window)[0], "out")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths", [[1], [2], [15, 16, 17], [31, 32, 33], [63, 64, 65], [127, 128, 129], [255, 257], [513]])
+def test_attend_lengths(mure, dtype, lengths):
+    say(f"[attend lengths] {dtype} {lengths}")
+    q, k, v = qkv(lengths[0], lengths, 2, 1, 48, TYPES[dtype])
+    for causal in (True, False):
+        out = mure.sequences(lengths).attend(*cuda(q, k, v), head_dim=48, causal=causal)
+        R.close(out, R.attend(q, k, v, lengths, 48, causal=causal)[0], f"causal={causal}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 3.0, 40.0])
+def test_attend_scales(mure, dtype, scale):
+    """Equal weights, the largest products counting least, and weights that leave one key."""
+    say(f"[attend scale] {dtype} {scale}")
+    lengths = [3, 70, 150]
+    q, k, v = qkv(7, lengths, 2, 2, 32, TYPES[dtype])
+    out = mure.sequences(lengths).attend(*cuda(q, k, v), head_dim=32, scale=scale)
+    R.close(out, R.attend(q, k, v, lengths, 32, scale=scale)[0], "out")
+
+
+def held(seed, n, capacity, width, dtype, M=1):
+    g = torch.Generator().manual_seed(seed)
+    return tuple(normal(g, M, n, capacity, width, dtype=dtype) for _ in range(2))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,H,G,lengths,past,capacity,causal,window,M", [
+    (128, 8, 2, [1, 1, 1, 1], [0, 31, 600, 1199], 1200, True, None, 1),
+    (64, 4, 4, [1, 1], [511, 512], 600, True, None, 2),
+    (32, 6, 2, [3, 16, 0, 17, 40], [700, 0, 5, 1100, 60], 1300, True, None, 1),
+    (80, 2, 1, [5, 20], [33, 1030], 1100, False, None, 1),
+    (48, 4, 1, [1, 9, 30], [1500, 1400, 1300], 1600, True, 100, 1),
+    (256, 2, 1, [1, 18], [530, 1025], 1100, True, None, 1),
+    (17, 3, 1, [2, 40, 1], [520, 30, 0], 700, False, 64, 1),
+    (64, 2, 1, [130, 600], [200, 1000], 2048, True, None, 1),
+    (8, 64, 1, [16, 1], [900, 40], 1000, True, None, 1)])
+def test_attend_over_a_cache(mure, dtype, dim, H, G, lengths, past, capacity, causal, window, M):
+    say(f"[attend cache] {dtype} dim={dim} H={H} G={G} {lengths} {past}")
+    q, k, v = qkv(dim, lengths, H, G, dim, TYPES[dtype], M)
+    cache, p = held(1, len(lengths), capacity, G * dim, TYPES[dtype], M), torch.tensor(past, dtype=torch.int32)
+    expected, after = R.attend(q, k, v, lengths, dim, causal=causal, window=window, cache=cache, past=p)
+    mine = cuda(*cache)
+    out = mure.sequences(lengths).attend(*cuda(q, k, v), head_dim=dim, causal=causal, window=window, cache=mine, past=p.cuda())
+    R.close(out, expected, "out")
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(mine, after)), "caches"
+
+
+# ---------------------------------------------------------------- gated feed-forward layer
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,inner,outer,act,bias,M,shared_x,shared_w", [
+    (1, 64, 64, "silu", False, 1, True, True), (130, 200, 72, "gelu", True, 1, True, True), (65, 33, 129, "sigmoid", True, 3, True, False),
+    (7, 1, 1, None, True, 2, False, True), (300, 257, 3, "relu", False, 2, False, False), (40, 129, 65, "gelu_tanh", True, 2, False, True),
+    (16, 1003, 50, "silu", False, 1, True, True), (17, 512, 200, "silu", True, 4, True, False), (128, 96, 64, "silu", False, 3, False, True)])
+def test_gated(mure, dtype, rows, inner, outer, act, bias, M, shared_x, shared_w):
+    say(f"[gated] {dtype} {rows} x {inner} -> {outer} {act} M={M}")
+    g = torch.Generator().manual_seed(rows + inner)
+    dt = TYPES[dtype]
+    x = normal(g, 1 if shared_x else M, rows, inner, dtype=dt)
+    gate, up = (normal(g, 1 if shared_w else M, outer, inner, dtype=dt, std=inner ** -0.5) for _ in range(2))
+    gb, ub = (normal(g, 1 if shared_w else M, outer), normal(g, 1, outer)) if bias else (None, None)
+    out = mure.gated(*cuda(x, gate, up), gate_bias=cuda(gb)[0], up_bias=cuda(ub)[0], activation=act)
+    R.close(out, R.gated(x, gate, up, gb, ub, act), "out")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gated_rows_do_not_depend_on_others(mure, dtype):
+    """Any number of rows, any place among them, and any strides: the same bits."""
+    say(f"[gated rows] {dtype}")
+    g = torch.Generator().manual_seed(9)
+    dt, K, N = TYPES[dtype], 320, 200
+    x, gate, up = cuda(normal(g, 700, K, dtype=dt), normal(g, N, K, dtype=dt, std=0.1), normal(g, N, K, dtype=dt, std=0.1))
+    whole = mure.gated(x, gate, up)
+    for first, n in ((0, 1), (5, 3), (17, 16), (100, 33), (650, 50), (3, 130), (40, 600)):
+        assert torch.equal(mure.gated(x[first:first + n], gate, up), whole[first:first + n]), (first, n)
+    odd = torch.zeros(700, K + 1, dtype=dt, device="cuda")
+    odd[:, 1:] = x
+    assert torch.equal(mure.gated(odd[:, 1:], gate, up), whole)
+    assert torch.equal(mure.gated(x.expand(3, -1, -1).contiguous(), gate, up), whole.expand(3, -1, -1))

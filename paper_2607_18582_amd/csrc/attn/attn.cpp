@@ -96,8 +96,9 @@ Span cache_span(const char* name, const mure_attn_cache& c, int64_t es, int64_t 
   return s;
 }
 
+// Whether rows at these strides (the first between rows) are aligned pieces of 16 bytes, 64 rows within 2^31 bytes.
 bool pieces(const void* p, int64_t es, std::initializer_list<int64_t> strides) {
-  bool ok = reinterpret_cast<uintptr_t>(p) % 16 == 0;
+  bool ok = reinterpret_cast<uintptr_t>(p) % 16 == 0 && *strides.begin() * es < 1 << 24;
   for (int64_t v : strides) ok = ok && v * es % 16 == 0;
   return ok;
 }

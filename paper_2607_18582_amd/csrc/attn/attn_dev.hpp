@@ -66,6 +66,9 @@ template <typename T> struct Rows {
   __device__ __forceinline__ const T* at(int j) const { return j < past ? held + j * held_stride : own + (int64_t)(j - past) * own_stride; }
 };
 
+// A number that is the same in all lanes, for the scalar unit (a division leaves it in the vector unit's registers).
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Waits for the wave's own copies to LDS.
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -84,27 +87,67 @@ template <typename T> __device__ __forceinline__ v4u load_piece(const T* p, int 
   return u.v;
 }
 
-// Copies KT keys' rows from key t0 on into a tile, zeros from key `end` on and behind n elements: 1024 bytes a wave
-// and step.  FAST: rows are whole aligned pieces and go to LDS directly (wait_copies).
-template <typename T, int DB, int KT, bool VALUES, bool FAST>
-__device__ __forceinline__ void fetch(char* tile, const Rows<T>& rows, int t0, int end, int n, int first, int step, int lane) {
+// Copies of KT keys' rows into a tile by W waves, 1024 bytes a wave and step.
+template <typename T, int DB, int KT, int W, bool VALUES> struct Copy {
   using H = Head<T, DB>;
-  constexpr int COPIES = KT * H::ROW / 1024;
+  static constexpr int COPIES = KT * H::ROW / 1024, STEPS = (COPIES + W - 1) / W;
+  static_assert(COPIES % W == 0 || COPIES < W, "");
+
+  // The place of the lane's piece of copy q: its key in the tile, its first element there.
+  static __device__ __forceinline__ void place(int q, int lane, int& key, int& e) {
+    const int byte = q * 1024 + lane * 16;
+    key = byte / H::ROW;
+    e = (byte % H::ROW / 16 ^ (VALUES ? v_twist<T, H::PIECES>(key) : k_twist<H::PIECES>(key))) * (16 / (int)sizeof(T));
+  }
+
+  // Rows of n elements from key t0 on, zeros from key `end` on and behind the row, element by element where need be.
+  static __device__ __forceinline__ void slowly(char* tile, const Rows<T>& rows, int t0, int end, int n, int wave, int lane) {
 #pragma unroll
-  for (int s = 0; s < COPIES; ++s) {
-    const int q = first + s * step;
-    if (q >= COPIES) break;
-    const int byte = q * 1024 + lane * 16, key = byte / H::ROW, slot = byte % H::ROW / 16;
-    const int piece = slot ^ (VALUES ? v_twist<T, H::PIECES>(key) : k_twist<H::PIECES>(key)), e = piece * (16 / (int)sizeof(T));
-    const bool in = t0 + key < end && e < n;
-    if constexpr (FAST) {
-      const void* p = in ? static_cast<const void*>(rows.at(t0 + key) + e) : ZEROS;
-      __builtin_amdgcn_global_load_lds(p, (lds_void*)(tile + q * 1024), 16, 0, 0);
-    } else {
-      *reinterpret_cast<v4u*>(tile + byte) = in ? load_piece<T>(rows.at(t0 + key), e, n) : v4u{0, 0, 0, 0};
+    for (int s = 0; s < STEPS; ++s) {
+      const int q = wave + s * W;
+      if (COPIES % W && q >= COPIES) break;
+      int key, e;
+      place(q, lane, key, e);
+      *reinterpret_cast<v4u*>(tile + q * 1024 + lane * 16) = t0 + key < end && e < n ? load_piece<T>(rows.at(t0 + key), e, n) : v4u{0, 0, 0, 0};
     }
   }
-}
+
+  // Keys from ... to - 1 of the tile whose key 0 is (or would be) at p, straight to LDS (wait_copies) through a buffer that
+  // ends with key to - 1: what lies behind it, or behind a row, reads as zeros.  A tile's rows lie within 2^31 bytes.
+  static __device__ __forceinline__ void straight(char* tile, const T* p, int64_t stride, int from, int to, int n, int wave, int lane) {
+    constexpr int KEYS = 1024 / H::ROW, PERIOD = !VALUES ? 16 : sizeof(T) == 4 ? 8 : 4;       // keys of a copy; of the twists
+    const int pitch = (int)(stride * (int)sizeof(T)), bytes = (to - 1) * pitch + n * (int)sizeof(T);
+    if constexpr (W * KEYS % PERIOD) asm("" : "+v"(lane));     // places stay out of registers between tiles
+    int key, e;
+    place(wave, lane, key, e);
+    unsigned off = (unsigned)(key * pitch) + (e < n ? (unsigned)(e * (int)sizeof(T)) : 0x80000000u);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int q = wave + s * W;
+      if (COPIES % W && q >= COPIES) break;
+      // the step's own place is in the buffer's base, so that the lanes' offsets are the same in every step
+      const int first = s * W * KEYS * pitch;
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(p)) + first, 0, max(0, bytes - first), 0x00027000);
+      if (s && W * KEYS % PERIOD) {
+        int k;
+        place(q, lane, k, e);
+        off = (unsigned)(key * pitch) + (e < n ? (unsigned)(e * (int)sizeof(T)) : 0x80000000u);
+      }
+      if (from <= 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + q * 1024), 16, (int)off, 0, 0, 0);
+      else if (key + s * W * KEYS >= from) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + q * 1024), 16, (int)off, 0, 0, 0);
+    }
+  }
+
+  template <bool FAST> static __device__ __forceinline__ void run(char* tile, const Rows<T>& rows, int t0, int end, int n, int wave, int lane) {
+    if constexpr (FAST) {
+      const int held = min(rows.past - t0, KT);                // keys of the tile that the cache holds: the others come from the call's own rows
+      if (held > 0) straight(tile, rows.held + (int64_t)t0 * rows.held_stride, rows.held_stride, 0, held, n, wave, lane);
+      if (held < KT) straight(tile, rows.own + (int64_t)(t0 - rows.past) * rows.own_stride, rows.own_stride, held, min(end - t0, KT), n, wave, lane);
+    } else {
+      slowly(tile, rows, t0, end, n, wave, lane);
+    }
+  }
+};
 
 // A row of queries times the scale's sign, as the second operand of S^T: pieces 2 s + (lane / 32) of it.  Scores are
 // then scaled by a positive number, which keeps their order and hides a key by -inf.
@@ -137,80 +180,81 @@ template <typename T> __device__ __forceinline__ v16f mma_piece(v4u a, v4u b, v1
   }
 }
 
-// S^T of 32 keys of a tile from key k0 on
-template <typename T, int DB> __device__ __forceinline__ v16f scores(const char* tile, int k0, int lane, const Query<T, DB>& q) {
+// A lane's places in a tile, from which all of its reads are constant steps or bits away.
+template <typename T, int DB> struct Reader {
   using H = Head<T, DB>;
-  const int key = k0 + (lane & 31), twist = k_twist<H::PIECES>(key);
-  const char* row = tile + key * H::ROW;
-  v16f s = {};
-#pragma unroll
-  for (int i = 0; i < H::STEPS; ++i) s = mma_piece<T>(*reinterpret_cast<const v4u*>(row + ((2 * i + (lane >> 5)) ^ twist) * 16), q[i], s);
-  return s;
-}
-
-// The first operand of O^T: channels 32 db + l % 32 of the values of instruction `step` of 32 keys from k0 on.
-template <typename T, int DB> __device__ __forceinline__ typename Mma<T>::frag values(const char* tile, int k0, int step, int db, int lane) {
-  using H = Head<T, DB>;
-  const int half = lane >> 5;
-  if constexpr (sizeof(T) == 2) {
-    // each read transposes 4 keys x 16 channels among 16 lanes
-    v4s r[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int key = k0 + 16 * step + 8 * i + 4 * half + (lane & 15) / 4, c = 32 * db + (lane & 16) + (lane & 3) * 4;
-      const char* p = tile + key * H::ROW + (((c >> 3) ^ v_twist<T, H::PIECES>(key)) << 4) + (c & 4) * 2;
-      r[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+  int k, v;
+  __device__ __forceinline__ explicit Reader(int lane) {
+    const int half = lane >> 5, key = lane & 31;
+    k = key * H::ROW + ((half ^ k_twist<H::PIECES>(key)) << 4);
+    if constexpr (sizeof(T) == 2) {
+      const int vk = 4 * half + (lane & 15) / 4, c = (lane & 16) + (lane & 3) * 4;
+      v = vk * H::ROW + (((c >> 3) ^ v_twist<T, H::PIECES>(vk)) << 4) + (c & 4) * 2;
+    } else {
+      const int vk = 4 * half, c = lane & 31;
+      v = vk * H::ROW + (((c >> 2) ^ v_twist<T, H::PIECES>(vk)) << 4) + (c & 3) * 4;
     }
-    return __builtin_bit_cast(v8bf, __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3, 4, 5, 6, 7));
-  } else {
-    const int key = k0 + 8 * (step / 4) + 4 * half + step % 4, c = 32 * db + (lane & 31);
-    return *reinterpret_cast<const float*>(tile + key * H::ROW + (((c >> 2) ^ v_twist<T, H::PIECES>(key)) << 4) + (c & 3) * 4);
   }
-}
 
-// Bits that say whether some of a fragment's values are infinite or NaN (add them up by |, ask with nonfinite).
-template <typename T> __device__ __forceinline__ uint32_t test_values(typename Mma<T>::frag f) {
-  if constexpr (sizeof(T) == 4) {
-    return (__float_as_uint(f) & 0x7f800000u) + 0x00800000u;    // exponents of ones carry into the sign's place
-  } else {
-    const v4u w = __builtin_bit_cast(v4u, f);
-    uint32_t t = 0;
+  // S^T of 32 keys of a tile from key k0 (a multiple of 32) on: twists have a period of at most 32 keys
+  __device__ __forceinline__ v16f scores(const char* tile, int k0, const Query<T, DB>& q) const {
+    // some pieces ahead of their products, and the next ones beside them
+    constexpr int G = H::STEPS % 4 == 0 ? 4 : H::STEPS % 3 == 0 ? 3 : 2;
+    const auto piece = [&](int i) { return *reinterpret_cast<const v4u*>(tile + (k ^ (i << 5)) + k0 * H::ROW); };
+    v16f s = {};
+    v4u a[2][G];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t |= (w[i] & 0x7f807f80u) + 0x00800080u;
-    return t;
+    for (int i = 0; i < G; ++i) a[0][i] = piece(i);
+#pragma unroll
+    for (int g = 0; g < H::STEPS; g += G) {
+      if (g + G < H::STEPS)
+#pragma unroll
+        for (int i = 0; i < G; ++i) a[g / G + 1 & 1][i] = piece(g + G + i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < G; ++i) s = mma_piece<T>(a[g / G & 1][i], q[g + i], s);
+    }
+    return s;
   }
-}
-template <typename T> __device__ __forceinline__ bool nonfinite(uint32_t t) { return __any((t & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)) != 0); }
 
-// A fragment with zeros in the place of what is not finite.
-template <typename T> __device__ __forceinline__ typename Mma<T>::frag finite_only(typename Mma<T>::frag f) {
-  if constexpr (sizeof(T) == 4) {
-    return (__float_as_uint(f) & 0x7f800000u) == 0x7f800000u ? 0.f : f;
-  } else {
-    v4u w = __builtin_bit_cast(v4u, f);
+  // The first operand of O^T: channels 32 db + l % 32 of the values of instruction `step` of 32 keys from k0 on.
+  __device__ __forceinline__ typename Mma<T>::frag values(const char* tile, int k0, int step, int db) const {
+    if constexpr (sizeof(T) == 2) {
+      // each read transposes 4 keys x 16 channels among 16 lanes
+      v4s r[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        r[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(tile + (v ^ (db << 6)) + (k0 + 16 * step + 8 * i) * H::ROW));
+      return __builtin_bit_cast(v8bf, __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      return *reinterpret_cast<const float*>(tile + (v ^ (db << 7)) + (k0 + 8 * (step / 4) + step % 4) * H::ROW);
+    }
+  }
+};
+
+// Puts zeros in the place of what is infinite or NaN in keys from ... to - 1 of a tile, and says whether there was any.
+// A hidden key's weight is 0, which must not meet it; the rows that see the key get it by add_nonfinite.
+template <typename T, int DB> __device__ __forceinline__ bool clean(char* tile, int from, int to, int tid, int threads) {
+  // exponents of ones carry into the sign's place
+  constexpr uint32_t ONES = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u, CARRY = sizeof(T) == 4 ? 0x00800000u : 0x00800080u;
+  constexpr uint32_t SIGN = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+  bool found = false;
+#pragma unroll 1
+  for (int byte = from * Head<T, DB>::ROW + tid * 16; byte < to * Head<T, DB>::ROW; byte += threads * 16) {
+    v4u w = *reinterpret_cast<const v4u*>(tile + byte);
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) any |= (w[i] & ONES) + CARRY;
+    if (!(any & SIGN)) continue;
+    found = true;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t x = w[i];
-      w[i] = ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u) | ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu);
+      const uint32_t t = ((w[i] & ONES) + CARRY) & SIGN;
+      w[i] &= sizeof(T) == 4 ? (t ? 0u : ~0u) : (t & 0x80000000u ? 0u : 0xffff0000u) | (t & 0x8000u ? 0u : 0xffffu);
     }
-    return __builtin_bit_cast(v8bf, w);
+    *reinterpret_cast<v4u*>(tile + byte) = w;
   }
-}
-
-// Adds the values of channels 32 db ... that are not finite to the sums of the rows that see their keys.
-template <typename T, int DB>
-__device__ __forceinline__ v16f add_nonfinite(const char* tile, int keys, int db, int lo, int hi, int half, v16f acc) {
-  using H = Head<T, DB>;
-#pragma unroll 1
-  for (int key = max(0, lo); key < min(keys, hi); ++key) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int c = 32 * db + 8 * (i / 4) + 4 * half + i % 4, at = c * (int)sizeof(T);
-      const float v = to_f<T>(*reinterpret_cast<const T*>(tile + key * H::ROW + (((at >> 4) ^ v_twist<T, H::PIECES>(key)) << 4) + (at & 15)));
-      acc[i] += fabsf(v) < __builtin_inff() ? 0.f : v;
-    }
-  }
-  return acc;
+  return found;
 }
 
 // The running softmax of a wave's rows: exponents of 2, the largest so far and the sum of the lane's half of the keys.
@@ -227,13 +271,12 @@ template <int DB> struct Running {
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
-// Takes KB times 32 keys of a tile into a wave's sums.  Rows see keys lo ... hi - 1, counted from the tile's first.
-// MASKED: some key is hidden from some row.  c: the scores' factor, log2(e) included.
-template <typename T, int DB, int KB, bool MASKED>
-__device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const char* vtile, int lo, int hi, float c, int lane) {
+// Takes KB times 32 keys of a tile into a wave's sums.  c: the scores' factor, log2(e) included.  hidden: some key is
+// hidden from some row, rows see keys lo ... hi - 1, counted from the tile's first.
+template <typename T, int DB, int KB>
+__device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const Reader<T, DB>& read, const char* vtile, bool hidden, int lo, int hi, float c, int half) {
   constexpr float LOWEST = -__builtin_inff();
-  const int half = lane >> 5;
-  if constexpr (MASKED) {
+  if (hidden) {
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -248,10 +291,16 @@ __device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const char
 #pragma unroll
     for (int i = 0; i < 16; ++i) m = fmaxf(m, s[b][i]);
   m = fmaxf(m, other_half(m)) * c;
-  m = fmaxf(run.m, m);
-  const float base = m == LOWEST ? 0.f : m;    // nothing above -inf yet: every weight is 0
-  const float old = __builtin_amdgcn_exp2f(run.m - base);
-  run.m = m;
+  // The sums stay where they are until a weight would pass 2^8: then, row by row, the largest exponent becomes their base.
+  const bool grows = m > run.m + 8.f;
+  if (__any(grows)) {
+    const float old = grows ? __builtin_amdgcn_exp2f(run.m - m) : 1.f;
+    run.m = grows ? m : run.m;
+    run.l *= old;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) run.o[d] *= old;
+  }
+  const float base = run.m == LOWEST ? 0.f : run.m;            // nothing above -inf yet: every weight is 0
   float l = 0.f;
 #pragma unroll
   for (int b = 0; b < KB; ++b)
@@ -260,9 +309,7 @@ __device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const char
       s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -base));
       l += s[b][i];
     }
-  run.l = run.l * old + l;
-#pragma unroll
-  for (int d = 0; d < DB; ++d) run.o[d] *= old;
+  run.l += l;
   constexpr int N = Mma<T>::N, STEPS = 16 / N;
   typename Mma<T>::frag p[KB][STEPS];
 #pragma unroll
@@ -277,35 +324,25 @@ __device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const char
         p[b][st] = __builtin_bit_cast(v8bf, w);
       }
     }
+  // fragments of one product ahead of the last one's
+  constexpr int G = KB * STEPS < 4 ? KB * STEPS : 4, GROUPS = KB * STEPS / G;
+  typename Mma<T>::frag v[2][G];
+  const auto fill = [&](int g) {
 #pragma unroll
-  for (int d = 0; d < DB; ++d) {
-    if constexpr (!MASKED) {
+    for (int i = 0; i < G; ++i) {
+      const int x = g % GROUPS * G + i;
+      v[g & 1][i] = read.values(vtile, 32 * (x / STEPS), x % STEPS, g / GROUPS);
+    }
+  };
+  fill(0);
 #pragma unroll
-      for (int b = 0; b < KB; ++b)
+  for (int g = 0; g < DB * GROUPS; ++g) {
+    if (g + 1 < DB * GROUPS) fill(g + 1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) run.o[d] = Mma<T>::mma(values<T, DB>(vtile, 32 * b, st, d, lane), p[b][st], run.o[d]);
-    } else {
-      // A hidden key's weight is 0, which infinity or NaN must not meet: where a value is not finite, the finite ones
-      // are summed again without it, and it is added for the rows that see it.
-      v16f acc = {};
-      uint32_t test = 0;
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          const auto v = values<T, DB>(vtile, 32 * b, st, d, lane);
-          test |= test_values<T>(v);
-          acc = Mma<T>::mma(v, p[b][st], acc);
-        }
-      if (nonfinite<T>(test)) {
-        acc = v16f{};
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-          for (int st = 0; st < STEPS; ++st) acc = Mma<T>::mma(finite_only<T>(values<T, DB>(vtile, 32 * b, st, d, lane)), p[b][st], acc);
-        acc = add_nonfinite<T, DB>(vtile, 32 * KB, d, lo, hi, half, acc);
-      }
-      run.o[d] += acc;
+    for (int i = 0; i < G; ++i) {
+      const int x = g % GROUPS * G + i;
+      run.o[g / GROUPS] = Mma<T>::mma(v[g & 1][i], p[x / STEPS][x % STEPS], run.o[g / GROUPS]);
     }
   }
 }
@@ -334,6 +371,25 @@ template <typename T, int DB> __device__ __forceinline__ void store_row(T* p, in
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int i = 0; i < 16; i += 4) store4<T>(p, 32 * d + 2 * i + 4 * half, n, o[d][i] * f, o[d][i + 1] * f, o[d][i + 2] * f, o[d][i + 3] * f);
+}
+
+// Adds what clean has taken out of keys from ... to - 1 of the tile at key t0 to the rows that see it: those keys lo ... hi - 1.
+template <typename T, int DB>
+__device__ __forceinline__ void add_nonfinite(Running<DB>& run, const Rows<T>& rows, int t0, int from, int to, int n, int lo, int hi, int half) {
+#pragma unroll 1
+  for (int key = from; key < to; ++key) {
+    asm("" : "+v"(half));                      // nothing of this is kept in registers elsewhere
+    const T* p = rows.at(t0 + key);
+    const bool sees = key >= lo && key < hi;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int c = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+        const float v = to_f<T>(p[min(c, n - 1)]);
+        run.o[d][i] += sees && !(fabsf(v) < __builtin_inff()) ? v : 0.f;
+      }
+  }
 }
 
 // The range of keys that a token at position `pos` of a sequence of `total` sees.

@@ -16,7 +16,7 @@ template <typename T> struct Source {
   __device__ __forceinline__ Source(const AttnArgs& k_, const SeqItem& it, int m, int g) {
     const mure_attn_attend_args& a = k_.a;
     const bool held = a.k_cache.p;
-    past = held && a.past ? a.past[it.seq] : 0;
+    past = uniform(held && a.past ? a.past[it.seq] : 0);
     bad = held && (past < 0 || past > a.capacity - it.total);
     total = past + it.total;
     const int64_t row = it.row0 - it.pos0, c = (int64_t)g * a.head_dim;
@@ -54,6 +54,11 @@ template <typename T> struct Source {
   }
 };
 
+__device__ __forceinline__ SeqItem item_of(const AttnArgs& k, int i) {
+  const SeqItem it = seq_item(k.items, i);
+  return {uniform(it.seq), uniform(it.row0), uniform(it.len), uniform(it.pos0), uniform(it.total), it.slot};
+}
+
 // Head and mutant number i of n: neighbouring blocks go to the chip's eight dies in turn, so each die gets neighbouring
 // heads, which share keys and values in its L2.
 __device__ __forceinline__ int spread(int i, int n) { return n % 8 ? i : i % 8 * (n / 8) + i / 8; }
@@ -72,9 +77,9 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   constexpr int KT = R::KT, KB = KT / 32;
   extern __shared__ char lds[];
   const mure_attn_attend_args& a = k.a;
-  const int n = a.heads * a.n_mutants, hm = spread(blockIdx.x % n, n), m = hm / a.heads, h = hm % a.heads, group = a.heads / a.kv_heads, g = h / group;
-  const int at = blockIdx.x / n, part = at % k.parts, i = k.item0 + at / k.parts;
-  const SeqItem it = seq_item(k.items, i);
+  const int n = a.heads * a.n_mutants, at = uniform(blockIdx.x / n), hm = spread(blockIdx.x - at * n, n), m = uniform(hm / a.heads), h = hm - m * a.heads;
+  const int group = uniform(a.heads / a.kv_heads), g = uniform(h / group), part = uniform(at % k.parts), i = k.item0 + uniform(at / k.parts);
+  const SeqItem it = item_of(k, i);
   const Source<T> src(k, it, m, g);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5;
   T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * a.out.row_stride + (int64_t)h * a.head_dim;
@@ -86,9 +91,9 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   if (a.k_cache.p && part == 0 && h % group == 0) src.keep(a, it, m, tid, 256);
   // keys that any row of the block sees, in this part
   const int first = src.past + it.pos0, last = first + it.len - 1;
-  int from, to, none;
-  sees(a, first, src.total, from, none);
-  sees(a, last, src.total, none, to);
+  int from, to, block_lo, block_hi, none;      // ... and that all rows see
+  sees(a, first, src.total, from, block_hi);
+  sees(a, last, src.total, block_lo, to);
   if (k.parts > 1) {
     from = max(from, part * ATTN_KEYS_MID);
     to = (int)min((int64_t)to, (int64_t)(part + 1) * ATTN_KEYS_MID);
@@ -97,11 +102,10 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   const int row = wave * 32 + (lane & 31), pos = min(first + row, last);
   int lo, hi;
   sees(a, pos, src.total, lo, hi);
-  // ... that all rows of the wave see, and that any of them sees
-  const int wave_first = min(first + wave * 32, last), wave_last = min(first + wave * 32 + 31, last);
-  int all_lo, all_hi, any_lo, any_hi;
-  sees(a, wave_first, src.total, any_lo, all_hi);
-  sees(a, wave_last, src.total, all_lo, any_hi);
+  // ... that any row of the wave sees
+  int any_lo, any_hi;
+  sees(a, min(first + wave * 32, last), src.total, any_lo, none);
+  sees(a, min(first + wave * 32 + 31, last), src.total, none, any_hi);
   const bool idle = wave * 32 >= it.len;
   Query<T, DB> q;
   load_query<T, DB>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)(pos - first)) * a.q.row_stride + (int64_t)h * a.head_dim,
@@ -109,10 +113,11 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   const float c = factor(a.scale);
   Running<DB> run;
   run.start();
+  const Reader<T, DB> read(lane);
   auto load = [&](int t, int buffer) {
     char* tile = lds + buffer * 2 * R::TILE;
-    fetch<T, DB, KT, false, FAST>(tile, src.k, t, src.total, a.head_dim, wave, 4, lane);
-    fetch<T, DB, KT, true, FAST>(tile + R::TILE, src.v, t, src.total, a.head_dim, wave, 4, lane);
+    Copy<T, DB, KT, 4, false>::template run<FAST>(tile, src.k, t, src.total, a.head_dim, wave, lane);
+    Copy<T, DB, KT, 4, true>::template run<FAST>(tile + R::TILE, src.v, t, src.total, a.head_dim, wave, lane);
   };
   int t = from / KT * KT, buffer = 0;
   load(t, 0);
@@ -120,15 +125,25 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
     wait_copies();
     __syncthreads();                           // the tile is there, and the last one has been used
     if (t + KT < to) load(t + KT, buffer ^ 1);
+    char* tile = lds + buffer * 2 * R::TILE;
+    // Keys hidden from some row of the block are those before and behind what all of them see, of the part.
+    const int see_from = max(block_lo, from) - t, see_to = min(block_hi, to) - t, there = min(KT, src.total - t);
+    const bool hidden = see_from > 0 || see_to < KT, some = see_from > 0 || see_to < there;
+    bool apart = false;                        // a hidden one's value is not finite
+    if (some) {
+      const bool before = clean<T, DB>(tile + R::TILE, 0, min(see_from, there), tid, 256), behind = clean<T, DB>(tile + R::TILE, max(0, see_to), there, tid, 256);
+      apart = __syncthreads_or(before || behind);
+    }
     if (idle || t >= any_hi || t + KT <= any_lo) continue;
-    const char* tile = lds + buffer * 2 * R::TILE;
     v16f s[KB];
 #pragma unroll
-    for (int b = 0; b < KB; ++b) s[b] = scores<T, DB>(tile, 32 * b, lane, q);
-    // a tile that starts before the part's keys or ends behind them is cut to them
-    const int first_key = max(lo, from), end_key = min(hi, to);
-    if (t >= max(all_lo, from) && t + KT <= min(all_hi, to)) take<T, DB, KB, false>(run, s, tile + R::TILE, 0, 0, c, lane);
-    else take<T, DB, KB, true>(run, s, tile + R::TILE, first_key - t, end_key - t, c, lane);
+    for (int b = 0; b < KB; ++b) s[b] = read.scores(tile, 32 * b, q);
+    const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
+    take<T, DB, KB>(run, s, read, tile + R::TILE, hidden, row_lo, row_hi, c, half);
+    if (apart) {
+      add_nonfinite<T, DB>(run, src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, half);
+      add_nonfinite<T, DB>(run, src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, half);
+    }
   }
   if (row >= it.len) return;
   const float l = run.l + other_half(run.l);
@@ -158,9 +173,9 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   using S = Short<T, DB>;
   extern __shared__ char lds[];
   const mure_attn_attend_args& a = k.a;
-  const int n = a.kv_heads * a.n_mutants, gm = spread(blockIdx.x % n, n), m = gm / a.kv_heads, g = gm % a.kv_heads, group = a.heads / a.kv_heads;
-  const int at = blockIdx.x / n, unit = at % units, part = at / units % k.parts, i = k.item0 + at / units / k.parts;
-  const SeqItem it = seq_item(k.items, i);
+  const int n = a.kv_heads * a.n_mutants, at = uniform(blockIdx.x / n), gm = spread(blockIdx.x - at * n, n), m = uniform(gm / a.kv_heads), g = gm - m * a.kv_heads;
+  const int group = uniform(a.heads / a.kv_heads), ip = uniform(at / units), unit = at - ip * units, part = uniform(ip % k.parts), i = k.item0 + uniform(ip / k.parts);
+  const SeqItem it = item_of(k, i);
   if (unit * 32 >= it.len * group) return;
   const Source<T> src(k, it, m, g);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5;
@@ -176,10 +191,10 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
     return;
   }
   if (a.k_cache.p && part == 0 && unit == 0) src.keep(a, it, m, tid, 256);
-  int lo, hi, from, to, none;
+  int lo, hi, from, to, all_lo, all_hi;        // keys that the row sees, that any token sees, that all do
   sees(a, src.past + token, src.total, lo, hi);
-  sees(a, src.past, src.total, from, none);
-  sees(a, src.total - 1, src.total, none, to);
+  sees(a, src.past, src.total, from, all_hi);
+  sees(a, src.total - 1, src.total, all_lo, to);
   const int64_t part0 = (int64_t)part * ATTN_KEYS_SHORT;
   if (max((int64_t)from, part0) >= min((int64_t)to, part0 + ATTN_KEYS_SHORT)) return;
   from = (int)max((int64_t)from, part0 + wave * S::PER);
@@ -190,6 +205,7 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   const float c = factor(a.scale);
   Running<DB> run;
   run.start();
+  const Reader<T, DB> read(lane);
   char* tile = lds + wave * S::TILES * S::TILE;
   char* vtile = tile + (S::TILES - 1) * S::TILE;
   auto landed = [] {                           // the wave's own copies
@@ -199,17 +215,30 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   };
   for (int t = from / S::KT * S::KT; t < to; t += S::KT) {
     __builtin_amdgcn_wave_barrier();
-    fetch<T, DB, S::KT, false, FAST>(tile, src.k, t, src.total, a.head_dim, 0, 1, lane);
-    if constexpr (S::TILES == 2) fetch<T, DB, S::KT, true, FAST>(vtile, src.v, t, src.total, a.head_dim, 0, 1, lane);
+    Copy<T, DB, S::KT, 1, false>::template run<FAST>(tile, src.k, t, src.total, a.head_dim, 0, lane);
+    if constexpr (S::TILES == 2) Copy<T, DB, S::KT, 1, true>::template run<FAST>(vtile, src.v, t, src.total, a.head_dim, 0, lane);
     landed();
-    v16f s[1] = {scores<T, DB>(tile, 0, lane, q)};
+    v16f s[1] = {read.scores(tile, 0, q)};
     if constexpr (S::TILES == 1) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      fetch<T, DB, S::KT, true, FAST>(vtile, src.v, t, src.total, a.head_dim, 0, 1, lane);
+      Copy<T, DB, S::KT, 1, true>::template run<FAST>(vtile, src.v, t, src.total, a.head_dim, 0, lane);
       landed();
     }
-    take<T, DB, 1, true>(run, s, vtile, max(lo, from) - t, min(hi, to) - t, c, lane);
+    const int see_from = max(all_lo, from) - t, see_to = min(all_hi, to) - t, there = min(S::KT, src.total - t);
+    bool apart = false;
+    if (see_from > 0 || see_to < there) {
+      const bool before = clean<T, DB>(vtile, 0, min(see_from, there), lane, 64), behind = clean<T, DB>(vtile, max(0, see_to), there, lane, 64);
+      apart = __any(before || behind);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
+    take<T, DB, 1>(run, s, read, vtile, see_from > 0 || see_to < S::KT, row_lo, row_hi, c, half);
+    if (apart) {
+      add_nonfinite<T, DB>(run, src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, half);
+      add_nonfinite<T, DB>(run, src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, half);
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
   // the waves' sums, added in order

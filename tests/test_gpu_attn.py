@@ -170,6 +170,57 @@ def test_attend_over_a_cache(mure, dtype, dim, H, G, lengths, past, capacity, ca
     assert all(torch.equal(a.cpu(), b) for a, b in zip(mine, after)), "caches"
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,lengths,causal,window", [(64, [200, 7, 12], True, None), (128, [150, 5], True, 9), (80, [90, 16, 3], False, 4),
+                                                       (192, [70, 9], True, None), (17, [40, 11], True, 3)])
+def test_attend_infinities_reach_those_that_see_them(mure, dtype, dim, lengths, causal, window):
+    say(f"[attend inf] {dtype} dim={dim} {lengths} causal={causal} window={window}")
+    q, k, v = qkv(11, lengths, 2, 1, dim, TYPES[dtype])
+    inf, nan = float("inf"), float("nan")
+    for row, c, x in ((0, 0, inf), (3, 1, -inf), (6, 2, nan), (lengths[0] // 2, 3, inf), (lengths[0] // 2 + 1, 3, -inf), (lengths[0] - 1, 4, nan),
+                      (lengths[0] + 2, 5, inf), (lengths[0] + lengths[1] - 1, 6, nan)):
+        v[0, row, c] = x
+    k[0, lengths[0] - 2, 0], k[0, lengths[0] + 3, 1] = nan, nan              # rows that see these keys are NaN
+    q[0, 2, 3] = nan
+    out = mure.sequences(lengths).attend(*cuda(q, k, v), head_dim=dim, causal=causal, window=window)
+    R.close(out, R.attend(q, k, v, lengths, dim, causal=causal, window=window)[0], "out")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attend_infinities_in_a_cache(mure, dtype):
+    """Rows behind the past may hold anything; what the cache holds is seen by window and place."""
+    say(f"[attend cache inf] {dtype}")
+    dim, lengths, past, capacity = 64, [1, 6, 30, 1], [700, 40, 1100, 0], 1300
+    q, k, v = qkv(12, lengths, 2, 1, dim, TYPES[dtype])
+    cache = held(2, 4, capacity, dim, TYPES[dtype])
+    inf, nan = float("inf"), float("nan")
+    for i, p in enumerate(past):
+        for c in cache:
+            c[0, i, p:] = nan
+    cache[1][0, 0, 650, 3], cache[1][0, 0, 5, 4], cache[1][0, 1, 39, 2], cache[1][0, 2, 1050, 7] = inf, nan, -inf, nan
+    v[0, 4, 9], v[0, 20, 11] = nan, inf
+    p = torch.tensor(past, dtype=torch.int32)
+    for window in (None, 64):
+        mine = cuda(*cache)
+        out = mure.sequences(lengths).attend(*cuda(q, k, v), head_dim=dim, window=window, cache=mine, past=p.cuda())
+        R.close(out, R.attend(q, k, v, lengths, dim, window=window, cache=cache, past=p)[0], f"window={window}")
+
+
+def test_attend_past_that_does_not_fit(mure):
+    """Such sequences' results are NaN, their caches and the others' results as ever."""
+    say("[attend past]")
+    dim, lengths, past, capacity = 32, [2, 40, 3, 20, 0, 1, 5], [-1, 30, 10, 600, 5, 700, 695], 700
+    q, k, v = qkv(13, lengths, 2, 2, dim, torch.bfloat16)
+    cache, p = held(3, 7, capacity, 2 * dim, torch.bfloat16), torch.tensor(past, dtype=torch.int32)
+    p[3] = -(2 ** 31)
+    expected, after = R.attend(q, k, v, lengths, dim, cache=cache, past=p)
+    mine = cuda(*cache)
+    out = mure.sequences(lengths).attend(*cuda(q, k, v), head_dim=dim, cache=mine, past=p.cuda())
+    assert bool(torch.isnan(expected[0][0, :2]).all()) and bool(torch.isnan(expected[0][0, 45:65]).all()) and bool(torch.isnan(expected[0][0, 65]).all())
+    R.close(out, expected, "out")
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(mine, after))
+
+
 # ---------------------------------------------------------------- gated feed-forward layer
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

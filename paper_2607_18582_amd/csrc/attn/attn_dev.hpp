@@ -46,16 +46,24 @@ template <typename T, int DB> struct Head {
   static constexpr int STEPS = BYTES / 32;     // two 16-byte pieces of a row of keys, one per half wave
 };
 
+// What a tile holds, by the reads of it: keys in 16-byte pieces of 16 rows, values in 64 bytes of 4 rows (float32: 128
+// bytes of two) for 32x32 products, values in 32 bytes of 8 rows (float32: 64 of four) for 16x16 products.
+enum Reads { KEYS, VALUES32, VALUES16 };
+
 // The place of a row's 16-byte pieces in LDS is xored with a number of the row's, so that the rows that lanes read
-// together lie in different banks: 16-byte reads of one piece of 16 keys, 8-byte reads of 64 bytes of 4 values (of
-// 128 bytes of two, in float32).
-template <int PIECES> __device__ __forceinline__ int k_twist(int key) {
-  return PIECES >= 16 ? key & 15 : PIECES == 8 ? (key >> 1) & 7 : (key >> 2) & 3;
-}
-template <typename T, int PIECES> __device__ __forceinline__ int v_twist(int key) {
-  if (sizeof(T) == 4) return PIECES >= 16 ? ((key >> 2) & 1) << 3 : 0;
-  return PIECES >= 16 ? (key & 3) << 2 : PIECES == 8 ? ((key >> 1) & 1) << 2 : 0;
-}
+// together lie in different banks.  PERIOD: rows after which the numbers repeat.
+template <typename T, int PIECES, Reads R> struct Twist {
+  static constexpr int PERIOD = R == KEYS ? 16 : R == VALUES16 ? sizeof(T) == 4 ? 16 : 8 : sizeof(T) == 4 ? 8 : 4;
+  static __device__ __forceinline__ int of(int key) {
+    if (R == KEYS) return PIECES >= 16 ? key & 15 : PIECES == 8 ? (key >> 1) & 7 : (key >> 2) & 3;
+    if (R == VALUES32) {
+      if (sizeof(T) == 4) return PIECES >= 16 ? ((key >> 2) & 1) << 3 : 0;
+      return PIECES >= 16 ? (key & 3) << 2 : PIECES == 8 ? ((key >> 1) & 1) << 2 : 0;
+    }
+    if (sizeof(T) == 4) return PIECES >= 16 ? ((key >> 2) & 3) << 2 : ((key >> 2) & 1) << 2;
+    return PIECES >= 16 ? (key & 7) << 1 : PIECES == 8 ? ((key >> 1) & 3) << 1 : ((key >> 2) & 1) << 1;
+  }
+};
 
 // The rows of one sequence's keys (or values) of one head: its cache's first, then the call's own.
 template <typename T> struct Rows {
@@ -69,8 +77,8 @@ template <typename T> struct Rows {
 // A number that is the same in all lanes, for the scalar unit (a division leaves it in the vector unit's registers).
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// Waits for the wave's own copies to LDS.
-__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits for the wave's own copies to LDS but the last N.
+template <int N = 0> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // 16 bytes from p + first on of a row of n elements, zeros behind its end.
 template <typename T> __device__ __forceinline__ v4u load_piece(const T* p, int first, int n) {
@@ -88,8 +96,9 @@ template <typename T> __device__ __forceinline__ v4u load_piece(const T* p, int 
 }
 
 // Copies of KT keys' rows into a tile by W waves, 1024 bytes a wave and step.
-template <typename T, int DB, int KT, int W, bool VALUES> struct Copy {
+template <typename T, int DB, int KT, int W, Reads R> struct Copy {
   using H = Head<T, DB>;
+  using Tw = Twist<T, H::PIECES, R>;
   static constexpr int COPIES = KT * H::ROW / 1024, STEPS = (COPIES + W - 1) / W;
   static_assert(COPIES % W == 0 || COPIES < W, "");
 
@@ -97,7 +106,7 @@ template <typename T, int DB, int KT, int W, bool VALUES> struct Copy {
   static __device__ __forceinline__ void place(int q, int lane, int& key, int& e) {
     const int byte = q * 1024 + lane * 16;
     key = byte / H::ROW;
-    e = (byte % H::ROW / 16 ^ (VALUES ? v_twist<T, H::PIECES>(key) : k_twist<H::PIECES>(key))) * (16 / (int)sizeof(T));
+    e = (byte % H::ROW / 16 ^ Tw::of(key)) * (16 / (int)sizeof(T));
   }
 
   // Rows of n elements from key t0 on, zeros from key `end` on and behind the row, element by element where need be.
@@ -115,9 +124,9 @@ template <typename T, int DB, int KT, int W, bool VALUES> struct Copy {
   // Keys from ... to - 1 of the tile whose key 0 is (or would be) at p, straight to LDS (wait_copies) through a buffer that
   // ends with key to - 1: what lies behind it, or behind a row, reads as zeros.  A tile's rows lie within 2^31 bytes.
   static __device__ __forceinline__ void straight(char* tile, const T* p, int64_t stride, int from, int to, int n, int wave, int lane) {
-    constexpr int KEYS = 1024 / H::ROW, PERIOD = !VALUES ? 16 : sizeof(T) == 4 ? 8 : 4;       // keys of a copy; of the twists
+    constexpr int EACH = 1024 / H::ROW;        // keys of a copy
     const int pitch = (int)(stride * (int)sizeof(T)), bytes = (to - 1) * pitch + n * (int)sizeof(T);
-    if constexpr (W * KEYS % PERIOD) asm("" : "+v"(lane));     // places stay out of registers between tiles
+    if constexpr (W * EACH % Tw::PERIOD) asm("" : "+v"(lane));     // places stay out of registers between tiles
     int key, e;
     place(wave, lane, key, e);
     unsigned off = (unsigned)(key * pitch) + (e < n ? (unsigned)(e * (int)sizeof(T)) : 0x80000000u);
@@ -126,18 +135,19 @@ template <typename T, int DB, int KT, int W, bool VALUES> struct Copy {
       const int q = wave + s * W;
       if (COPIES % W && q >= COPIES) break;
       // the step's own place is in the buffer's base, so that the lanes' offsets are the same in every step
-      const int first = s * W * KEYS * pitch;
+      const int first = s * W * EACH * pitch;
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(p)) + first, 0, max(0, bytes - first), 0x00027000);
-      if (s && W * KEYS % PERIOD) {
+      if (s && W * EACH % Tw::PERIOD) {
         int k;
         place(q, lane, k, e);
         off = (unsigned)(key * pitch) + (e < n ? (unsigned)(e * (int)sizeof(T)) : 0x80000000u);
       }
       if (from <= 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + q * 1024), 16, (int)off, 0, 0, 0);
-      else if (key + s * W * KEYS >= from) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + q * 1024), 16, (int)off, 0, 0, 0);
+      else if (key + s * W * EACH >= from) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + q * 1024), 16, (int)off, 0, 0, 0);
     }
   }
 
+  // A tile at key t0; at least STEPS copies a wave.
   template <bool FAST> static __device__ __forceinline__ void run(char* tile, const Rows<T>& rows, int t0, int end, int n, int wave, int lane) {
     if constexpr (FAST) {
       const int held = min(rows.past - t0, KT);                // keys of the tile that the cache holds: the others come from the call's own rows
@@ -149,20 +159,20 @@ template <typename T, int DB, int KT, int W, bool VALUES> struct Copy {
   }
 };
 
-// A row of queries times the scale's sign, as the second operand of S^T: pieces 2 s + (lane / 32) of it.  Scores are
-// then scaled by a positive number, which keeps their order and hides a key by -inf.
+// A row of queries times the scale's sign, as the second operand of S^T: pieces W s + w of it.  Scores are then scaled by a
+// positive number, which keeps their order and hides a key by -inf.
 template <typename T, int DB> using Query = v4u[Head<T, DB>::STEPS];
-template <typename T, int DB> __device__ __forceinline__ void load_query(Query<T, DB>& q, const T* p, int n, int half, float scale) {
+template <typename T, int STEPS, int W> __device__ __forceinline__ void load_query(v4u* q, const T* p, int n, int w, float scale) {
 #pragma unroll
-  for (int s = 0; s < Head<T, DB>::STEPS; ++s) {
-    const int e = (2 * s + half) * (16 / (int)sizeof(T));
+  for (int s = 0; s < STEPS; ++s) {
+    const int e = (W * s + w) * (16 / (int)sizeof(T));
     q[s] = e < n ? load_piece<T>(p, e, n) : v4u{0, 0, 0, 0};
     if (scale < 0.f) q[s] ^= sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
     if (scale == 0.f) {                        // 0, or NaN of what is not finite
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t w = q[s][i], hi = (w & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u;
-        q[s][i] = sizeof(T) == 4 ? hi : hi | ((w & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u);
+        const uint32_t x = q[s][i], hi = (x & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u;
+        q[s][i] = sizeof(T) == 4 ? hi : hi | ((x & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u);
       }
     }
   }
@@ -186,13 +196,13 @@ template <typename T, int DB> struct Reader {
   int k, v;
   __device__ __forceinline__ explicit Reader(int lane) {
     const int half = lane >> 5, key = lane & 31;
-    k = key * H::ROW + ((half ^ k_twist<H::PIECES>(key)) << 4);
+    k = key * H::ROW + ((half ^ Twist<T, H::PIECES, KEYS>::of(key)) << 4);
     if constexpr (sizeof(T) == 2) {
       const int vk = 4 * half + (lane & 15) / 4, c = (lane & 16) + (lane & 3) * 4;
-      v = vk * H::ROW + (((c >> 3) ^ v_twist<T, H::PIECES>(vk)) << 4) + (c & 4) * 2;
+      v = vk * H::ROW + (((c >> 3) ^ Twist<T, H::PIECES, VALUES32>::of(vk)) << 4) + (c & 4) * 2;
     } else {
       const int vk = 4 * half, c = lane & 31;
-      v = vk * H::ROW + (((c >> 2) ^ v_twist<T, H::PIECES>(vk)) << 4) + (c & 3) * 4;
+      v = vk * H::ROW + (((c >> 2) ^ Twist<T, H::PIECES, VALUES32>::of(vk)) << 4) + (c & 3) * 4;
     }
   }
 
@@ -261,6 +271,7 @@ template <typename T, int DB> __device__ __forceinline__ bool clean(char* tile, 
 template <int DB> struct Running {
   v16f o[DB];
   float m, l;
+  static __device__ __forceinline__ int channel(int i, int lane) { return i / 16 * 32 + 8 * (i / 4 % 4) + 4 * (lane >> 5) + i % 4; }
   __device__ __forceinline__ void start() {
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[i] = v16f{};
@@ -347,6 +358,16 @@ __device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const Read
   }
 }
 
+// 64 bytes of the summed axis of 16 x 16 results: a lane's piece is a quarter of them.
+template <typename T> __device__ __forceinline__ v4f mma16(v4u a, v4u b, v4f c) {
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+  else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+    return c;
+  }
+}
+
 // Four neighbouring channels c ... of n
 template <typename T> __device__ __forceinline__ void store4(T* p, int c, int n, float a, float b, float d, float e) {
   const float v[4] = {a, b, d, e};
@@ -374,21 +395,19 @@ template <typename T, int DB> __device__ __forceinline__ void store_row(T* p, in
 }
 
 // Adds what clean has taken out of keys from ... to - 1 of the tile at key t0 to the rows that see it: those keys lo ... hi - 1.
-template <typename T, int DB>
-__device__ __forceinline__ void add_nonfinite(Running<DB>& run, const Rows<T>& rows, int t0, int from, int to, int n, int lo, int hi, int half) {
+// N registers of sums a lane, of channels channel(i).
+template <int N, typename T, typename F, typename S>
+__device__ __forceinline__ void add_nonfinite(const Rows<T>& rows, int t0, int from, int to, int n, int lo, int hi, int lane, F&& channel, S&& add) {
 #pragma unroll 1
   for (int key = from; key < to; ++key) {
-    asm("" : "+v"(half));                      // nothing of this is kept in registers elsewhere
+    asm("" : "+v"(lane));                      // nothing of this is kept in registers elsewhere
     const T* p = rows.at(t0 + key);
     const bool sees = key >= lo && key < hi;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int c = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
-        const float v = to_f<T>(p[min(c, n - 1)]);
-        run.o[d][i] += sees && !(fabsf(v) < __builtin_inff()) ? v : 0.f;
-      }
+    for (int i = 0; i < N; ++i) {
+      const float v = to_f<T>(p[min(channel(i, lane), n - 1)]);
+      add(i, sees && !(fabsf(v) < __builtin_inff()) ? v : 0.f);
+    }
   }
 }
 

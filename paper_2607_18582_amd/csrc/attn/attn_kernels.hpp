@@ -54,6 +54,9 @@ template <typename T> struct Source {
   }
 };
 
+// A wave's own reads and writes of LDS before this are done.
+__device__ __forceinline__ void settle() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 __device__ __forceinline__ SeqItem item_of(const AttnArgs& k, int i) {
   const SeqItem it = seq_item(k.items, i);
   return {uniform(it.seq), uniform(it.row0), uniform(it.len), uniform(it.pos0), uniform(it.total), it.slot};
@@ -108,7 +111,7 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   sees(a, min(first + wave * 32 + 31, last), src.total, none, any_hi);
   const bool idle = wave * 32 >= it.len;
   Query<T, DB> q;
-  load_query<T, DB>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)(pos - first)) * a.q.row_stride + (int64_t)h * a.head_dim,
+  load_query<T, Head<T, DB>::STEPS, 2>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)(pos - first)) * a.q.row_stride + (int64_t)h * a.head_dim,
                     a.head_dim, half, a.scale);
   const float c = factor(a.scale);
   Running<DB> run;
@@ -116,8 +119,8 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   const Reader<T, DB> read(lane);
   auto load = [&](int t, int buffer) {
     char* tile = lds + buffer * 2 * R::TILE;
-    Copy<T, DB, KT, 4, false>::template run<FAST>(tile, src.k, t, src.total, a.head_dim, wave, lane);
-    Copy<T, DB, KT, 4, true>::template run<FAST>(tile + R::TILE, src.v, t, src.total, a.head_dim, wave, lane);
+    Copy<T, DB, KT, 4, KEYS>::template run<FAST>(tile, src.k, t, src.total, a.head_dim, wave, lane);
+    Copy<T, DB, KT, 4, VALUES32>::template run<FAST>(tile + R::TILE, src.v, t, src.total, a.head_dim, wave, lane);
   };
   int t = from / KT * KT, buffer = 0;
   load(t, 0);
@@ -141,8 +144,9 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
     const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
     take<T, DB, KB>(run, s, read, tile + R::TILE, hidden, row_lo, row_hi, c, half);
     if (apart) {
-      add_nonfinite<T, DB>(run, src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, half);
-      add_nonfinite<T, DB>(run, src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, half);
+      auto add = [&](int i, float v) { run.o[i / 16][i % 16] += v; };
+      add_nonfinite<16 * DB>(src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
+      add_nonfinite<16 * DB>(src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
     }
   }
   if (row >= it.len) return;
@@ -156,36 +160,41 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   }
 }
 
-// ---- short sequences: 32 rows (token, head of a group) a block, the keys spread over its waves
+// ---- short sequences: 16 rows (token, head of a group) a block, the keys spread over its waves
+//
+// As above in 16x16 products: a lane has row l % 16 of the queries and of every 16 keys those numbered 4 (l / 16) + i.
+// Bound by the cache's bytes, so what counts is how many are on their way: small tiles of each wave's own, keys straight
+// into registers, and four blocks a compute unit.
 
 template <typename T, int DB> struct Short {
   using H = Head<T, DB>;
-  static constexpr int KT = 32;
-  static constexpr int TILE = KT * H::ROW;
-  static constexpr int WAVES = 4;
+  static constexpr int KT = 32, WAVES = 4;
   static constexpr int PER = ATTN_KEYS_SHORT / WAVES;          // keys of a wave
-  static constexpr int TILES = 2 * WAVES * TILE <= 160 << 10 ? 2 : 1;    // of a wave: keys and values in one another's place where both do not fit
-  static constexpr int SUMS = 32 * 32 * DB * 4;
-  static constexpr int LDS = TILES * WAVES * TILE > SUMS + 1024 ? TILES * WAVES * TILE : SUMS + 1024;
+  static constexpr int PITCH = 32 * DB + 4;                    // floats of a row of sums
+  static constexpr int EACH = KT * H::ROW > 16 * PITCH * 4 ? KT * H::ROW : 16 * PITCH * 4;
+  static constexpr int LDS = WAVES * EACH + WAVES * 16 * 2 * 4;
 };
 
-template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <= 4 ? 2 : 1) void short_kernel(AttnArgs k, int units) {
+template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB * sizeof(T) <= 8 ? 4 : DB * sizeof(T) <= 24 ? 2 : 1) void short_kernel(AttnArgs k, int units) {
   using S = Short<T, DB>;
+  using H = Head<T, DB>;
+  constexpr int STEPS = H::BYTES / 64, E = 16 / (int)sizeof(T);
+  constexpr float LOWEST = -__builtin_inff();
   extern __shared__ char lds[];
   const mure_attn_attend_args& a = k.a;
   const int n = a.kv_heads * a.n_mutants, at = uniform(blockIdx.x / n), gm = spread(blockIdx.x - at * n, n), m = uniform(gm / a.kv_heads), g = gm - m * a.kv_heads;
   const int group = uniform(a.heads / a.kv_heads), ip = uniform(at / units), unit = at - ip * units, part = uniform(ip % k.parts), i = k.item0 + uniform(ip / k.parts);
   const SeqItem it = item_of(k, i);
-  if (unit * 32 >= it.len * group) return;
+  if (unit * 16 >= it.len * group) return;
   const Source<T> src(k, it, m, g);
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, half = lane >> 5;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, quarter = lane >> 4;
   // row r of the unit: token r / group, head g group + r % group
-  const int rows = min(32, it.len * group - unit * 32), r = min(unit * 32 + (lane & 31), it.len * group - 1), token = r / group, h = g * group + r % group;
+  const int rows = min(16, it.len * group - unit * 16), r = min(unit * 16 + (lane & 15), it.len * group - 1), token = r / group, h = g * group + r % group;
   T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * a.out.row_stride;
   if (src.bad) {
     if (part == 0)
       for (int x = tid; x < rows * a.head_dim; x += 256) {
-        const int y = unit * 32 + x / a.head_dim;
+        const int y = unit * 16 + x / a.head_dim;
         out[y / group * a.out.row_stride + (int64_t)(g * group + y % group) * a.head_dim + x % a.head_dim] = from_f<T>(__builtin_nanf(""));
       }
     return;
@@ -199,126 +208,177 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   if (max((int64_t)from, part0) >= min((int64_t)to, part0 + ATTN_KEYS_SHORT)) return;
   from = (int)max((int64_t)from, part0 + wave * S::PER);
   to = (int)min((int64_t)to, part0 + (wave + 1) * S::PER);
-  Query<T, DB> q;
-  load_query<T, DB>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)token) * a.q.row_stride + (int64_t)h * a.head_dim, a.head_dim,
-                    half, a.scale);
-  const float c = factor(a.scale);
-  Running<DB> run;
-  run.start();
-  const Reader<T, DB> read(lane);
-  char* tile = lds + wave * S::TILES * S::TILE;
-  char* vtile = tile + (S::TILES - 1) * S::TILE;
-  auto landed = [] {                           // the wave's own copies
-    wait_copies();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  };
-  for (int t = from / S::KT * S::KT; t < to; t += S::KT) {
-    __builtin_amdgcn_wave_barrier();
-    Copy<T, DB, S::KT, 1, false>::template run<FAST>(tile, src.k, t, src.total, a.head_dim, 0, lane);
-    if constexpr (S::TILES == 2) Copy<T, DB, S::KT, 1, true>::template run<FAST>(vtile, src.v, t, src.total, a.head_dim, 0, lane);
-    landed();
-    v16f s[1] = {read.scores(tile, 0, q)};
-    if constexpr (S::TILES == 1) {
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      Copy<T, DB, S::KT, 1, true>::template run<FAST>(vtile, src.v, t, src.total, a.head_dim, 0, lane);
-      landed();
+  v4f o[2 * DB];
+#pragma unroll
+  for (int d = 0; d < 2 * DB; ++d) o[d] = v4f{};
+  float top = LOWEST, l = 0.f;
+  char* tile = lds + wave * S::EACH;
+  if (from < to) {
+    v4u q[STEPS];
+    load_query<T, STEPS, 4>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)token) * a.q.row_stride + (int64_t)h * a.head_dim, a.head_dim,
+                            quarter, a.scale);
+    const float c = factor(a.scale);
+    for (int t = from / S::KT * S::KT; t < to; t += S::KT) {
+      // keys 16 b + l % 16; those behind the sequence's are hidden
+      v4u keys[2][STEPS];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const T* p = src.k.at(min(t + 16 * b + (lane & 15), src.total - 1));
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          const int e = (4 * s + quarter) * E;
+          if constexpr (FAST) keys[b][s] = e < a.head_dim ? *reinterpret_cast<const v4u*>(p + e) : v4u{0, 0, 0, 0};
+          else keys[b][s] = e < a.head_dim ? load_piece<T>(p, e, a.head_dim) : v4u{0, 0, 0, 0};
+        }
+      }
+      Copy<T, DB, S::KT, 1, VALUES16>::template run<FAST>(tile, src.v, t, src.total, a.head_dim, 0, lane);
+      v4f s[2] = {};
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int x = 0; x < STEPS; ++x) s[b] = mma16<T>(keys[b][x], q[x], s[b]);
+      const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
+      float most = LOWEST;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int key = 16 * b + 4 * quarter + x;
+          s[b][x] = key >= row_lo && key < row_hi ? s[b][x] : LOWEST;
+          most = fmaxf(most, s[b][x]);
+        }
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32)) * c;
+      const bool grows = most > top + 8.f;
+      if (__any(grows)) {
+        const float old = grows ? __builtin_amdgcn_exp2f(top - most) : 1.f;
+        top = grows ? most : top;
+        l *= old;
+#pragma unroll
+        for (int d = 0; d < 2 * DB; ++d) o[d] *= old;
+      }
+      const float base = top == LOWEST ? 0.f : top;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          s[b][x] = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, -base));
+          l += s[b][x];
+        }
+      wait_copies();
+      settle();
+      const int see_from = max(all_lo, from) - t, see_to = min(all_hi, to) - t, there = min(S::KT, src.total - t);
+      bool apart = false;
+      if (see_from > 0 || see_to < there) {
+        const bool before = clean<T, DB>(tile, 0, min(see_from, there), lane, 64), behind = clean<T, DB>(tile, max(0, see_to), there, lane, 64);
+        apart = __any(before || behind);
+        settle();
+      }
+      if constexpr (sizeof(T) == 2) {
+        v4u w;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) w[x] = f2bf2(s[x / 2][2 * (x & 1)], s[x / 2][2 * (x & 1) + 1]);
+        const v8bf p = __builtin_bit_cast(v8bf, w);
+        const int key = 4 * quarter + (lane & 15) / 4, twist = Twist<T, H::PIECES, VALUES16>::of(key);       // and key + 16
+        const int v = key * H::ROW + ((((lane & 3) >> 1) ^ twist) << 4) + (lane & 1) * 8;
+#pragma unroll
+        for (int d = 0; d < 2 * DB; ++d) {
+          v4s x[2];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) x[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(tile + (v ^ (d << 5)) + 16 * b * H::ROW));
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7)), p, o[d], 0, 0, 0);
+        }
+      } else {
+        const int key = 4 * quarter, twist = Twist<T, H::PIECES, VALUES16>::of(key), v = key * H::ROW + ((((lane & 15) >> 2) ^ twist) << 4) + (lane & 3) * 4;
+#pragma unroll
+        for (int d = 0; d < 2 * DB; ++d)
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float*>(tile + (v ^ (d << 6)) + (16 * (x / 4) + x % 4) * H::ROW), s[x / 4][x % 4], o[d], 0, 0, 0);
+      }
+      if (apart) {
+        auto channel = [](int x, int lane) { return x / 4 * 16 + (lane >> 4) * 4 + x % 4; };
+        auto add = [&](int x, float v) { o[x / 4][x % 4] += v; };
+        add_nonfinite<8 * DB>(src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, lane, channel, add);
+        add_nonfinite<8 * DB>(src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, lane, channel, add);
+      }
+      settle();
     }
-    const int see_from = max(all_lo, from) - t, see_to = min(all_hi, to) - t, there = min(S::KT, src.total - t);
-    bool apart = false;
-    if (see_from > 0 || see_to < there) {
-      const bool before = clean<T, DB>(vtile, 0, min(see_from, there), lane, 64), behind = clean<T, DB>(vtile, max(0, see_to), there, lane, 64);
-      apart = __any(before || behind);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    }
-    const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
-    take<T, DB, 1>(run, s, read, vtile, see_from > 0 || see_to < S::KT, row_lo, row_hi, c, half);
-    if (apart) {
-      add_nonfinite<T, DB>(run, src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, half);
-      add_nonfinite<T, DB>(run, src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, half);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
   // the waves' sums, added in order
-  __syncthreads();
-  float* sums = reinterpret_cast<float*>(lds);
-  float* ml = reinterpret_cast<float*>(lds + S::SUMS);         // [4][32][2]
-  const float l = run.l + other_half(run.l);
-  if (!half) ml[(wave * 32 + lane) * 2] = run.m, ml[(wave * 32 + lane) * 2 + 1] = l;
-  __syncthreads();
-  float m_all = ml[(lane & 31) * 2];
-  for (int w = 1; w < S::WAVES; ++w) m_all = fmaxf(m_all, ml[(w * 32 + (lane & 31)) * 2]);
-  const float base = m_all == -__builtin_inff() ? 0.f : m_all;
-  float l_all = 0.f;
-  for (int w = 0; w < S::WAVES; ++w) l_all += ml[(w * 32 + (lane & 31)) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * 32 + (lane & 31)) * 2] - base);
-  const float f = __builtin_amdgcn_exp2f(run.m - base);
-  for (int w = 0; w < S::WAVES; ++w) {
-    if (w == wave && from < to)
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  float* sums = reinterpret_cast<float*>(tile);
+  float* ml = reinterpret_cast<float*>(lds + S::WAVES * S::EACH);              // [4][16][2]
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          float* p = sums + (32 * d + 8 * (x / 4) + 4 * half + x % 4) * 32 + (lane & 31);
-          *p = (w ? *p : 0.f) + run.o[d][x] * f;
-        }
-    else if (w == 0 && wave == 0)
-      for (int x = lane; x < 1024 * DB; x += 64) sums[x] = 0.f;
-    __syncthreads();
-  }
-  if (wave == 0 && !half) ml[lane * 2] = m_all, ml[lane * 2 + 1] = l_all;
+  for (int d = 0; d < 2 * DB; ++d) *reinterpret_cast<v4f*>(sums + (lane & 15) * S::PITCH + 16 * d + 4 * quarter) = o[d];
+  if (!quarter) ml[(wave * 16 + lane) * 2] = top, ml[(wave * 16 + lane) * 2 + 1] = l;
   __syncthreads();
   for (int x = tid; x < rows * a.head_dim; x += 256) {
-    const int y = x / a.head_dim, e = x % a.head_dim, all = unit * 32 + y, tk = all / group, hd = g * group + all % group;
-    const float v = sums[e * 32 + y];
+    const int y = x / a.head_dim, e = x - y * a.head_dim, all = unit * 16 + y, tk = all / group, hd = g * group + all % group;
+    float most = LOWEST;
+#pragma unroll
+    for (int w = 0; w < S::WAVES; ++w) most = fmaxf(most, ml[(w * 16 + y) * 2]);
+    const float base = most == LOWEST ? 0.f : most;
+    float v = 0.f, size = 0.f;
+#pragma unroll
+    for (int w = 0; w < S::WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + y) * 2] - base);
+      size = fmaf(ml[(w * 16 + y) * 2 + 1], f, size);
+      v = fmaf(reinterpret_cast<const float*>(lds + w * S::EACH)[y * S::PITCH + e], f, v);
+    }
     if (k.parts > 1) {
       const int64_t slot = ((((int64_t)m * k.n_items + i) * k.rows_each + tk) * a.heads + hd) * k.parts + part;
       k.ws_o[slot * a.head_dim + e] = v;
-      if (e < 2) k.ws_ml[2 * slot + e] = ml[2 * y + e];
-      if (e == 0 && a.head_dim == 1) k.ws_ml[2 * slot + 1] = ml[2 * y + 1];
+      if (e == 0) k.ws_ml[2 * slot] = most, k.ws_ml[2 * slot + 1] = size;
     } else {
-      out[tk * a.out.row_stride + (int64_t)hd * a.head_dim + e] = from_f<T>(v * (1.f / ml[2 * y + 1]));
+      out[tk * a.out.row_stride + (int64_t)hd * a.head_dim + e] = from_f<T>(v * (1.f / size));
     }
   }
 }
 
-// ---- the parts' results of one token and head, added in order
+// ---- the parts' results of one token and head: every 16th part in order, then the 16 sums in order
 
-template <typename T> __global__ __launch_bounds__(256) void join_kernel(AttnArgs k, int keys, int64_t total_rows) {
+template <typename T> __global__ __launch_bounds__(1024) void join_kernel(AttnArgs k, int keys) {
+  __shared__ float sums[16][MURE_ATTN_MAX_HEAD], sizes[16];
   const mure_attn_attend_args& a = k.a;
-  const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (x >= total_rows) return;
-  const int h = x % a.heads, row = x / a.heads % k.rows_each;
-  const int64_t im = x / a.heads / k.rows_each;
-  const int i = im % k.n_items, m = im / k.n_items;
-  const SeqItem it = seq_item(k.items, i);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int rows = a.heads * k.rows_each, im = uniform(blockIdx.x / rows), x = blockIdx.x - im * rows, row = uniform(x / a.heads), h = x - row * a.heads;
+  const int m = uniform(im / k.n_items), i = im - m * k.n_items;
+  const SeqItem it = item_of(k, i);
   if (row >= it.len) return;
-  const int past = a.past ? a.past[it.seq] : 0;
+  const int past = uniform(a.past ? a.past[it.seq] : 0);
   if (past < 0 || past > a.capacity - it.total) return;        // NaN already
-  int lo, hi, none, block_lo, block_hi;
+  int lo, hi;
   sees(a, past + it.pos0 + row, past + it.total, lo, hi);
-  // parts that the kernel worked on: those with keys of any of the item's rows
-  sees(a, past + it.pos0, past + it.total, block_lo, none);
-  sees(a, past + it.pos0 + it.len - 1, past + it.total, none, block_hi);
-  const int p0 = lo / keys, p1 = (hi - 1) / keys;
-  const int64_t slot = x * k.parts;
-  float mx = -__builtin_inff();
-  for (int p = p0; p <= p1; ++p) mx = fmaxf(mx, k.ws_ml[2 * (slot + p)]);
-  const float base = mx == -__builtin_inff() ? 0.f : mx;
-  float l = 0.f, o[4] = {};
-  for (int p = p0; p <= p1; ++p) {
-    const float f = __builtin_amdgcn_exp2f(k.ws_ml[2 * (slot + p)] - base);
-    l += k.ws_ml[2 * (slot + p) + 1] * f;
+  const int first = lo / keys, last = (hi - 1) / keys;         // the parts with keys that the row sees
+  const float* ml = k.ws_ml + 2 * (int64_t)blockIdx.x * k.parts;
+  const float* o = k.ws_o + (int64_t)blockIdx.x * k.parts * a.head_dim;
+  float top = -__builtin_inff();
+  for (int p = first + lane; p <= last; p += 64) top = fmaxf(top, ml[2 * p]);
+  for (int w = 1; w < 64; w *= 2) top = fmaxf(top, __shfl_xor(top, w));
+  const float base = top == -__builtin_inff() ? 0.f : top;
+  for (int slot = wave; slot < 16; slot += waves) {
+    float l = 0.f, v[4] = {};
+#pragma unroll 4
+    for (int p = first + slot; p <= last; p += 16) {
+      const float f = __builtin_amdgcn_exp2f(ml[2 * p] - base);
+      l = fmaf(ml[2 * p + 1], f, l);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (lane + 64 * j < a.head_dim) o[j] += k.ws_o[(slot + p) * a.head_dim + lane + 64 * j] * f;
+      for (int j = 0; j < 4; ++j)
+        if (lane + 64 * j < a.head_dim) v[j] = fmaf(o[(int64_t)p * a.head_dim + lane + 64 * j], f, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[slot][lane + 64 * j] = v[j];
+    if (lane == 0) sizes[slot] = l;
   }
+  __syncthreads();
+  const int c = threadIdx.x;
+  if (c >= a.head_dim) return;
+  float l = 0.f, v = 0.f;
+  for (int s = 0; s < 16; ++s) l += sizes[s], v += sums[s][c];
   T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (it.row0 + (int64_t)row) * a.out.row_stride + (int64_t)h * a.head_dim;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (lane + 64 * j < a.head_dim) out[lane + 64 * j] = from_f<T>(o[j] * (1.f / l));
+  out[c] = from_f<T>(v * (1.f / l));
 }
 
 // ---- launches
@@ -347,7 +407,7 @@ template <typename... P, typename... A> hipError_t launch_lds(void (*kernel)(P..
 }
 
 template <typename T, int DB, bool FAST> hipError_t short_f(AttnArgs k, hipStream_t s) {
-  const int units = (k.rows_each * (k.a.heads / k.a.kv_heads) + 31) / 32;
+  const int units = (k.rows_each * (k.a.heads / k.a.kv_heads) + 15) / 16;
   return over_items(k, (int64_t)k.a.kv_heads * k.a.n_mutants * units * k.parts,
                     [&](unsigned grid) { return launch_lds(short_kernel<T, DB, FAST>, grid, Short<T, DB>::LDS, s, k, units); });
 }
@@ -372,10 +432,12 @@ template <typename T> hipError_t with_head(const AttnArgs& k, bool brief, hipStr
   return with_speed<T, 8>(k, brief, s);
 }
 
-template <typename T> hipError_t join(const AttnArgs& k, int keys, hipStream_t s) {
-  const int64_t rows = (int64_t)k.a.n_mutants * k.n_items * k.rows_each * k.a.heads, blocks = (rows + 3) / 4;
-  if (blocks > BLOCKS) return hipErrorInvalidConfiguration;
-  return launch(join_kernel<T>, dim3((unsigned)blocks), 256, s, k, keys, rows);
+template <typename T> hipError_t join(AttnArgs k, int keys, hipStream_t s) {
+  const int64_t rows = (int64_t)k.rows_each * k.a.heads, blocks = (int64_t)k.a.n_mutants * k.n_items * rows;
+  // few rows get a wave for every 16th part; otherwise the waves take several each
+  const unsigned threads = blocks < 512 && k.parts > 16 ? 1024 : 256;
+  if (blocks > ((int64_t)1 << 32) / threads - 1) return hipErrorInvalidConfiguration;
+  return launch(join_kernel<T>, dim3((unsigned)blocks), threads, s, k, keys);
 }
 
 }  // namespace mure

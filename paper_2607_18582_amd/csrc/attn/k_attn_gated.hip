@@ -26,16 +26,6 @@ __device__ __forceinline__ float activated(float v, int act) {
   return v;
 }
 
-// 64 bytes of the summed axis: a lane's piece is a quarter of them.
-template <typename T> __device__ __forceinline__ v4f mma16(v4u a, v4u b, v4f c) {
-  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
-  else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
-    return c;
-  }
-}
-
 __device__ __forceinline__ int twist(int row) { return (row >> 1) & 7; }
 
 // WM x WN waves

@@ -76,6 +76,10 @@ template <typename T> struct Rows {
 
 // A number that is the same in all lanes, for the scalar unit (a division leaves it in the vector unit's registers).
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <typename T> __device__ __forceinline__ T* uniform(T* p) {
+  const uint64_t v = (uint64_t)p;
+  return (T*)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
 
 // Waits for the wave's own copies to LDS but the last N.
 template <int N = 0> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
@@ -125,7 +129,9 @@ template <typename T, int DB, int KT, int W, Reads R> struct Copy {
   // ends with key to - 1: what lies behind it, or behind a row, reads as zeros.  A tile's rows lie within 2^31 bytes.
   static __device__ __forceinline__ void straight(char* tile, const T* p, int64_t stride, int from, int to, int n, int wave, int lane) {
     constexpr int EACH = 1024 / H::ROW;        // keys of a copy
-    const int pitch = (int)(stride * (int)sizeof(T)), bytes = (to - 1) * pitch + n * (int)sizeof(T);
+    // scalars, every one of them: a buffer's description in vector registers costs a loop around each copy
+    const int pitch = uniform((int)(stride * (int)sizeof(T))), bytes = uniform((to - 1) * pitch + n * (int)sizeof(T));
+    char* const base = uniform(const_cast<char*>(reinterpret_cast<const char*>(p)));
     if constexpr (W * EACH % Tw::PERIOD) asm("" : "+v"(lane));     // places stay out of registers between tiles
     int key, e;
     place(wave, lane, key, e);
@@ -136,7 +142,7 @@ template <typename T, int DB, int KT, int W, Reads R> struct Copy {
       if (COPIES % W && q >= COPIES) break;
       // the step's own place is in the buffer's base, so that the lanes' offsets are the same in every step
       const int first = s * W * EACH * pitch;
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(p)) + first, 0, max(0, bytes - first), 0x00027000);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(base + first, 0, max(0, bytes - first), 0x00027000);
       if (s && W * EACH % Tw::PERIOD) {
         int k;
         place(q, lane, k, e);

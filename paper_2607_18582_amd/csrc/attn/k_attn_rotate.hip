@@ -34,6 +34,10 @@ template <typename T, int V> struct Raw {
   typedef T raw __attribute__((ext_vector_type(V)));
   typedef raw __attribute__((aligned(sizeof(T)))) any;
 };
+template <typename T> struct Raw<T, 1> {
+  typedef T raw;
+  typedef T any;
+};
 
 template <typename T, int V> __device__ __forceinline__ void get(const T* p, float (&v)[V]) {
   if constexpr (V == 1) v[0] = to_f<T>(*p);
@@ -50,16 +54,22 @@ template <typename T, int V> __device__ __forceinline__ void put(T* p, const flo
     typename Raw<T, V>::raw r;
 #pragma unroll
     for (int j = 0; j < V; ++j) r[j] = from_f<T>(v[j]);
-    *reinterpret_cast<typename Raw<T, V>::any*>(p) = r;
+    __builtin_nontemporal_store(r, reinterpret_cast<typename Raw<T, V>::any*>(p));
   }
 }
 
+template <typename T, int V> __device__ __forceinline__ T element(const typename Raw<T, V>::raw& r, int j) {
+  if constexpr (V == 1) return r;
+  else return r[j];
+}
+
 // V pairs a unit, U units a lane.
-template <typename T, int V, int U>
+template <typename T, int V, int U, bool INTERLEAVED>
 __global__ __launch_bounds__(THREADS) void rotate_kernel(AttnRotateArgs k, int team) {
   extern __shared__ float2 turn[];             // [tokens][pairs]
   const mure_attn_rotate_args& a = k.a;
   const int m = blockIdx.x % a.n_mutants, item = k.item0 + blockIdx.x / a.n_mutants, tid = threadIdx.x;
+  const int begin = gridDim.y == 1 ? 0 : blockIdx.y, end = gridDim.y == 1 ? 2 : begin + 1;    // of queries and keys
   const SeqItem it = seq_item(k.items, item);
   const int pairs = a.rotated / 2, D = a.head_dim;
   const float* freq = a.frequencies.p + m * a.frequencies.mutant_stride;
@@ -68,109 +78,115 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(AttnRotateArgs k, int t
     const int t = x / pairs, i = x % pairs;
     double position = (double)(at + t);
     if (a.positions) {
-      int axis = 0, end = a.section[0];
-      while (i >= end && axis + 1 < a.axes) end += a.section[++axis];
+      int axis = 0, behind = a.section[0];
+      while (i >= behind && axis + 1 < a.axes) behind += a.section[++axis];
       position = a.positions[axis * k.tokens + it.row0 + t];
     }
     turn[x] = cos_sin(position * (double)freq[i]);
   }
   __syncthreads();
-  const int heads = a.q_heads + a.k_heads, lane = tid & (team - 1), units = (D + 2 * V - 1) / (2 * V), turning = pairs / V;
-  for (int x = tid / team; x < it.len * heads; x += THREADS / team) {
-    const int t = x / heads, h = x % heads;
-    const bool key = h >= a.q_heads;
-    const mure_seq_in& src = key ? a.k : a.q;
-    const mure_seq_out& dst = key ? a.k_out : a.q_out;
-    const int64_t row = it.row0 + t, col = (int64_t)(key ? h - a.q_heads : h) * D;
-    const T* p = static_cast<const T*>(src.p) + m * src.mutant_stride + row * src.row_stride + col;
-    T* o = static_cast<T*>(dst.p) + m * dst.mutant_stride + row * dst.row_stride + col;
-    const mure_seq_param& wp = key ? a.k_weight : a.q_weight;
-    float v[U][2][V];
-    int e[U][2];
-    float sum = 0.f;
+  // a team's lanes have the same channels of every head: their weights stay in registers, and the next head's
+  // channels are on their way while this one's are worked on
+  const int lane = tid & (team - 1), units = (D + 2 * V - 1) / (2 * V), turning = pairs / V, teams = THREADS / team;
+  int e[U][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int unit = lane + u * team;
-      const bool turns = unit < turning;
-      e[u][0] = a.interleaved || !turns ? unit * 2 * V : unit * V;     // channels behind the pairs are 2 V a unit too
-      e[u][1] = a.interleaved || !turns ? e[u][0] + V : pairs + unit * V;
+  for (int u = 0; u < U; ++u) {
+    const int unit = lane + u * team;
+    const bool apart = !INTERLEAVED && unit < turning;                 // channels behind the pairs are 2 V a unit too
+    e[u][0] = apart ? unit * V : unit * 2 * V;
+    e[u][1] = apart ? pairs + unit * V : e[u][0] + V;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      if (unit >= units || e[u][s] >= D) e[u][s] = -1;
+  }
+#pragma unroll 1
+  for (int which = begin; which < end; ++which) {
+    const int heads = which ? a.k_heads : a.q_heads, count = it.len * heads;
+    const mure_seq_in& src = which ? a.k : a.q;
+    const mure_seq_out& dst = which ? a.k_out : a.q_out;
+    const mure_seq_param& wp = which ? a.k_weight : a.q_weight;
+    const T* in = static_cast<const T*>(src.p) + m * src.mutant_stride + it.row0 * src.row_stride;
+    T* out = static_cast<T*>(dst.p) + m * dst.mutant_stride + it.row0 * dst.row_stride;
+    float w[U][2][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        if (unit < units && e[u][s] < D) get<T, V>(p + e[u][s], v[u][s]);
-        else {
 #pragma unroll
-          for (int j = 0; j < V; ++j) v[u][s][j] = 0.f;
-          e[u][s] = -1;
-        }
+        for (int j = 0; j < V; ++j) w[u][s][j] = 1.f;
+        if (wp.p && e[u][s] >= 0) get<float, V>(wp.p + m * wp.mutant_stride + e[u][s], w[u][s]);
+      }
+    typename Raw<T, V>::raw next[U][2];
+    const auto fetch = [&](int x) {
+      const int t = x / heads, h = x - t * heads;
+      const T* p = in + t * src.row_stride + (int64_t)h * D;
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum += v[u][s][j];
-      }
-    }
-    if (a.norm) {
-      float mean = 0.f;
-      if (a.norm == MURE_SEQ_LAYER) {
-        for (int w = 1; w < team; w *= 2) sum += __shfl_xor(sum, w);
-        mean = sum / (float)D;
-      }
-      float sq = 0.f;
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (e[u][s] >= 0) next[u][s] = *reinterpret_cast<const typename Raw<T, V>::any*>(p + e[u][s]);
+    };
+    int x = tid / team;
+    if (x < count) fetch(x);
+    for (; x < count; x += teams) {
+      const int t = x / heads, h = x - t * heads;
+      float v[U][2][V], sum = 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            if (e[u][s] >= 0) v[u][s][j] -= mean;
-            sq = fmaf(v[u][s][j], v[u][s][j], sq);
+            v[u][s][j] = e[u][s] >= 0 ? to_f<T>(element<T, V>(next[u][s], j)) : 0.f;
+            sum += v[u][s][j];
           }
-      for (int w = 1; w < team; w *= 2) sq += __shfl_xor(sq, w);
-      const float f = 1.f / sqrtf(sq / (float)D + a.eps);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          float w[V];
-#pragma unroll
-          for (int j = 0; j < V; ++j) w[j] = 1.f;
-          if (wp.p && e[u][s] >= 0) get<float, V>(wp.p + m * wp.mutant_stride + e[u][s], w);
-#pragma unroll
-          for (int j = 0; j < V; ++j) v[u][s][j] = v[u][s][j] * f * w[j];
+      if (x + teams < count) fetch(x + teams);
+      if (a.norm) {
+        float mean = 0.f;
+        if (a.norm == MURE_SEQ_LAYER) {
+          for (int d = 1; d < team; d *= 2) sum += __shfl_xor(sum, d);
+          mean = sum / (float)D;
         }
-    }
+        float sq = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int unit = lane + u * team;
-      if (unit < turning) {
-        const float2* cs = turn + t * pairs + unit * V;
-        if (a.interleaved) {
-          if constexpr (V > 1) {
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {      // pair j: channels 2 j, 2 j + 1 of the unit's 2 V
-              float& x0 = v[u][2 * j / V][2 * j % V];
-              float& x1 = v[u][2 * j / V][2 * j % V + 1];
-              const float2 f = cs[j];
-              const float y = x0 * f.x - x1 * f.y;
-              x1 = x0 * f.y + x1 * f.x;
-              x0 = y;
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+              if (e[u][s] >= 0) v[u][s][j] -= mean;
+              sq = fmaf(v[u][s][j], v[u][s][j], sq);
             }
-          } else {
-            const float2 f = cs[0];
-            const float y = v[u][0][0] * f.x - v[u][1][0] * f.y;
-            v[u][1][0] = v[u][0][0] * f.y + v[u][1][0] * f.x;
-            v[u][0][0] = y;
-          }
-        } else {
+        for (int d = 1; d < team; d *= 2) sq += __shfl_xor(sq, d);
+        const float f = 1.f / sqrtf(sq / (float)D + a.eps);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[u][s][j] *= f * w[u][s][j];
+      }
+      T* o = out + t * dst.row_stride + (int64_t)h * D;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int unit = lane + u * team;
+        if (unit < turning) {
+          const float2* cs = turn + t * pairs + unit * V;
 #pragma unroll
           for (int j = 0; j < V; ++j) {
+            // interleaved: channels 2 j, 2 j + 1 of the unit's 2 V
             const float2 f = cs[j];
-            const float y = v[u][0][j] * f.x - v[u][1][j] * f.y;
-            v[u][1][j] = v[u][0][j] * f.y + v[u][1][j] * f.x;
-            v[u][0][j] = y;
+            float& x0 = INTERLEAVED && V > 1 ? v[u][2 * j / V][2 * j % V] : v[u][0][j];
+            float& x1 = INTERLEAVED && V > 1 ? v[u][2 * j / V][(2 * j + 1) % V] : v[u][1][j];
+            const float y = x0 * f.x - x1 * f.y;
+            x1 = x0 * f.y + x1 * f.x;
+            x0 = y;
           }
         }
-      }
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        if (e[u][s] >= 0) put<T, V>(o + e[u][s], v[u][s]);
+        for (int s = 0; s < 2; ++s)
+          if (e[u][s] >= 0) put<T, V>(o + e[u][s], v[u][s]);
+      }
     }
   }
 }
@@ -178,10 +194,12 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(AttnRotateArgs k, int t
 template <typename T, int V, int U> hipError_t rotate_u(AttnRotateArgs k, int team, hipStream_t s) {
   const int n = k.n_items, M = k.a.n_mutants, most = std::min(n, (int)(((1 << 24) - 1) / M));
   const unsigned lds = (unsigned)(k.longest * (k.a.rotated / 2) * sizeof(float2));
+  // where blocks are few, queries and keys get their own: 64 sequences of one token take 4.6 us so and 6.0 one after the other
+  const unsigned y = k.a.k_heads && (int64_t)n * M < 1024 ? 2 : 1;
   for (k.item0 = 0; k.item0 < n; k.item0 += most) {
     std::tuple<AttnRotateArgs, int> params(k, team);
     void* at[] = {&std::get<0>(params), &std::get<1>(params)};
-    if (const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(rotate_kernel<T, V, U>), dim3((unsigned)(std::min(most, n - k.item0) * M)), dim3(THREADS), at, lds, s);
+    if (const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(k.a.interleaved ? rotate_kernel<T, V, U, true> : rotate_kernel<T, V, U, false>), dim3((unsigned)(std::min(most, n - k.item0) * M), y), dim3(THREADS), at, lds, s);
         e != hipSuccess)
       return e;
   }

@@ -88,15 +88,14 @@ template <int N = 0> __device__ __forceinline__ void wait_copies() { asm volatil
 template <typename T> __device__ __forceinline__ v4u load_piece(const T* p, int first, int n) {
   constexpr int E = 16 / sizeof(T);
   if (first + E <= n) return *reinterpret_cast<const v4u_any*>(p + first);
-  union {
-    v4u v;
-    T e[E];
-  } u;
-  u.v = v4u{0, 0, 0, 0};
+  v4u v = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < E; ++i)
-    if (first + i < n) u.e[i] = p[first + i];
-  return u.v;
+    if (first + i < n) {
+      if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(p[first + i]);
+      else v[i / 2] |= (uint32_t)p[first + i] << (i & 1 ? 16 : 0);
+    }
+  return v;
 }
 
 // Copies of KT keys' rows into a tile by W waves, 1024 bytes a wave and step.
@@ -364,14 +363,15 @@ __device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const Read
   }
 }
 
-// 64 bytes of the summed axis of 16 x 16 results: a lane's piece is a quarter of them.
-template <typename T> __device__ __forceinline__ v4f mma16(v4u a, v4u b, v4f c) {
+// 64 bytes of the summed axis of 16 x 16 results, a lane's piece being a quarter of them: one instruction, or in float32 four.
+template <typename T> __device__ __forceinline__ v4f mma16_part(v4u a, v4u b, int e, v4f c) {
   if constexpr (sizeof(T) == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
-  else {
+  else return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+}
+template <typename T> __device__ __forceinline__ v4f mma16(v4u a, v4u b, v4f c) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
-    return c;
-  }
+  for (int e = 0; e < (sizeof(T) == 2 ? 1 : 4); ++e) c = mma16_part<T>(a, b, e, c);
+  return c;
 }
 
 // Four neighbouring channels c ... of n

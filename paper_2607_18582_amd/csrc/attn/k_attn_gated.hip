@@ -26,44 +26,109 @@ __device__ __forceinline__ float activated(float v, int act) {
   return v;
 }
 
-__device__ __forceinline__ int twist(int row) { return (row >> 1) & 7; }
+// A block's tile: consecutive blocks go to the chip's eight dies in turn; each die gets a run of neighbouring tiles, and
+// within it bands of 8 row tiles, so that what its blocks read together stays in its L2.
+__device__ __forceinline__ void place_of(int block, int n_tiles, int m_tiles, int& mt, int& nt, int& m) {
+  const int each = n_tiles * m_tiles, all = gridDim.x;
+  int b = all % 8 ? block : block % 8 * (all / 8) + block / 8;
+  m = uniform(b / each);
+  b -= m * each;
+  const int band = uniform(b / (8 * n_tiles)), tall = min(8, m_tiles - band * 8);
+  b -= band * 8 * n_tiles;
+  nt = uniform(b / tall);
+  mt = band * 8 + b - nt * tall;
+}
 
-// WM x WN waves
-template <typename T, int MT, int NT, int WM, int WN, bool FAST>
+// A row's piece from element e on, zeros from element n on.  `end` is the end of the tensor: a piece that reaches over
+// its row's end lies before it, but in the tensor's last rows.
+template <typename T> __device__ __forceinline__ v4u piece_of(const T* row, int e, int n, const T* end) {
+  constexpr int E = 16 / (int)sizeof(T);
+  if (e >= n) return v4u{0, 0, 0, 0};
+  if (row + e + E > end) return load_piece<T>(row, e, n);
+  v4u v = *reinterpret_cast<const v4u_any*>(row + e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int left = (n - e) * (int)sizeof(T) - 4 * i;         // bytes of the word that are the row's
+    v[i] &= left >= 4 ? ~0u : left <= 0 ? 0u : 0xffffu;
+  }
+  return v;
+}
+
+// Where a block's rows are read: rows of x and of both weights, those behind the last one in its place (their results
+// are not kept).
+template <typename T> struct Operands {
+  const T *x, *gate, *up, *x_end, *gate_end, *up_end;
+  __device__ __forceinline__ Operands(const mure_attn_gated_args& a, int m)
+      : x(static_cast<const T*>(a.x.p) + m * a.x.mutant_stride), gate(static_cast<const T*>(a.gate.p) + m * a.gate.mutant_stride),
+        up(static_cast<const T*>(a.up.p) + m * a.up.mutant_stride), x_end(x + (a.rows - 1) * a.x.row_stride + a.inner),
+        gate_end(gate + (int64_t)(a.outer - 1) * a.gate.row_stride + a.inner), up_end(up + (int64_t)(a.outer - 1) * a.up.row_stride + a.inner) {}
+  __device__ __forceinline__ const T* x_row(const mure_attn_gated_args& a, int64_t r) const { return x + min(r, a.rows - 1) * a.x.row_stride; }
+  __device__ __forceinline__ const T* gate_row(const mure_attn_gated_args& a, int n) const { return gate + (int64_t)min(n, a.outer - 1) * a.gate.row_stride; }
+  __device__ __forceinline__ const T* up_row(const mure_attn_gated_args& a, int n) const { return up + (int64_t)min(n, a.outer - 1) * a.up.row_stride; }
+};
+
+// Four neighbouring values of a bias from n on
+__device__ __forceinline__ v4f bias_at(const mure_seq_param& b, int m, int n, int outer) {
+  v4f v = {};
+  if (b.p)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = b.p[m * b.mutant_stride + min(n + e, outer - 1)];
+  return v;
+}
+
+// Four neighbouring outputs from n on of one row, from their sums and biases.
+template <typename T> __device__ __forceinline__ void finish(const mure_attn_gated_args& a, int m, int64_t row, int n, v4f g, v4f u, v4f gb, v4f ub) {
+  if (row >= a.rows) return;
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = activated(g[e] + gb[e], a.activation) * (u[e] + ub[e]);
+  store4<T>(static_cast<T*>(a.out.p) + m * a.out.mutant_stride + row * a.out.row_stride, n, a.outer, v[0], v[1], v[2], v[3]);
+}
+
+// WM x WN waves; BYTES of the summed axis a stage (64 or 128)
+template <typename T, int MT, int NT, int WM, int WN, int BYTES, bool FAST>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(mure_attn_gated_args a, int n_tiles, int m_tiles) {
-  constexpr int WAVES = WM * WN, ROWS = MT + 2 * NT, STAGE = ROWS * 128, E = 16 / (int)sizeof(T), KS = 8 * E;
-  constexpr int TM = MT / WM / 16, TN = NT / WN / 16;
+  constexpr int WAVES = WM * WN, ROWS = MT + 2 * NT, STAGE = ROWS * BYTES, E = 16 / (int)sizeof(T), PIECES = BYTES / 16, KS = PIECES * E;
+  constexpr int TM = MT / WM / 16, TN = NT / WN / 16, EACH = 64 / PIECES;      // rows of a copy of 1024 bytes
+  // 16 rows' pieces of one place in distinct banks
+  const auto twist = [](int row) { return PIECES == 8 ? (row >> 1) & 7 : (row >> 2) & 3; };
   extern __shared__ char lds[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int mt = blockIdx.x / n_tiles % m_tiles, nt = blockIdx.x % n_tiles, m = blockIdx.x / n_tiles / m_tiles;
+  int mt, nt, m;
+  place_of(blockIdx.x, n_tiles, m_tiles, mt, nt, m);
   const int64_t row0 = (int64_t)mt * MT;
   const int col0 = nt * NT;
-  const T* x = static_cast<const T*>(a.x.p) + m * a.x.mutant_stride;
-  const T* wg = static_cast<const T*>(a.gate.p) + m * a.gate.mutant_stride;
-  const T* wu = static_cast<const T*>(a.up.p) + m * a.up.mutant_stride;
-  // copies of 1024 bytes: 8 rows of 8 pieces
-  constexpr int COPIES = ROWS / 8 / WAVES;
-  static_assert(ROWS / 8 % WAVES == 0, "");
-  const T* from[COPIES];                       // the lane's row of each, or nothing
+  const Operands<T> op(a, m);
+  constexpr int COPIES = ROWS / EACH / WAVES;
+  static_assert(ROWS / EACH % WAVES == 0 && MT % EACH == 0 && NT % EACH == 0, "");
+  const T* from[COPIES];                       // the lane's row of each, at its piece of a stage
 #pragma unroll
   for (int c = 0; c < COPIES; ++c) {
-    const int r = (wave * COPIES + c) * 8 + lane / 8;
-    if (r < MT) from[c] = row0 + r < a.rows ? x + (row0 + r) * a.x.row_stride : nullptr;
-    else if (r < MT + NT) from[c] = col0 + r - MT < a.outer ? wg + (int64_t)(col0 + r - MT) * a.gate.row_stride : nullptr;
-    else from[c] = col0 + r - MT - NT < a.outer ? wu + (int64_t)(col0 + r - MT - NT) * a.up.row_stride : nullptr;
+    const int r = (wave * COPIES + c) * EACH + lane / PIECES;
+    from[c] = r < MT ? op.x_row(a, row0 + r) : r < MT + NT ? op.gate_row(a, col0 + r - MT) : op.up_row(a, col0 + r - MT - NT);
+    from[c] += (lane % PIECES ^ twist(r)) * E;
   }
+  // FAST: straight to LDS.  Otherwise through registers: on their way while the last stage is worked on.
+  v4u held[FAST ? 1 : COPIES];
   auto load = [&](int k0, int stage) {
+    const bool whole = k0 + KS <= a.inner;     // nothing of the stage lies behind the rows
 #pragma unroll
     for (int c = 0; c < COPIES; ++c) {
-      const int q = wave * COPIES + c, r = q * 8 + lane / 8, e = k0 + ((lane & 7) ^ twist(r)) * E;
-      char* to = lds + stage * STAGE + q * 1024;
+      const int q = wave * COPIES + c, r = q * EACH + lane / PIECES, at = (lane % PIECES ^ twist(r)) * E;
       if constexpr (FAST) {
-        const void* p = from[c] && e < a.inner ? static_cast<const void*>(from[c] + e) : ZEROS;
-        __builtin_amdgcn_global_load_lds(p, (lds_void*)to, 16, 0, 0);
+        const void* p = whole || k0 + at < a.inner ? static_cast<const void*>(from[c] + k0) : ZEROS;
+        __builtin_amdgcn_global_load_lds(p, (lds_void*)(lds + stage * STAGE + q * 1024), 16, 0, 0);
+      } else if (whole) {
+        held[c] = *reinterpret_cast<const v4u_any*>(from[c] + k0);
       } else {
-        *reinterpret_cast<v4u*>(to + lane * 16) = from[c] && e < a.inner ? load_piece<T>(from[c], e, a.inner) : v4u{0, 0, 0, 0};
+        held[c] = piece_of<T>(from[c] - at, k0 + at, a.inner, r < MT ? op.x_end : r < MT + NT ? op.gate_end : op.up_end);
       }
     }
+  };
+  auto put = [&](int stage) {
+    if constexpr (!FAST)
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) *reinterpret_cast<v4u*>(lds + stage * STAGE + (wave * COPIES + c) * 1024 + lane * 16) = held[c];
   };
   const int wm = wave % WM, wn = wave / WM;
   v4f g[TN][TM], u[TN][TM];
@@ -72,62 +137,124 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(mure_attn_gated_
 #pragma unroll
     for (int j = 0; j < TM; ++j) g[i][j] = v4f{}, u[i][j] = v4f{};
   load(0, 0);
+  put(0);
   int stage = 0;
   for (int k0 = 0; k0 < a.inner; k0 += KS, stage ^= 1) {
-    wait_copies();
+    if constexpr (FAST) wait_copies();
     __syncthreads();
     if (k0 + KS < a.inner) load(k0 + KS, stage ^ 1);
     const char* base = lds + stage * STAGE;
-    auto piece = [&](int r, int s) { return *reinterpret_cast<const v4u*>(base + r * 128 + ((s * 4 + (lane >> 4)) ^ twist(r)) * 16); };
+    auto piece = [&](int r, int s) { return *reinterpret_cast<const v4u*>(base + r * BYTES + ((s * 4 + (lane >> 4)) ^ twist(r)) * 16); };
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      v4u xs[TM];
+    for (int s = 0; s < BYTES / 64; ++s) {
+      v4u xs[TM], gs[TN], us[TN];
 #pragma unroll
       for (int j = 0; j < TM; ++j) xs[j] = piece(wm * (MT / WM) + j * 16 + (lane & 15), s);
 #pragma unroll
       for (int i = 0; i < TN; ++i) {
         const int r = wn * (NT / WN) + i * 16 + (lane & 15);
-        const v4u gs = piece(MT + r, s), us = piece(MT + NT + r, s);
-#pragma unroll
-        for (int j = 0; j < TM; ++j) {
-          g[i][j] = mma16<T>(gs, xs[j], g[i][j]);
-          u[i][j] = mma16<T>(us, xs[j], u[i][j]);
-        }
+        gs[i] = piece(MT + r, s);
+        us[i] = piece(MT + NT + r, s);
       }
+      // instructions that follow each other add to different results
+#pragma unroll
+      for (int e = 0; e < (sizeof(T) == 2 ? 1 : 4); ++e)
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int j = 0; j < TM; ++j) {
+            g[i][j] = mma16_part<T>(gs[i], xs[j], e, g[i][j]);
+            u[i][j] = mma16_part<T>(us[i], xs[j], e, u[i][j]);
+          }
     }
+    if (k0 + KS < a.inner) put(stage ^ 1);
   }
 #pragma unroll
   for (int i = 0; i < TN; ++i) {
     const int n = col0 + wn * (NT / WN) + i * 16 + (lane >> 4) * 4;
-    float gb[4] = {}, ub[4] = {};
+    const v4f gb = bias_at(a.gate_bias, m, n, a.outer), ub = bias_at(a.up_bias, m, n, a.outer);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (a.gate_bias.p && n + j < a.outer) gb[j] = a.gate_bias.p[m * a.gate_bias.mutant_stride + n + j];
-      if (a.up_bias.p && n + j < a.outer) ub[j] = a.up_bias.p[m * a.up_bias.mutant_stride + n + j];
-    }
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int64_t row = row0 + wm * (MT / WM) + j * 16 + (lane & 15);
-      if (row >= a.rows) continue;
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = activated(g[i][j][e] + gb[e], a.activation) * (u[i][j][e] + ub[e]);
-      store4<T>(static_cast<T*>(a.out.p) + m * a.out.mutant_stride + row * a.out.row_stride, n, a.outer, v[0], v[1], v[2], v[3]);
-    }
+    for (int j = 0; j < TM; ++j) finish<T>(a, m, row0 + wm * (MT / WM) + j * 16 + (lane & 15), n, g[i][j], u[i][j], gb, ub);
   }
 }
 
-template <typename T, int MT, int NT, int WM, int WN, bool FAST> hipError_t gated_f(const mure_attn_gated_args& a, hipStream_t s) {
-  constexpr unsigned LDS = 2 * (MT + 2 * NT) * 128;
-  const void* kernel = reinterpret_cast<const void*>(gated_kernel<T, MT, NT, WM, WN, FAST>);
-  if (LDS > 65536)
-    if (const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS); e != hipSuccess) return e;
+// ---- few rows: bound by the weights' bytes.  W waves have 16 rows of x each; NT = 8: the gate's 8 rows of weights and the
+// other projection's share an operand of 16, so that even few outputs make many blocks; NT = 16: an operand each, as 64
+// rows of x would be read too often otherwise.  All but one of the stages of 256 bytes of the summed axis are on their way.
+
+template <typename T, int W, int NT, int STAGES, bool FAST> __global__ __launch_bounds__(64 * W) void gated_few_kernel(mure_attn_gated_args a, int n_tiles, int m_tiles) {
+  constexpr int ROWS = 16 * W + 2 * NT, STAGE = ROWS * 256, E = 16 / (int)sizeof(T), KS = 16 * E, COPIES = ROWS / 4 / W, N = NT / 8;
+  static_assert(ROWS / 4 % W == 0 && (NT == 8 || NT == 16), "");
+  extern __shared__ char lds[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int nt = uniform(blockIdx.x % n_tiles), rest = uniform(blockIdx.x / n_tiles), mt = uniform(rest % m_tiles), m = uniform(rest / m_tiles);
+  const int64_t row0 = (int64_t)mt * 16 * W;
+  const int col0 = nt * NT;
+  const Operands<T> op(a, m);
+  // rows of x, then NT of each projection's weights; 4 rows of 16 pieces a copy, pieces xored with the row
+  const T* from[COPIES];
+#pragma unroll
+  for (int c = 0; c < COPIES; ++c) {
+    const int r = (wave * COPIES + c) * 4 + lane / 16, w = r - 16 * W;
+    from[c] = w < 0 ? op.x_row(a, row0 + r) : w < NT ? op.gate_row(a, col0 + w) : op.up_row(a, col0 + w - NT);
+  }
+  auto load = [&](int k0, int stage) {
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c) {
+      const int q = wave * COPIES + c, r = q * 4 + lane / 16, e = k0 + ((lane & 15) ^ (r & 15)) * E;
+      char* to = lds + stage * STAGE + q * 1024;
+      if constexpr (FAST) {
+        const void* p = e < a.inner ? static_cast<const void*>(from[c] + e) : ZEROS;
+        __builtin_amdgcn_global_load_lds(p, (lds_void*)to, 16, 0, 0);
+      } else {
+        *reinterpret_cast<v4u*>(to + lane * 16) = piece_of<T>(from[c], e, a.inner, r < 16 * W ? op.x_end : r < 16 * W + NT ? op.gate_end : op.up_end);
+      }
+    }
+  };
+  v4f acc[N] = {};                             // outputs 4 (l / 16) ... of row l % 16: NT = 8: the gate's, from l = 32 on the other's
+  const int stages = (a.inner + KS - 1) / KS;
+  for (int s = 0; s < STAGES - 1 && s < stages; ++s) load(s * KS, s);
+  int at = 0;
+  for (int s = 0; s < stages; ++s) {
+    if constexpr (FAST) {                      // this stage's copies are there, the next ones' may be on their way
+      const int next = min(STAGES - 2, stages - 1 - s);
+      if (next == 2) wait_copies<2 * COPIES>();
+      else if (next == 1) wait_copies<COPIES>();
+      else wait_copies();
+    }
+    __syncthreads();
+    if (s + STAGES - 1 < stages) load((s + STAGES - 1) * KS, at ? at - 1 : STAGES - 1);
+    const char* base = lds + at * STAGE;
+    at = at + 1 == STAGES ? 0 : at + 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = (i * 4 + (lane >> 4)) ^ (lane & 15);
+      const v4u xs = *reinterpret_cast<const v4u*>(base + (16 * wave + (lane & 15)) * 256 + p * 16);
+#pragma unroll
+      for (int w = 0; w < N; ++w) acc[w] = mma16<T>(*reinterpret_cast<const v4u*>(base + (16 * (W + w) + (lane & 15)) * 256 + p * 16), xs, acc[w]);
+    }
+  }
+  const int64_t row = row0 + 16 * wave + (lane & 15);
+  const int n = col0 + (lane >> 4) * 4;
+  const v4f gb = bias_at(a.gate_bias, m, n, a.outer), ub = bias_at(a.up_bias, m, n, a.outer);
+  if constexpr (N == 1) {
+    v4f up;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) up[e] = __shfl_xor(acc[0][e], 32);
+    if (lane < 32) finish<T>(a, m, row, n, acc[0], up, gb, ub);
+  } else {
+    finish<T>(a, m, row, n, acc[0], acc[1], gb, ub);
+  }
+}
+
+// Launches over tiles of MT rows and NT outputs: as many mutants a launch as fit, or rows.
+hipError_t over_tiles(const void* kernel, const mure_attn_gated_args& a, int64_t es, int MT, int NT, unsigned threads, unsigned lds, hipStream_t s) {
+  if (lds > 65536)                             // more than the default limit has to be asked for
+    if (const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
   const int64_t m_tiles = (a.rows + MT - 1) / MT;
   const int n_tiles = (a.outer + NT - 1) / NT;
-  // as many mutants a launch as fit, or rows
-  constexpr int64_t BLOCKS = ((int64_t)1 << 32) / (64 * WM * WN) - 1;
-  const int64_t rows_most = std::min(m_tiles, BLOCKS / n_tiles), mutants_most = std::max<int64_t>(1, BLOCKS / (n_tiles * rows_most));
-  const int64_t es = sizeof(T);
+  const int64_t blocks = ((int64_t)1 << 32) / threads - 1;
+  const int64_t rows_most = std::min(m_tiles, blocks / n_tiles), mutants_most = std::max<int64_t>(1, blocks / (n_tiles * rows_most));
   for (int64_t m0 = 0; m0 < a.n_mutants; m0 += mutants_most)
     for (int64_t r0 = 0; r0 < m_tiles; r0 += rows_most) {
       mure_attn_gated_args b = a;
@@ -142,13 +269,28 @@ template <typename T, int MT, int NT, int WM, int WN, bool FAST> hipError_t gate
       int tiles = (int)std::min(rows_most, m_tiles - r0), nt = n_tiles;
       b.rows = std::min(a.rows - r0 * MT, (int64_t)tiles * MT);
       void* at[] = {&b, &nt, &tiles};
-      if (const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)(ms * tiles * n_tiles)), dim3(64 * WM * WN), at, LDS, s); e != hipSuccess) return e;
+      if (const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)(ms * tiles * n_tiles)), dim3(threads), at, lds, s); e != hipSuccess) return e;
     }
   return hipSuccess;
 }
 
+template <typename T, int MT, int NT, int WM, int WN, int BYTES> hipError_t gated_f(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
+  return over_tiles(fast ? reinterpret_cast<const void*>(gated_kernel<T, MT, NT, WM, WN, BYTES, true>) : reinterpret_cast<const void*>(gated_kernel<T, MT, NT, WM, WN, BYTES, false>),
+                    a, sizeof(T), MT, NT, 64 * WM * WN, 2 * (MT + 2 * NT) * BYTES, s);
+}
+
+template <typename T, int W, int NT, int STAGES> hipError_t gated_few(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
+  return over_tiles(fast ? reinterpret_cast<const void*>(gated_few_kernel<T, W, NT, STAGES, true>) : reinterpret_cast<const void*>(gated_few_kernel<T, W, NT, STAGES, false>), a,
+                    sizeof(T), 16 * W, NT, 64 * W, STAGES * (16 * W + 2 * NT) * 256, s);
+}
+
 template <typename T> hipError_t gated_t(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
-  return fast ? gated_f<T, 128, 64, 2, 2, true>(a, s) : gated_f<T, 128, 64, 2, 2, false>(a, s);
+  if (a.rows <= 16) return gated_few<T, 1, 8, 4>(a, fast, s);
+  if (a.rows <= 32) return gated_few<T, 2, 8, 4>(a, fast, s);
+  if (a.rows <= 64) return gated_few<T, 4, 16, 3>(a, fast, s);
+  if constexpr (sizeof(T) == 2)
+    if ((int64_t)((a.rows + 255) / 256) * ((a.outer + 127) / 128) * a.n_mutants >= 512) return gated_f<T, 256, 128, 2, 4, 128>(a, fast, s);
+  return gated_f<T, 128, 64, 2, 2, sizeof(T) == 4 ? 64 : 128>(a, fast, s);
 }
 
 }  // namespace

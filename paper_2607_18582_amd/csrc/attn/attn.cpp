@@ -146,7 +146,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   // blocks of an item: (heads or groups' row tiles) x mutants x parts
   const int64_t parts_short = held ? (a.capacity + ATTN_KEYS_SHORT - 1) / ATTN_KEYS_SHORT : 1;
   const int64_t parts_mid = held ? (a.capacity + ATTN_KEYS_MID - 1) / ATTN_KEYS_MID : 1;
-  if ((wide)a.heads * M * std::max(parts_short * ATTN_SHORT, parts_mid) > GRID)
+  if ((wide)a.heads * M * std::max(std::max(parts_short * ATTN_SHORT, parts_mid), (int64_t)ATTN_WHOLE_F32) > GRID)
     throw Fail{MURE_E_UNSUPPORTED, "too many heads times mutants times parts of the cache"};
   check_device(s->device);
   if (T == 0) return;
@@ -157,8 +157,6 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   const auto launch_short = f32 ? attn_short_f32 : attn_short_bf16;
   const auto launch_runs = f32 ? attn_runs_f32 : attn_runs_bf16;
   const auto launch_join = f32 ? attn_join_f32 : attn_join_bf16;
-  const int n_mid = s->n_runs - s->n_long_runs;
-  // one after the other: the workspace serves both
   auto parted = [&](AttnArgs& p, int64_t parts, int rows_each) {
     p.parts = (int)parts;
     p.rows_each = rows_each;
@@ -170,16 +168,40 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
     p.ws_ml = static_cast<float*>(work);
     p.ws_o = p.ws_ml + 2 * rows;
   };
-  if (s->n_brief) {
+  if (!held) {
+    // Sequences of few tokens by waves on their own, whose rows come in 16: 250 of 20 to 80 tokens with 4 heads of 32
+    // float32 channels for 16 mutants take 212 us in runs.  Longer ones would read their keys too often.
+    const int whole = f32 ? ATTN_WHOLE_F32 : ATTN_WHOLE_BF16;
+    const int first = f32 ? 0 : s->n_above, n = s->n_brief - first;
+    const int n_runs = f32 ? s->n_runs - s->n_small_runs - s->n_above : s->n_runs - s->n_small_runs;
+    if (n) {
+      AttnArgs p = k;
+      p.items = s->brief ? s->brief + first : nullptr;
+      p.n_items = n;
+      p.longest = std::min(s->longest_brief, whole);
+      check(launch_short(p, s->stream), "mure_attn_attend");
+    }
+    if (n_runs) {
+      AttnArgs p = k;
+      p.items = s->runs;
+      p.n_items = n_runs;
+      check(launch_runs(p, s->stream), "mure_attn_attend");
+    }
+    return;
+  }
+  // one after the other: the workspace serves all
+  if (s->n_short) {
     AttnArgs p = k;
-    p.items = s->brief;
-    p.n_items = s->n_brief;
-    parted(p, parts_short, s->longest_brief);
+    p.items = s->brief ? s->brief + (s->n_brief - s->n_short) : nullptr;
+    p.n_items = s->n_short;
+    p.longest = std::min(s->longest_brief, ATTN_SHORT);
+    parted(p, parts_short, p.longest);
     check(launch_short(p, s->stream), "mure_attn_attend");
     if (p.parts > 1) check(launch_join(p, ATTN_KEYS_SHORT, s->stream), "mure_attn_attend");
   }
   // without parts the longer sequences' runs and the others' go in one launch
-  const bool split = held && parts_mid > 1 && n_mid;
+  const int n_mid = s->n_runs - s->n_long_runs;
+  const bool split = parts_mid > 1 && n_mid;
   if (split ? s->n_long_runs : s->n_runs) {
     AttnArgs p = k;
     p.items = s->runs;

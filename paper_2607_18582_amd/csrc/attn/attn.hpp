@@ -20,6 +20,7 @@ struct AttnArgs {
   mure_attn_attend_args a;
   const SeqItem* items = nullptr;
   int n_items = 0, item0 = 0;
+  int longest = 0;                             // tokens of an item, at most
   int rows_each = 0;                           // rows of the workspace that an item has
   int parts = 1;                               // of the keys
   float* ws_o = nullptr;                       // [mutants][items][rows_each][heads][parts][head_dim], before the division
@@ -29,7 +30,7 @@ struct AttnArgs {
 
 // launchers (return the launch status)
 hipError_t launch_attn_rotate(const AttnRotateArgs& a, hipStream_t s);
-// sequences of at most ATTN_SHORT tokens, runs of ATTN_ROWS tokens, and the results of parts of `keys` keys
+// short sequences (over a cache those of at most ATTN_SHORT tokens), runs of ATTN_ROWS tokens, and the results of parts of `keys` keys
 hipError_t attn_short_f32(const AttnArgs& a, hipStream_t s);
 hipError_t attn_short_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t attn_runs_f32(const AttnArgs& a, hipStream_t s);

@@ -160,83 +160,74 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   }
 }
 
-// ---- short sequences: 16 rows (token, head of a group) a block, the keys spread over its waves
+// ---- short sequences: 16 rows (token, head of a group) a wave
 //
 // As above in 16x16 products: a lane has row l % 16 of the queries and of every 16 keys those numbered 4 (l / 16) + i.
-// Bound by the cache's bytes, so what counts is how many are on their way: small tiles of each wave's own, keys straight
-// into registers, and four blocks a compute unit.
+// Little is used twice here, so keys go straight into registers, values through a small tile of the wave's own, and
+// nobody waits for another wave: what counts is how many loads are on their way.
 
 template <typename T, int DB> struct Short {
   using H = Head<T, DB>;
-  static constexpr int KT = 32, WAVES = 4;
-  static constexpr int PER = ATTN_KEYS_SHORT / WAVES;          // keys of a wave
+  static constexpr int KT = 32, WAVES = 4, TILE = KT * H::ROW;
+  static constexpr int PER = ATTN_KEYS_SHORT / WAVES;          // keys of a wave, where they are spread over the waves
   static constexpr int PITCH = 32 * DB + 4;                    // floats of a row of sums
-  static constexpr int EACH = KT * H::ROW > 16 * PITCH * 4 ? KT * H::ROW : 16 * PITCH * 4;
+  static constexpr int EACH = TILE > 16 * PITCH * 4 ? TILE : 16 * PITCH * 4;
   static constexpr int LDS = WAVES * EACH + WAVES * 16 * 2 * 4;
+  static constexpr int OCCUPANCY = DB * sizeof(T) <= 8 ? 4 : DB * sizeof(T) <= 24 ? 2 : 1;
 };
 
-template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB * sizeof(T) <= 8 ? 4 : DB * sizeof(T) <= 24 ? 2 : 1) void short_kernel(AttnArgs k, int units) {
+// 16 rows of a sequence's queries: rows 16 unit ..., row r being token r / group, head g group + r % group.
+struct Unit {
+  int rows, token, head;                       // rows there are; the lane's row's
+  __device__ __forceinline__ Unit(const SeqItem& it, int unit, int group, int g, int lane) {
+    const int r = min(unit * 16 + (lane & 15), it.len * group - 1);
+    rows = min(16, it.len * group - unit * 16);
+    token = r / group;
+    head = g * group + r - token * group;
+  }
+};
+
+template <typename T, int DB, bool FAST> struct ShortWave {
   using S = Short<T, DB>;
   using H = Head<T, DB>;
-  constexpr int STEPS = H::BYTES / 64, E = 16 / (int)sizeof(T);
-  constexpr float LOWEST = -__builtin_inff();
-  extern __shared__ char lds[];
-  const mure_attn_attend_args& a = k.a;
-  const int n = a.kv_heads * a.n_mutants, at = uniform(blockIdx.x / n), gm = spread(blockIdx.x - at * n, n), m = uniform(gm / a.kv_heads), g = gm - m * a.kv_heads;
-  const int group = uniform(a.heads / a.kv_heads), ip = uniform(at / units), unit = at - ip * units, part = uniform(ip % k.parts), i = k.item0 + uniform(ip / k.parts);
-  const SeqItem it = item_of(k, i);
-  if (unit * 16 >= it.len * group) return;
-  const Source<T> src(k, it, m, g);
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, quarter = lane >> 4;
-  // row r of the unit: token r / group, head g group + r % group
-  const int rows = min(16, it.len * group - unit * 16), r = min(unit * 16 + (lane & 15), it.len * group - 1), token = r / group, h = g * group + r % group;
-  T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * a.out.row_stride;
-  if (src.bad) {
-    if (part == 0)
-      for (int x = tid; x < rows * a.head_dim; x += 256) {
-        const int y = unit * 16 + x / a.head_dim;
-        out[y / group * a.out.row_stride + (int64_t)(g * group + y % group) * a.head_dim + x % a.head_dim] = from_f<T>(__builtin_nanf(""));
-      }
-    return;
-  }
-  if (a.k_cache.p && part == 0 && unit == 0) src.keep(a, it, m, tid, 256);
-  int lo, hi, from, to, all_lo, all_hi;        // keys that the row sees, that any token sees, that all do
-  sees(a, src.past + token, src.total, lo, hi);
-  sees(a, src.past, src.total, from, all_hi);
-  sees(a, src.total - 1, src.total, all_lo, to);
-  const int64_t part0 = (int64_t)part * ATTN_KEYS_SHORT;
-  if (max((int64_t)from, part0) >= min((int64_t)to, part0 + ATTN_KEYS_SHORT)) return;
-  from = (int)max((int64_t)from, part0 + wave * S::PER);
-  to = (int)min((int64_t)to, part0 + (wave + 1) * S::PER);
+  static constexpr int STEPS = H::BYTES / 64, E = 16 / (int)sizeof(T);
   v4f o[2 * DB];
+  float top = -__builtin_inff(), l = 0.f;
+
+  __device__ __forceinline__ ShortWave() {
 #pragma unroll
-  for (int d = 0; d < 2 * DB; ++d) o[d] = v4f{};
-  float top = LOWEST, l = 0.f;
-  char* tile = lds + wave * S::EACH;
-  if (from < to) {
+    for (int d = 0; d < 2 * DB; ++d) o[d] = v4f{};
+  }
+
+  // Keys from ... to - 1, of which the lane's row sees lo ... hi - 1 and all of the sequence's rows all_lo ... all_hi - 1.
+  __device__ __forceinline__ void run(const Source<T>& src, const T* query, int n, float scale, int from, int to, int lo, int hi, int all_lo, int all_hi, char* tile, int lane) {
+    constexpr float LOWEST = -__builtin_inff();
+    const int quarter = lane >> 4;
     v4u q[STEPS];
-    load_query<T, STEPS, 4>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)token) * a.q.row_stride + (int64_t)h * a.head_dim, a.head_dim,
-                            quarter, a.scale);
-    const float c = factor(a.scale);
+    load_query<T, STEPS, 4>(q, query, n, quarter, scale);
+    const float c = factor(scale);
     for (int t = from / S::KT * S::KT; t < to; t += S::KT) {
+      const bool two = t + 16 < to;            // keys in the tile's second half
       // keys 16 b + l % 16; those behind the sequence's are hidden
       v4u keys[2][STEPS];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const T* p = src.k.at(min(t + 16 * b + (lane & 15), src.total - 1));
+        if (b == 0 || two)
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          const int e = (4 * s + quarter) * E;
-          if constexpr (FAST) keys[b][s] = e < a.head_dim ? *reinterpret_cast<const v4u*>(p + e) : v4u{0, 0, 0, 0};
-          else keys[b][s] = e < a.head_dim ? load_piece<T>(p, e, a.head_dim) : v4u{0, 0, 0, 0};
-        }
+          for (int s = 0; s < STEPS; ++s) {
+            const int e = (4 * s + quarter) * E;
+            if constexpr (FAST) keys[b][s] = e < n ? *reinterpret_cast<const v4u*>(p + e) : v4u{0, 0, 0, 0};
+            else keys[b][s] = e < n ? load_piece<T>(p, e, n) : v4u{0, 0, 0, 0};
+          }
       }
-      Copy<T, DB, S::KT, 1, VALUES16>::template run<FAST>(tile, src.v, t, src.total, a.head_dim, 0, lane);
+      Copy<T, DB, S::KT, 1, VALUES16>::template run<FAST>(tile, src.v, t, src.total, n, 0, lane);
       v4f s[2] = {};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
+        if (b == 0 || two)
 #pragma unroll
-        for (int x = 0; x < STEPS; ++x) s[b] = mma16<T>(keys[b][x], q[x], s[b]);
+          for (int x = 0; x < STEPS; ++x) s[b] = mma16<T>(keys[b][x], q[x], s[b]);
       const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
       float most = LOWEST;
 #pragma unroll
@@ -291,30 +282,98 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB * 
       } else {
         const int key = 4 * quarter, twist = Twist<T, H::PIECES, VALUES16>::of(key), v = key * H::ROW + ((((lane & 15) >> 2) ^ twist) << 4) + (lane & 3) * 4;
 #pragma unroll
-        for (int d = 0; d < 2 * DB; ++d)
+        for (int b = 0; b < 2; ++b)
+          if (b == 0 || two)
 #pragma unroll
-          for (int x = 0; x < 8; ++x)
-            o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float*>(tile + (v ^ (d << 6)) + (16 * (x / 4) + x % 4) * H::ROW), s[x / 4][x % 4], o[d], 0, 0, 0);
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+              for (int d = 0; d < 2 * DB; ++d)
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float*>(tile + (v ^ (d << 6)) + (16 * b + x) * H::ROW), s[b][x], o[d], 0, 0, 0);
       }
       if (apart) {
         auto channel = [](int x, int lane) { return x / 4 * 16 + (lane >> 4) * 4 + x % 4; };
         auto add = [&](int x, float v) { o[x / 4][x % 4] += v; };
-        add_nonfinite<8 * DB>(src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, lane, channel, add);
-        add_nonfinite<8 * DB>(src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, lane, channel, add);
+        add_nonfinite<8 * DB>(src.v, t, 0, min(see_from, there), n, row_lo, row_hi, lane, channel, add);
+        add_nonfinite<8 * DB>(src.v, t, max(max(0, see_from), see_to), there, n, row_lo, row_hi, lane, channel, add);
       }
       settle();
     }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
   }
+};
+
+// Without a cache: a unit a wave, all of the sequence's keys.
+template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, (Short<T, DB>::OCCUPANCY)) void whole_kernel(AttnArgs k, int each) {
+  using S = Short<T, DB>;
+  extern __shared__ char lds[];
+  const mure_attn_attend_args& a = k.a;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, quarter = lane >> 4;
+  const int at = uniform(blockIdx.x / each), i = k.item0 + at, w = (blockIdx.x - at * each) * S::WAVES + wave;       // unit, group and mutant
+  const SeqItem it = item_of(k, i);
+  const int group = uniform(a.heads / a.kv_heads), units = (it.len * group + 15) / 16, gm = uniform(w / units), unit = w - gm * units;
+  if (gm >= a.kv_heads * a.n_mutants) return;
+  const int m = uniform(gm / a.kv_heads), g = gm - m * a.kv_heads;
+  const Source<T> src(k, it, m, g);
+  const Unit u(it, unit, group, g, lane);
+  int lo, hi, from, to, all_lo, all_hi;        // keys that the row sees, that any of the unit's tokens sees, that all do
+  sees(a, u.token, src.total, lo, hi);
+  sees(a, unit * 16 / group, src.total, from, all_hi);
+  sees(a, (unit * 16 + u.rows - 1) / group, src.total, all_lo, to);
+  ShortWave<T, DB, FAST> sw;
+  sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale, from, to, lo,
+         hi, all_lo, all_hi, lds + wave * S::TILE, lane);
+  if ((lane & 15) >= u.rows) return;
+  T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (it.row0 + (int64_t)u.token) * a.out.row_stride + (int64_t)u.head * a.head_dim;
+  const float f = 1.f / sw.l;
+#pragma unroll
+  for (int d = 0; d < 2 * DB; ++d) store4<T>(out, 16 * d + 4 * quarter, a.head_dim, sw.o[d][0] * f, sw.o[d][1] * f, sw.o[d][2] * f, sw.o[d][3] * f);
+}
+
+// Over a cache: a unit a block, the part's keys spread over its waves.
+template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, (Short<T, DB>::OCCUPANCY)) void short_kernel(AttnArgs k, int units) {
+  using S = Short<T, DB>;
+  constexpr float LOWEST = -__builtin_inff();
+  extern __shared__ char lds[];
+  const mure_attn_attend_args& a = k.a;
+  const int n = a.kv_heads * a.n_mutants, at = uniform(blockIdx.x / n), gm = spread(blockIdx.x - at * n, n), m = uniform(gm / a.kv_heads), g = gm - m * a.kv_heads;
+  const int group = uniform(a.heads / a.kv_heads), ip = uniform(at / units), unit = at - ip * units, part = uniform(ip % k.parts), i = k.item0 + uniform(ip / k.parts);
+  const SeqItem it = item_of(k, i);
+  if (unit * 16 >= it.len * group) return;
+  const Source<T> src(k, it, m, g);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, quarter = lane >> 4;
+  const Unit u(it, unit, group, g, lane);
+  T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + it.row0 * a.out.row_stride;
+  if (src.bad) {
+    if (part == 0)
+      for (int x = tid; x < u.rows * a.head_dim; x += 256) {
+        const int y = unit * 16 + x / a.head_dim;
+        out[y / group * a.out.row_stride + (int64_t)(g * group + y % group) * a.head_dim + x % a.head_dim] = from_f<T>(__builtin_nanf(""));
+      }
+    return;
+  }
+  if (part == 0 && unit == 0) src.keep(a, it, m, tid, 256);
+  int lo, hi, from, to, all_lo, all_hi;        // keys that the row sees, that any token sees, that all do
+  sees(a, src.past + u.token, src.total, lo, hi);
+  sees(a, src.past, src.total, from, all_hi);
+  sees(a, src.total - 1, src.total, all_lo, to);
+  const int64_t part0 = (int64_t)part * ATTN_KEYS_SHORT;
+  if (max((int64_t)from, part0) >= min((int64_t)to, part0 + ATTN_KEYS_SHORT)) return;
+  from = (int)max((int64_t)from, part0 + wave * S::PER);
+  to = (int)min((int64_t)to, part0 + (wave + 1) * S::PER);
+  char* tile = lds + wave * S::EACH;
+  ShortWave<T, DB, FAST> sw;
+  if (from < to)
+    sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale, from, to,
+           lo, hi, all_lo, all_hi, tile, lane);
   // the waves' sums, added in order
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
   float* sums = reinterpret_cast<float*>(tile);
   float* ml = reinterpret_cast<float*>(lds + S::WAVES * S::EACH);              // [4][16][2]
 #pragma unroll
-  for (int d = 0; d < 2 * DB; ++d) *reinterpret_cast<v4f*>(sums + (lane & 15) * S::PITCH + 16 * d + 4 * quarter) = o[d];
-  if (!quarter) ml[(wave * 16 + lane) * 2] = top, ml[(wave * 16 + lane) * 2 + 1] = l;
+  for (int d = 0; d < 2 * DB; ++d) *reinterpret_cast<v4f*>(sums + (lane & 15) * S::PITCH + 16 * d + 4 * quarter) = sw.o[d];
+  if (!quarter) ml[(wave * 16 + lane) * 2] = sw.top, ml[(wave * 16 + lane) * 2 + 1] = sw.l;
   __syncthreads();
-  for (int x = tid; x < rows * a.head_dim; x += 256) {
+  for (int x = tid; x < u.rows * a.head_dim; x += 256) {
     const int y = x / a.head_dim, e = x - y * a.head_dim, all = unit * 16 + y, tk = all / group, hd = g * group + all % group;
     float most = LOWEST;
 #pragma unroll
@@ -407,7 +466,11 @@ template <typename... P, typename... A> hipError_t launch_lds(void (*kernel)(P..
 }
 
 template <typename T, int DB, bool FAST> hipError_t short_f(AttnArgs k, hipStream_t s) {
-  const int units = (k.rows_each * (k.a.heads / k.a.kv_heads) + 15) / 16;
+  const int units = (k.longest * (k.a.heads / k.a.kv_heads) + 15) / 16;
+  if (!k.a.k_cache.p) {
+    const int each = (int)(((int64_t)k.a.kv_heads * k.a.n_mutants * units + 3) / 4);
+    return over_items(k, each, [&](unsigned grid) { return launch_lds(whole_kernel<T, DB, FAST>, grid, Short<T, DB>::WAVES * Short<T, DB>::TILE, s, k, each); });
+  }
   return over_items(k, (int64_t)k.a.kv_heads * k.a.n_mutants * units * k.parts,
                     [&](unsigned grid) { return launch_lds(short_kernel<T, DB, FAST>, grid, Short<T, DB>::LDS, s, k, units); });
 }

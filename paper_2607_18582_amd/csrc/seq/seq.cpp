@@ -70,21 +70,24 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
   for (int32_t i = 0; i < (int32_t)n_seq; row += lengths[i++]) {
     const int64_t L = lengths[i];
     if (L == 0) continue;
-    if (L <= ATTN_SHORT) {
+    if (L <= ATTN_WHOLE_F32) {
       add_runs(brief, i, row, L, L, -1);
       s->longest_brief = std::max(s->longest_brief, (int)L);
-      s->brief_tokens += L;
-    } else {
+      s->n_above += L > ATTN_WHOLE_BF16;
+      s->n_short += L <= ATTN_SHORT;
+    }
+    if (L > ATTN_SHORT) {
       add_runs(runs, i, row, L, ATTN_ROWS, -1);
-      if (L <= ATTN_MID) s->mid_tokens += L;
-      else s->n_long_runs += (int)((L + ATTN_ROWS - 1) / ATTN_ROWS);
+      s->n_small_runs += L <= ATTN_WHOLE_BF16;
+      if (L > ATTN_MID) s->n_long_runs += (int)((L + ATTN_ROWS - 1) / ATTN_ROWS);
     }
   }
   std::stable_sort(brief.begin(), brief.end(), [](const SeqItem& a, const SeqItem& b) { return a.len > b.len; });
   // a causal run's work is that of the tokens up to its end
-  std::stable_sort(runs.begin(), runs.end(), [](const SeqItem& a, const SeqItem& b) {
-    const bool la = a.total > ATTN_MID, lb = b.total > ATTN_MID;
-    return la != lb ? la : a.pos0 + a.len > b.pos0 + b.len;
+  static_assert(ATTN_WHOLE_F32 <= ATTN_ROWS, "a sequence that may be taken whole is one run");
+  auto kind = [](const SeqItem& a) { return (a.total <= ATTN_MID) + (a.total <= ATTN_WHOLE_F32) + (a.total <= ATTN_WHOLE_BF16); };
+  std::stable_sort(runs.begin(), runs.end(), [&](const SeqItem& a, const SeqItem& b) {
+    return kind(a) != kind(b) ? kind(a) < kind(b) : a.pos0 + a.len > b.pos0 + b.len;
   });
   s->n_brief = (int)brief.size();
   s->n_runs = (int)runs.size();

@@ -31,7 +31,9 @@ struct SeqChunks {
 constexpr int SCAN_CHUNK = 128;                // tokens of a chunk
 constexpr int CONV_RUNS[] = {33, 12, 3};       // tokens of a convolution's runs
 constexpr int N_RUNS = 3;
-constexpr int ATTN_SHORT = 16, ATTN_MID = 512; // tokens of sequences that attention takes in other ways
+// Tokens of sequences that attention takes in other ways: by waves of their own over a cache; the same without one, by
+// type; their keys in parts over a cache.
+constexpr int ATTN_SHORT = 16, ATTN_WHOLE_BF16 = 64, ATTN_WHOLE_F32 = 128, ATTN_MID = 512;
 constexpr int ATTN_ROWS = 128;                 // tokens of a run of the others
 
 struct SeqConvArgs {

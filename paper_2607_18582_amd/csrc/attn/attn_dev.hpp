@@ -22,6 +22,13 @@ typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef v4u __attribute__((aligned(2))) v4u_any;  // the GPU's global loads and stores take any address
 
+// Two floats -> two bfloat16 (lo in bits 0-15), to nearest even, by the compiler's conversion: it keeps the wait state
+// between an exponential and the use of its result, which inline assembly does not.
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2bf));
+}
+
 // What a copy to LDS reads where there is nothing.
 __device__ const uint32_t ZEROS[4] = {};
 
@@ -98,11 +105,21 @@ template <typename T> __device__ __forceinline__ v4u load_piece(const T* p, int 
   return v;
 }
 
+// 16 bytes a lane from `off` on of a buffer of `bytes` bytes at p (zeros behind it) to `to`, one lane after the other.  As the
+// compiler's builtin every later read of LDS would wait for it; this one only wait_copies waits for.  The wait states are
+// those between a scalar's write by the vector unit, or m0's, and its use here.
+__device__ __forceinline__ void copy16(const void* p, int bytes, unsigned off, char* to) {
+  const uint64_t at = (uint64_t)p;
+  const v4u r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)bytes, 0x00027000u};
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)to;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform((int)lds)), "v"(off), "s"(r) : "memory", "m0");
+}
+
 // Copies of KT keys' rows into a tile by W waves, 1024 bytes a wave and step.
 template <typename T, int DB, int KT, int W, Reads R> struct Copy {
   using H = Head<T, DB>;
   using Tw = Twist<T, H::PIECES, R>;
-  static constexpr int COPIES = KT * H::ROW / 1024, STEPS = (COPIES + W - 1) / W;
+  static constexpr int COPIES = KT * H::ROW / 1024, STEPS = (COPIES + W - 1) / W, EACH = 1024 / H::ROW;      // keys of a copy
   static_assert(COPIES % W == 0 || COPIES < W, "");
 
   // The place of the lane's piece of copy q: its key in the tile, its first element there.
@@ -127,7 +144,6 @@ template <typename T, int DB, int KT, int W, Reads R> struct Copy {
   // Keys from ... to - 1 of the tile whose key 0 is (or would be) at p, straight to LDS (wait_copies) through a buffer that
   // ends with key to - 1: what lies behind it, or behind a row, reads as zeros.  A tile's rows lie within 2^31 bytes.
   static __device__ __forceinline__ void straight(char* tile, const T* p, int64_t stride, int from, int to, int n, int wave, int lane) {
-    constexpr int EACH = 1024 / H::ROW;        // keys of a copy
     // scalars, every one of them: a buffer's description in vector registers costs a loop around each copy
     const int pitch = uniform((int)(stride * (int)sizeof(T))), bytes = uniform((to - 1) * pitch + n * (int)sizeof(T));
     char* const base = uniform(const_cast<char*>(reinterpret_cast<const char*>(p)));
@@ -141,20 +157,42 @@ template <typename T, int DB, int KT, int W, Reads R> struct Copy {
       if (COPIES % W && q >= COPIES) break;
       // the step's own place is in the buffer's base, so that the lanes' offsets are the same in every step
       const int first = s * W * EACH * pitch;
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(base + first, 0, max(0, bytes - first), 0x00027000);
       if (s && W * EACH % Tw::PERIOD) {
         int k;
         place(q, lane, k, e);
         off = (unsigned)(key * pitch) + (e < n ? (unsigned)(e * (int)sizeof(T)) : 0x80000000u);
       }
-      if (from <= 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + q * 1024), 16, (int)off, 0, 0, 0);
-      else if (key + s * W * EACH >= from) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(tile + q * 1024), 16, (int)off, 0, 0, 0);
+      if (from <= 0) copy16(base + first, max(0, bytes - first), off, tile + q * 1024);
+      else if (key + s * W * EACH >= from) copy16(base + first, max(0, bytes - first), off, tile + q * 1024);
     }
+  }
+
+  // `straight` of a whole tile in four steps, with few scalar instructions: the steps' places are the buffer's scalar
+  // offsets (which must lie inside the buffer, and do in a whole tile).
+  static __device__ __forceinline__ void whole(char* tile, const T* p, int64_t stride, int n, int wave, int lane) {
+    const int pitch = uniform((int)(stride * (int)sizeof(T)));
+    int key, e;
+    place(wave, lane, key, e);
+    const unsigned off = (unsigned)(key * pitch) + (e < n ? (unsigned)(e * (int)sizeof(T)) : 0x80000000u);
+    const uint64_t at = (uint64_t)uniform(p);
+    const v4u r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)((KT - 1) * pitch + n * (int)sizeof(T)), 0x00027000u};
+    const uint32_t lds = (uint32_t)uniform((int)(uint32_t)(uintptr_t)(lds_void*)(tile + wave * 1024));
+    const int step = W * EACH * pitch;
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %4 offen lds\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %5 offen lds" ::"s"(lds), "v"(off), "s"(r), "s"(step), "s"(2 * step), "s"(3 * step), "n"(W * 1024)
+        : "memory", "m0", "scc");
   }
 
   // A tile at key t0; at least STEPS copies a wave.
   template <bool FAST> static __device__ __forceinline__ void run(char* tile, const Rows<T>& rows, int t0, int end, int n, int wave, int lane) {
     if constexpr (FAST) {
+      if constexpr (COPIES == 4 * W && W * EACH % Tw::PERIOD == 0) {
+        if (t0 >= rows.past && t0 + KT <= end) return whole(tile, rows.own + (int64_t)(t0 - rows.past) * rows.own_stride, rows.own_stride, n, wave, lane);
+        if (t0 + KT <= rows.past) return whole(tile, rows.held + (int64_t)t0 * rows.held_stride, rows.held_stride, n, wave, lane);
+      }
       const int held = min(rows.past - t0, KT);                // keys of the tile that the cache holds: the others come from the call's own rows
       if (held > 0) straight(tile, rows.held + (int64_t)t0 * rows.held_stride, rows.held_stride, 0, held, n, wave, lane);
       if (held < KT) straight(tile, rows.own + (int64_t)(t0 - rows.past) * rows.own_stride, rows.own_stride, held, min(end - t0, KT), n, wave, lane);
@@ -211,20 +249,22 @@ template <typename T, int DB> struct Reader {
     }
   }
 
-  // S^T of 32 keys of a tile from key k0 (a multiple of 32) on: twists have a period of at most 32 keys
+  // A piece of the lane's key of 32 from key k0 (a multiple of 32) on: twists have a period of at most 32 keys
+  __device__ __forceinline__ v4u piece(const char* tile, int k0, int i) const { return *reinterpret_cast<const v4u*>(tile + (k ^ (i << 5)) + k0 * H::ROW); }
+
+  // S^T of 32 keys of a tile
   __device__ __forceinline__ v16f scores(const char* tile, int k0, const Query<T, DB>& q) const {
     // some pieces ahead of their products, and the next ones beside them
     constexpr int G = H::STEPS % 4 == 0 ? 4 : H::STEPS % 3 == 0 ? 3 : 2;
-    const auto piece = [&](int i) { return *reinterpret_cast<const v4u*>(tile + (k ^ (i << 5)) + k0 * H::ROW); };
     v16f s = {};
     v4u a[2][G];
 #pragma unroll
-    for (int i = 0; i < G; ++i) a[0][i] = piece(i);
+    for (int i = 0; i < G; ++i) a[0][i] = piece(tile, k0, i);
 #pragma unroll
     for (int g = 0; g < H::STEPS; g += G) {
       if (g + G < H::STEPS)
 #pragma unroll
-        for (int i = 0; i < G; ++i) a[g / G + 1 & 1][i] = piece(g + G + i);
+        for (int i = 0; i < G; ++i) a[g / G + 1 & 1][i] = piece(tile, k0, g + G + i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < G; ++i) s = mma_piece<T>(a[g / G & 1][i], q[g + i], s);
@@ -272,7 +312,46 @@ template <typename T, int DB> __device__ __forceinline__ bool clean(char* tile, 
   return found;
 }
 
-// The running softmax of a wave's rows: exponents of 2, the largest so far and the sum of the lane's half of the keys.
+// The weights of 32 keys, as operands of O^T.
+template <typename T> struct Weights {
+  static constexpr int N = 16 / Mma<T>::N;
+  typename Mma<T>::frag p[N];
+  __device__ __forceinline__ void set(int i, const v16f& s) {
+    if constexpr (Mma<T>::N == 1) p[i] = s[i];
+    else {
+      v4u w;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[x] = pack2(s[8 * i + 2 * x], s[8 * i + 2 * x + 1]);
+      p[i] = __builtin_bit_cast(v8bf, w);
+    }
+  }
+};
+
+// Scores of keys that the lane's row does not see: it sees lo ... hi - 1 of the 32.
+__device__ __forceinline__ void hide(v16f& s, int lo, int hi, int half) {
+  lo -= 4 * half;                              // so that the keys' numbers are constants
+  hi -= 4 * half;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int key = 8 * (i / 4) + i % 4;
+    s[i] = key >= lo && key < hi ? s[i] : -__builtin_inff();
+  }
+}
+
+// A lane's number and that of the lane 32 further, in both.
+struct Halves {
+  float a, b;
+  __device__ __forceinline__ explicit Halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    a = __uint_as_float(r[0]);
+    b = __uint_as_float(r[1]);
+  }
+};
+
+// The factor of sums whose base rises by -d: never 0, so that an infinite sum stays infinite.
+__device__ __forceinline__ float shrink(float d) { return fmaxf(__builtin_amdgcn_exp2f(d), 0x1p-126f); }
+
+// The running softmax of a wave's rows: exponents of 2, their base and the sum of the lane's half of the keys' weights.
 template <int DB> struct Running {
   v16f o[DB];
   float m, l;
@@ -283,85 +362,100 @@ template <int DB> struct Running {
     m = -__builtin_inff();
     l = 0.f;
   }
-};
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+  // The base for 32 more scores: it stays where it is until a weight would pass 2^8, then, row by row, the largest exponent
+  // becomes the base.  True: the row's sums have to be multiplied by `old` (l has been) before such weights are added.
+  // c: the scores' factor, log2(e) included.
+  __device__ __forceinline__ bool base_for(const v16f& s, float c, float& old) {
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    const Halves both(top);
+    top = fmaxf(both.a, both.b) * c;
+    const bool grows = top > m + 8.f;
+    old = grows ? shrink(m - top) : 1.f;
+    m = grows ? top : m;
+    l *= old;
+    return grows;
+  }
+  __device__ __forceinline__ void rescale(float old) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] *= old;
+  }
 
-// Takes KB times 32 keys of a tile into a wave's sums.  c: the scores' factor, log2(e) included.  hidden: some key is
-// hidden from some row, rows see keys lo ... hi - 1, counted from the tile's first.
-template <typename T, int DB, int KB>
-__device__ __forceinline__ void take(Running<DB>& run, v16f (&s)[KB], const Reader<T, DB>& read, const char* vtile, bool hidden, int lo, int hi, float c, int half) {
-  constexpr float LOWEST = -__builtin_inff();
-  if (hidden) {
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = 32 * b + 8 * (i / 4) + 4 * half + i % 4;
-        s[b][i] = key >= lo && key < hi ? s[b][i] : LOWEST;
-      }
-  }
-  float m = s[0][0];
-#pragma unroll
-  for (int b = 0; b < KB; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) m = fmaxf(m, s[b][i]);
-  m = fmaxf(m, other_half(m)) * c;
-  // The sums stay where they are until a weight would pass 2^8: then, row by row, the largest exponent becomes their base.
-  const bool grows = m > run.m + 8.f;
-  if (__any(grows)) {
-    const float old = grows ? __builtin_amdgcn_exp2f(run.m - m) : 1.f;
-    run.m = grows ? m : run.m;
-    run.l *= old;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) run.o[d] *= old;
-  }
-  const float base = run.m == LOWEST ? 0.f : run.m;            // nothing above -inf yet: every weight is 0
-  float l = 0.f;
-#pragma unroll
-  for (int b = 0; b < KB; ++b)
+  // The weights of 32 scores; nothing above -inf yet: every weight is 0.
+  __device__ __forceinline__ float weight(float s, float c, float base) { return __builtin_amdgcn_exp2f(fmaf(s, c, -base)); }
+  template <typename T> __device__ __forceinline__ Weights<T> weigh(v16f s, float c) {
+    const float base = m == -__builtin_inff() ? 0.f : m;
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -base));
-      l += s[b][i];
+      s[i] = weight(s[i], c, base);
+      sum += s[i];
     }
-  run.l += l;
-  constexpr int N = Mma<T>::N, STEPS = 16 / N;
-  typename Mma<T>::frag p[KB][STEPS];
+    l += sum;
+    Weights<T> w;
 #pragma unroll
-  for (int b = 0; b < KB; ++b)
+    for (int i = 0; i < Weights<T>::N; ++i) w.set(i, s);
+    return w;
+  }
+
+  // Adds the values of 32 keys of a tile from key k0 on.
+  template <typename T> __device__ __forceinline__ void add(const Reader<T, DB>& read, const char* tile, int k0, const Weights<T>& w) {
+    // some fragments ahead of their products, and the next ones beside them
+    constexpr int N = Weights<T>::N, G = N < 4 ? N : 4;
+    typename Mma<T>::frag v[2][G];
+    const auto fill = [&](int g) {
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      if constexpr (N == 1) p[b][st] = s[b][st];
-      else {
-        v4u w;
+      for (int i = 0; i < G; ++i) v[g & 1][i] = read.values(tile, k0, g * G % N + i, g * G / N);
+    };
+    fill(0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = f2bf2(s[b][8 * st + 2 * i], s[b][8 * st + 2 * i + 1]);
-        p[b][st] = __builtin_bit_cast(v8bf, w);
-      }
-    }
-  // fragments of one product ahead of the last one's
-  constexpr int G = KB * STEPS < 4 ? KB * STEPS : 4, GROUPS = KB * STEPS / G;
-  typename Mma<T>::frag v[2][G];
-  const auto fill = [&](int g) {
+    for (int g = 0; g < DB * N / G; ++g) {
+      if (g + 1 < DB * N / G) fill(g + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < G; ++i) {
-      const int x = g % GROUPS * G + i;
-      v[g & 1][i] = read.values(vtile, 32 * (x / STEPS), x % STEPS, g / GROUPS);
-    }
-  };
-  fill(0);
-#pragma unroll
-  for (int g = 0; g < DB * GROUPS; ++g) {
-    if (g + 1 < DB * GROUPS) fill(g + 1);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < G; ++i) {
-      const int x = g % GROUPS * G + i;
-      run.o[g / GROUPS] = Mma<T>::mma(v[g & 1][i], p[x / STEPS][x % STEPS], run.o[g / GROUPS]);
+      for (int i = 0; i < G; ++i) o[g * G / N] = Mma<T>::mma(v[g & 1][i], w.p[g * G % N + i], o[g * G / N]);
     }
   }
-}
+
+  // weigh of these scores, the next keys' scores and add of the last ones: after every product a share of the softmax, its
+  // operand read some products ahead.
+  template <typename T>
+  __device__ __forceinline__ void mixed(const v16f& s, float c, Weights<T>& mine, const Reader<T, DB>& read, const char* next, int next_at, const Query<T, DB>& q, v16f& after,
+                                        const char* last, int last_at, const Weights<T>& w) {
+    static_assert(sizeof(T) == 2, "");
+    constexpr int QK = Head<T, DB>::STEPS, PRODUCTS = 2 * QK, AHEAD = 3;
+    const float base = m == -__builtin_inff() ? 0.f : m;
+    v4u ring[AHEAD + 1];
+    const auto fetch = [&](int n) {
+      if (n < QK) ring[n % (AHEAD + 1)] = read.piece(next, next_at, n);
+      else if (n < PRODUCTS) ring[n % (AHEAD + 1)] = __builtin_bit_cast(v4u, read.values(last, last_at, (n - QK) % 2, (n - QK) / 2));
+    };
+    v16f p;
+    float sum = 0.f;
+    v4u packed[2];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) fetch(n);
+#pragma unroll
+    for (int n = 0; n < PRODUCTS; ++n) {
+      fetch(n + AHEAD);
+      const v8bf f = __builtin_bit_cast(v8bf, ring[n % (AHEAD + 1)]);
+      if (n < QK) after = Mma<T>::mma(f, __builtin_bit_cast(v8bf, q[n]), n ? after : v16f{});
+      else o[(n - QK) / 2] = Mma<T>::mma(f, w.p[(n - QK) % 2], o[(n - QK) / 2]);
+#pragma unroll
+      for (int i = n * 16 / PRODUCTS; i < (n + 1) * 16 / PRODUCTS; ++i) {
+        p[i] = weight(s[i], c, base);
+        sum += p[i];
+        if (i & 1) packed[i / 8][i / 2 % 4] = pack2(p[i - 1], p[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l += sum;
+    mine.p[0] = __builtin_bit_cast(v8bf, packed[0]);
+    mine.p[1] = __builtin_bit_cast(v8bf, packed[1]);
+  }
+};
 
 // 64 bytes of the summed axis of 16 x 16 results, a lane's piece being a quarter of them: one instruction, or in float32 four.
 template <typename T> __device__ __forceinline__ v4f mma16_part(v4u a, v4u b, int e, v4f c) {
@@ -381,7 +475,7 @@ template <typename T> __device__ __forceinline__ void store4(T* p, int c, int n,
     if constexpr (sizeof(T) == 2) {
       typedef uint32_t v2u __attribute__((ext_vector_type(2)));
       typedef v2u __attribute__((aligned(2))) any;
-      *reinterpret_cast<any*>(p + c) = v2u{f2bf2(a, b), f2bf2(d, e)};
+      *reinterpret_cast<any*>(p + c) = v2u{pack2(a, b), pack2(d, e)};
     } else {
       typedef v4f __attribute__((aligned(4))) any;
       *reinterpret_cast<any*>(p + c) = v4f{a, b, d, e};

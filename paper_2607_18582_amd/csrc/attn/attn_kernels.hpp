@@ -67,12 +67,17 @@ __device__ __forceinline__ SeqItem item_of(const AttnArgs& k, int i) {
 __device__ __forceinline__ int spread(int i, int n) { return n % 8 ? i : i % 8 * (n / 8) + i / 8; }
 
 // ---- runs of tokens: one head, 128 tokens, 32 of them a wave; tiles of keys and values in LDS, two at a time
+//
+// Every 32 keys cost a wave as many cycles of matrix instructions as of others (an exponential, a multiply-add, a sum and
+// half a maximum and a conversion per score).  Two waves on a SIMD overlap them by a fifth only, so a wave does it itself:
+// the softmax of one block goes between the products of the next and of the last one.
 
 template <typename T, int DB> struct Run {
   using H = Head<T, DB>;
   static constexpr int KT = H::ROW <= 256 ? 64 : 32;           // keys of a tile
   static constexpr int TILE = KT * H::ROW;
-  static constexpr int LDS = 4 * TILE;
+  static constexpr int LDS = 4 * TILE;         // keys twice, values twice
+  static constexpr bool MIXED = sizeof(T) == 2 && DB <= 4;     // float32 is bound by its matrix instructions anyway
 };
 
 template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <= 4 ? 2 : 1) void run_kernel(AttnArgs k) {
@@ -105,11 +110,12 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   const int row = wave * 32 + (lane & 31), pos = min(first + row, last);
   int lo, hi;
   sees(a, pos, src.total, lo, hi);
-  // ... that any row of the wave sees
-  int any_lo, any_hi;
-  sees(a, min(first + wave * 32, last), src.total, any_lo, none);
-  sees(a, min(first + wave * 32 + 31, last), src.total, none, any_hi);
-  const bool idle = wave * 32 >= it.len;
+  // ... that any row of the wave sees, and that all of them see
+  int any_lo, any_hi, wave_lo, wave_hi;
+  sees(a, min(first + wave * 32, last), src.total, any_lo, wave_hi);
+  sees(a, min(first + wave * 32 + 31, last), src.total, wave_lo, any_hi);
+  wave_lo = max(wave_lo, from);
+  wave_hi = min(wave_hi, to);
   Query<T, DB> q;
   load_query<T, Head<T, DB>::STEPS, 2>(q, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)(pos - first)) * a.q.row_stride + (int64_t)h * a.head_dim,
                     a.head_dim, half, a.scale);
@@ -117,40 +123,114 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   Running<DB> run;
   run.start();
   const Reader<T, DB> read(lane);
-  auto load = [&](int t, int buffer) {
-    char* tile = lds + buffer * 2 * R::TILE;
-    Copy<T, DB, KT, 4, KEYS>::template run<FAST>(tile, src.k, t, src.total, a.head_dim, wave, lane);
-    Copy<T, DB, KT, 4, VALUES32>::template run<FAST>(tile + R::TILE, src.v, t, src.total, a.head_dim, wave, lane);
+  using Keys = Copy<T, DB, KT, 4, KEYS>;
+  using Values = Copy<T, DB, KT, 4, VALUES32>;
+  const int t0 = from / KT * KT, tiles = (to - t0 + KT - 1) / KT;
+  const auto k_tile = [&](int i) { return lds + (i & 1) * R::TILE; };
+  const auto v_tile = [&](int i) { return lds + (2 + (i & 1)) * R::TILE; };
+  const auto load_k = [&](int i) { Keys::template run<FAST>(k_tile(i), src.k, t0 + i * KT, src.total, a.head_dim, wave, lane); };
+  const auto load_v = [&](int i) { Values::template run<FAST>(v_tile(i), src.v, t0 + i * KT, src.total, a.head_dim, wave, lane); };
+  // Blocks of 32 keys, numbered from t0 on, of which the wave's rows see any: begin ... end - 1.
+  const int begin = wave * 32 >= it.len ? 0 : (max(any_lo, from) - t0) / 32, end = wave * 32 >= it.len ? 0 : (min(any_hi, to) - t0 + 31) / 32;
+  const auto seen = [&](int j) { return j >= begin && j < end; };
+  // Scores of the block that is next and weights of the one before it, for even blocks and odd ones.
+  v16f s[2] = {};
+  Weights<T> w[2];
+  // One step: the last block's values, the softmax of block j, the next block's scores.
+  const auto step = [&](int j, v16f& mine, v16f& after, Weights<T>& before, Weights<T>& weights, const char* next, int next_at, const char* last, int last_at) {
+    const int t = t0 + 32 * j;
+    if (seen(j - 1)) run.template add<T>(read, last, last_at, before);
+    if (seen(j)) {
+      if (t < wave_lo || t + 32 > wave_hi) hide(mine, max(lo, from) - t, min(hi, to) - t, half);
+      float old;
+      if (__any(run.base_for(mine, c, old))) run.rescale(old);
+      weights = run.template weigh<T>(mine, c);
+    }
+    if (seen(j + 1)) after = read.scores(next, next_at, q);
   };
-  int t = from / KT * KT, buffer = 0;
-  load(t, 0);
-  for (; t < to; t += KT, buffer ^= 1) {
-    wait_copies();
-    __syncthreads();                           // the tile is there, and the last one has been used
-    if (t + KT < to) load(t + KT, buffer ^ 1);
-    char* tile = lds + buffer * 2 * R::TILE;
-    // Keys hidden from some row of the block are those before and behind what all of them see, of the part.
-    const int see_from = max(block_lo, from) - t, see_to = min(block_hi, to) - t, there = min(KT, src.total - t);
-    const bool hidden = see_from > 0 || see_to < KT, some = see_from > 0 || see_to < there;
-    bool apart = false;                        // a hidden one's value is not finite
-    if (some) {
-      const bool before = clean<T, DB>(tile + R::TILE, 0, min(see_from, there), tid, 256), behind = clean<T, DB>(tile + R::TILE, max(0, see_to), there, tid, 256);
-      apart = __syncthreads_or(before || behind);
-    }
-    if (idle || t >= any_hi || t + KT <= any_lo) continue;
-    v16f s[KB];
-#pragma unroll
-    for (int b = 0; b < KB; ++b) s[b] = read.scores(tile, 32 * b, q);
+  // The same with the products between the parts of the softmax, so that the matrix units and the others are busy at once,
+  // where all rows of the wave see the three blocks.
+  const auto mixed = [&](const v16f& mine, v16f& after, const Weights<T>& before, Weights<T>& weights, const char* next, int next_at, const char* last, int last_at) {
+    float old;
+    const bool grows = run.base_for(mine, c, old);
+    if constexpr (R::MIXED) run.template mixed<T>(mine, c, weights, read, next, next_at, q, after, last, last_at, before);
+    if (__any(grows)) run.rescale(old);
+  };
+  const auto aside = [&](int i) {              // whether values of tile i are hidden from some row of the block
+    const int t = t0 + i * KT;
+    return max(block_lo, from) > t || min(block_hi, to) < min(t + KT, src.total);
+  };
+  // Values of tile i that are not finite in places hidden from some row are put aside; its other rows get them here.
+  const auto put_aside = [&](int i) {
+    if (!aside(i)) return;
+    const int t = t0 + i * KT, see_from = max(block_lo, from) - t, see_to = min(block_hi, to) - t, there = min(KT, src.total - t);
+    char* tile = v_tile(i);
+    const bool before = clean<T, DB>(tile, 0, min(see_from, there), tid, 256), behind = clean<T, DB>(tile, max(0, see_to), there, tid, 256);
+    if (!__syncthreads_or(before || behind) || begin >= end) return;
+    auto add = [&](int x, float v) { run.o[x / 16][x % 16] += v; };
     const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
-    take<T, DB, KB>(run, s, read, tile + R::TILE, hidden, row_lo, row_hi, c, half);
-    if (apart) {
-      auto add = [&](int i, float v) { run.o[i / 16][i % 16] += v; };
-      add_nonfinite<16 * DB>(src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
-      add_nonfinite<16 * DB>(src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
+    add_nonfinite<16 * DB>(src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
+    add_nonfinite<16 * DB>(src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
+  };
+  load_k(0);
+  if (KB == 2) load_v(0);
+  if (tiles > 1) load_k(1);
+  wait_copies();
+  __syncthreads();
+  if (seen(0)) s[0] = read.scores(k_tile(0), 0, q);
+  if constexpr (KB == 2) {
+    // Tile i's first block reads the second one's keys and the last tile's second values; its second block the next
+    // tile's first keys and its own first values.  In between, the places of this tile's keys and the last one's values
+    // are free.
+    const auto middle = [&](int i) {
+      wait_copies();
+      __syncthreads();
+      if (i + 2 < tiles) load_k(i + 2);
+      if (i + 1 < tiles) load_v(i + 1);
+    };
+    const auto careful = [&](int i) {
+      step(2 * i, s[0], s[1], w[1], w[0], k_tile(i), 32, v_tile(i - 1), 32);
+      middle(i);
+      put_aside(i);
+      step(2 * i + 1, s[1], s[0], w[0], w[1], k_tile(i + 1), 0, v_tile(i), 0);
+    };
+    // Tiles in which all rows of the wave see all keys, and so in the blocks beside them, and none of whose values is to be
+    // put aside: clear ... cloudy - 1.
+    const int see_from = max(block_lo, from), see_to = min(block_hi, to);
+    int clear = max(begin / 2 + 1, (max(wave_lo, see_from) - t0 + KT - 1) / KT);
+    int cloudy = min(min((end - 1) / 2, (wave_hi - t0) / KT), see_to >= src.total ? tiles : (see_to - t0) / KT);
+    if (!R::MIXED || begin >= end || clear >= cloudy) clear = cloudy = tiles;
+    int i = 0;
+    for (; i < clear; ++i) careful(i);
+    if constexpr (R::MIXED) {
+      for (; i < cloudy; ++i) {
+        mixed(s[0], s[1], w[1], w[0], k_tile(i), 32, v_tile(i - 1), 32);
+        middle(i);
+        mixed(s[1], s[0], w[0], w[1], k_tile(i + 1), 0, v_tile(i), 0);
+      }
+      for (; i < tiles; ++i) careful(i);
     }
+    if (seen(2 * tiles - 1)) run.template add<T>(read, v_tile(tiles - 1), 32, w[1]);
+  } else {
+    // Block i reads the next tile's keys and the last one's values; this tile's keys and the values before are done with.
+    for (int i = 0; i < tiles; ++i) {
+      wait_copies();
+      __syncthreads();
+      if (i + 2 < tiles) load_k(i + 2);
+      load_v(i);
+      if (i) put_aside(i - 1);
+      step(i, s[0], s[1], w[0], w[1], k_tile(i + 1), 0, v_tile(i - 1), 0);
+      s[0] = s[1];
+      w[0] = w[1];
+    }
+    wait_copies();
+    __syncthreads();
+    put_aside(tiles - 1);
+    if (seen(tiles - 1)) run.template add<T>(read, v_tile(tiles - 1), 0, w[0]);
   }
   if (row >= it.len) return;
-  const float l = run.l + other_half(run.l);
+  const Halves both(run.l);
+  const float l = both.a + both.b;
   if (k.parts > 1) {
     const int64_t at_row = (((int64_t)m * k.n_items + i) * k.rows_each + row) * a.heads + h, slot = at_row * k.parts + part;
     store_row<float, DB>(k.ws_o + slot * a.head_dim, a.head_dim, run.o, 1.f, half);
@@ -242,7 +322,7 @@ template <typename T, int DB, bool FAST> struct ShortWave {
       most = fmaxf(most, __shfl_xor(most, 32)) * c;
       const bool grows = most > top + 8.f;
       if (__any(grows)) {
-        const float old = grows ? __builtin_amdgcn_exp2f(top - most) : 1.f;
+        const float old = grows ? shrink(top - most) : 1.f;
         top = grows ? most : top;
         l *= old;
 #pragma unroll
@@ -268,7 +348,7 @@ template <typename T, int DB, bool FAST> struct ShortWave {
       if constexpr (sizeof(T) == 2) {
         v4u w;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) w[x] = f2bf2(s[x / 2][2 * (x & 1)], s[x / 2][2 * (x & 1) + 1]);
+        for (int x = 0; x < 4; ++x) w[x] = pack2(s[x / 2][2 * (x & 1)], s[x / 2][2 * (x & 1) + 1]);
         const v8bf p = __builtin_bit_cast(v8bf, w);
         const int key = 4 * quarter + (lane & 15) / 4, twist = Twist<T, H::PIECES, VALUES16>::of(key);       // and key + 16
         const int v = key * H::ROW + ((((lane & 3) >> 1) ^ twist) << 4) + (lane & 1) * 8;

@@ -445,9 +445,15 @@ template <int DB> struct Running {
       else o[(n - QK) / 2] = Mma<T>::mma(f, w.p[(n - QK) % 2], o[(n - QK) / 2]);
 #pragma unroll
       for (int i = n * 16 / PRODUCTS; i < (n + 1) * 16 / PRODUCTS; ++i) {
-        p[i] = weight(s[i], c, base);
-        sum += p[i];
-        if (i & 1) packed[i / 8][i / 2 % 4] = pack2(p[i - 1], p[i]);
+        float x = weight(s[i], c, base);
+        sum += x;
+        asm volatile("" : "+v"(x), "+v"(sum));                 // here, not where the weights are needed
+        p[i] = x;
+        if (i & 1) {
+          uint32_t pair = pack2(p[i - 1], x);
+          asm volatile("" : "+v"(pair));
+          packed[i / 8][i / 2 % 4] = pair;
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }

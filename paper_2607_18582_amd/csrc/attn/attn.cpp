@@ -148,6 +148,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   const int64_t parts_mid = held ? (a.capacity + ATTN_KEYS_MID - 1) / ATTN_KEYS_MID : 1;
   if ((wide)a.heads * M * std::max(std::max(parts_short * ATTN_SHORT, parts_mid), (int64_t)ATTN_WHOLE_F32) > GRID)
     throw Fail{MURE_E_UNSUPPORTED, "too many heads times mutants times parts of the cache"};
+  if ((wide)M * s->n_brief > INT32_MAX || (wide)M * s->n_runs > INT32_MAX) throw Fail{MURE_E_UNSUPPORTED, "too many sequences times mutants"};
   check_device(s->device);
   if (T == 0) return;
   k.fast = D * es % 16 == 0 && pieces(a.k.p, es, {a.k.row_stride, a.k.mutant_stride}) && pieces(a.v.p, es, {a.v.row_stride, a.v.mutant_stride}) &&

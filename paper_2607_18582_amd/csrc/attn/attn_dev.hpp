@@ -107,13 +107,17 @@ template <typename T> __device__ __forceinline__ v4u load_piece(const T* p, int 
 
 // 16 bytes a lane from `off` on of a buffer of `bytes` bytes at p (zeros behind it) to `to`, one lane after the other.  As the
 // compiler's builtin every later read of LDS would wait for it; this one only wait_copies waits for.  The wait states are
-// those between a scalar's write by the vector unit, or m0's, and its use here.
+// those between a scalar's write by the vector unit, or m0's, and its use here.  Nothing else in these kernels uses m0, so
+// the warning that the compiler need not keep it is moot.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy16(const void* p, int bytes, unsigned off, char* to) {
   const uint64_t at = (uint64_t)p;
   const v4u r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)bytes, 0x00027000u};
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)to;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform((int)lds)), "v"(off), "s"(r) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Copies of KT keys' rows into a tile by W waves, 1024 bytes a wave and step.
 template <typename T, int DB, int KT, int W, Reads R> struct Copy {

@@ -478,11 +478,12 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, (Shor
 
 // ---- the parts' results of one token and head: every 16th part in order, then the 16 sums in order
 
-template <typename T> __global__ __launch_bounds__(1024) void join_kernel(AttnArgs k, int keys) {
+template <typename T> __global__ __launch_bounds__(1024) void join_kernel(AttnArgs k, int keys, int64_t first_row) {
   __shared__ float sums[16][MURE_ATTN_MAX_HEAD], sizes[16];
   const mure_attn_attend_args& a = k.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const int rows = a.heads * k.rows_each, im = uniform(blockIdx.x / rows), x = blockIdx.x - im * rows, row = uniform(x / a.heads), h = x - row * a.heads;
+  const int64_t at = first_row + blockIdx.x;
+  const int rows = a.heads * k.rows_each, im = uniform((int)(at / rows)), x = (int)(at - (int64_t)im * rows), row = uniform(x / a.heads), h = x - row * a.heads;
   const int m = uniform(im / k.n_items), i = im - m * k.n_items;
   const SeqItem it = item_of(k, i);
   if (row >= it.len) return;
@@ -491,8 +492,8 @@ template <typename T> __global__ __launch_bounds__(1024) void join_kernel(AttnAr
   int lo, hi;
   sees(a, past + it.pos0 + row, past + it.total, lo, hi);
   const int first = lo / keys, last = (hi - 1) / keys;         // the parts with keys that the row sees
-  const float* ml = k.ws_ml + 2 * (int64_t)blockIdx.x * k.parts;
-  const float* o = k.ws_o + (int64_t)blockIdx.x * k.parts * a.head_dim;
+  const float* ml = k.ws_ml + 2 * at * k.parts;
+  const float* o = k.ws_o + at * k.parts * a.head_dim;
   float top = -__builtin_inff();
   for (int p = first + lane; p <= last; p += 64) top = fmaxf(top, ml[2 * p]);
   for (int w = 1; w < 64; w *= 2) top = fmaxf(top, __shfl_xor(top, w));
@@ -579,8 +580,10 @@ template <typename T> hipError_t join(AttnArgs k, int keys, hipStream_t s) {
   const int64_t rows = (int64_t)k.rows_each * k.a.heads, blocks = (int64_t)k.a.n_mutants * k.n_items * rows;
   // few rows get a wave for every 16th part; otherwise the waves take several each
   const unsigned threads = blocks < 512 && k.parts > 16 ? 1024 : 256;
-  if (blocks > ((int64_t)1 << 32) / threads - 1) return hipErrorInvalidConfiguration;
-  return launch(join_kernel<T>, dim3((unsigned)blocks), threads, s, k, keys);
+  const int64_t most = ((int64_t)1 << 32) / threads - 1;
+  for (int64_t first = 0; first < blocks; first += most)
+    if (const hipError_t e = launch(join_kernel<T>, dim3((unsigned)std::min(most, blocks - first)), threads, s, k, keys, first); e != hipSuccess) return e;
+  return hipSuccess;
 }
 
 }  // namespace mure

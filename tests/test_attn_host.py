@@ -1,0 +1,359 @@
+"""The operators of an attention block (include/mure_attn.h) on the host: the
+library exports what the header declares, and every invalid call is refused
+with its reason before any device work (planning-only contexts: a valid call
+ends in MURE_E_UNSUPPORTED)."""
+import ctypes as C
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+import torch.autograd.forward_ad as fwd
+
+from paper_2607_18582_amd import MURE_E_INVALID, MURE_E_UNSUPPORTED, Mure, MureError, load_library
+from paper_2607_18582_amd import attn as A
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+class Rows(C.Structure):                       # mure_seq_in, mure_seq_out
+    _fields_ = [("p", C.c_void_p), ("mutant_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class Param(C.Structure):                      # mure_seq_param
+    _fields_ = [("p", C.c_void_p), ("mutant_stride", C.c_int64)]
+
+
+class Cache(C.Structure):                      # mure_attn_cache
+    _fields_ = [("p", C.c_void_p), ("mutant_stride", C.c_int64), ("seq_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class mure_attn_rotate_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_mutants", "q_heads", "k_heads", "head_dim", "rotated", "norm", "interleaved", "axes")] + \
+               [("section", C.c_int32 * 4), ("eps", C.c_float), ("q", Rows), ("k", Rows), ("q_weight", Param), ("k_weight", Param),
+                ("frequencies", Param), ("positions", C.c_void_p), ("past", C.c_void_p), ("q_out", Rows), ("k_out", Rows)]
+
+
+class mure_attn_attend_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_mutants", "heads", "kv_heads", "head_dim", "causal")] + \
+               [("window", C.c_int64), ("scale", C.c_float), ("reserved", C.c_int32), ("q", Rows), ("k", Rows), ("v", Rows),
+                ("k_cache", Cache), ("v_cache", Cache), ("capacity", C.c_int64), ("past", C.c_void_p), ("out", Rows)]
+
+
+class mure_attn_gated_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_mutants", "inner", "outer", "activation", "reserved")] + \
+               [("rows", C.c_int64), ("x", Rows), ("gate", Rows), ("up", Rows), ("gate_bias", Param), ("up_bias", Param), ("out", Rows)]
+
+
+@pytest.fixture()
+def mure():
+    m = Mure(device=-1)
+    yield m
+    m.close()
+
+
+def test_library_exports_every_declared_symbol():
+    with open(os.path.join(ROOT, "include", "mure_attn.h")) as f:
+        declared = set(re.findall(r"\b(mure_attn_[a-z]+)\(", f.read()))
+    assert declared == set(A.ATTN_EXPORTED)
+    lib = load_library()
+    for name in declared:
+        assert hasattr(lib, name), name
+    assert lib.mure_attn_version() == A.ATTN_VERSION
+
+
+def test_structures_match_the_header(tmp_path):
+    lines, expected = [], []
+    for t in (mure_attn_rotate_args, mure_attn_attend_args, mure_attn_gated_args):
+        lines.append(f'printf("%zu\\n", sizeof({t.__name__}));')
+        expected.append(C.sizeof(t))
+        for name, _ in t._fields_:
+            lines.append(f'printf("%zu\\n", offsetof({t.__name__}, {name}));')
+            expected.append(getattr(t, name).offset)
+    src = tmp_path / "layout.c"
+    src.write_text("#include <stddef.h>\n#include <stdio.h>\n#include <mure_attn.h>\nint main(void) {\n" + "\n".join(lines) + "\nreturn 0; }\n")
+    exe = str(tmp_path / "layout")
+    subprocess.run(["gcc", "-I" + os.path.join(ROOT, "include"), str(src), "-o", exe], check=True)
+    assert [int(v) for v in subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()] == expected
+
+
+# ---- the C interface's own checks
+
+T, H, G, D, CAP = 7, 4, 2, 8, 32
+
+
+class Buffers:
+    """Host memory that stands for device memory: nothing reads it."""
+
+    def __init__(self):
+        self.keep = []
+
+    def __call__(self, n=65536):
+        b = (C.c_char * n)()
+        self.keep.append(b)
+        return C.addressof(b) + -C.addressof(b) % 16
+
+
+def rotate_args(m):
+    a = mure_attn_rotate_args(dtype=0, n_mutants=2, q_heads=H, k_heads=G, head_dim=D, rotated=6, norm=1, interleaved=0, eps=1e-5)
+    a.q, a.k = Rows(m(), T * H * D, H * D), Rows(m(), 0, G * D)
+    a.q_weight, a.k_weight, a.frequencies = Param(m(), D), Param(m(), 0), Param(m(), 0)
+    a.past = m()
+    a.q_out, a.k_out = Rows(m(), T * H * D, H * D), Rows(m(), T * G * D, G * D)
+    return a
+
+
+def attend_args(m):
+    a = mure_attn_attend_args(dtype=1, n_mutants=2, heads=H, kv_heads=G, head_dim=D, causal=1, window=0, scale=0.3, capacity=CAP)
+    a.q, a.k, a.v = Rows(m(), T * H * D, H * D), Rows(m(), T * G * D, G * D), Rows(m(), T * G * D, G * D)
+    a.k_cache, a.v_cache = (Cache(m(), 3 * CAP * G * D, CAP * G * D, G * D) for _ in range(2))
+    a.past = m()
+    a.out = Rows(m(), T * H * D, H * D)
+    return a
+
+
+def gated_args(m):
+    a = mure_attn_gated_args(dtype=1, n_mutants=2, inner=12, outer=10, activation=4, rows=T)
+    a.x = Rows(m(), 0, 12)
+    a.gate, a.up = Rows(m(), 120, 12), Rows(m(), 0, 12)
+    a.gate_bias, a.up_bias = Param(m(), 10), Param(m(), 0)
+    a.out = Rows(m(), T * 10, 10)
+    return a
+
+
+def put(a, path, value):
+    *way, last = path.split(".")
+    for w in way:
+        a = getattr(a, w)
+    setattr(a, last, value)
+
+
+def call(mure, op, args):
+    if op == "gated":
+        st = mure.lib.mure_attn_gated(mure.ctx, C.byref(args))
+    else:
+        seqs = mure.sequences([4, 0, 3])
+        st = (mure.lib.mure_attn_rotate if op == "rotate" else mure.lib.mure_attn_attend)(seqs.handle, C.byref(args))
+    return st, mure.lib.mure_last_error(mure.ctx).decode()
+
+
+MAKE = {"rotate": rotate_args, "attend": attend_args, "gated": gated_args}
+
+
+@pytest.mark.parametrize("op", list(MAKE))
+def test_valid_arguments_reach_the_device(mure, op):
+    st, msg = call(mure, op, MAKE[op](Buffers()))
+    assert st == MURE_E_UNSUPPORTED and "planning-only" in msg
+
+
+@pytest.mark.parametrize("op,path,value,word", [
+    ("rotate", "dtype", 2, "unknown type"), ("rotate", "n_mutants", 0, "n_mutants"), ("rotate", "n_mutants", 65536, "n_mutants"),
+    ("rotate", "q_heads", 0, "q_heads"), ("rotate", "q_heads", 1025, "q_heads"), ("rotate", "k_heads", -1, "k_heads"),
+    ("rotate", "head_dim", 0, "head_dim"), ("rotate", "head_dim", 257, "head_dim"), ("rotate", "rotated", 5, "odd"),
+    ("rotate", "rotated", 10, "rotated"), ("rotate", "rotated", -2, "rotated"), ("rotate", "norm", 3, "norm"),
+    ("rotate", "norm", 0, "weight without"), ("rotate", "interleaved", 2, "interleaved"), ("rotate", "eps", float("nan"), "eps"),
+    ("rotate", "eps", -1.0, "eps"), ("rotate", "frequencies.p", None, "frequencies is NULL"), ("rotate", "q.p", None, "q is NULL"),
+    ("rotate", "k.p", None, "k is NULL"), ("rotate", "q_out.p", None, "q_out is NULL"), ("rotate", "q.row_stride", -1, "negative"),
+    ("rotate", "q_out.row_stride", H * D - 1, "rows overlap"), ("rotate", "k_out.mutant_stride", 0, "rows overlap"),
+    ("attend", "dtype", -1, "unknown type"), ("attend", "n_mutants", 0, "n_mutants"), ("attend", "heads", 3, "multiple"),
+    ("attend", "kv_heads", 0, "kv_heads"), ("attend", "kv_heads", 5, "kv_heads"), ("attend", "head_dim", 300, "head_dim"),
+    ("attend", "causal", 2, "causal"), ("attend", "window", -1, "window"), ("attend", "scale", float("inf"), "scale"),
+    ("attend", "reserved", 1, "reserved"), ("attend", "v_cache.p", None, "go together"), ("attend", "capacity", 0, "capacity"),
+    ("attend", "capacity", 1 << 31, "capacity"), ("attend", "k_cache.row_stride", G * D - 1, "overlap"),
+    ("attend", "k_cache.seq_stride", CAP * G * D - 1, "overlap"), ("attend", "k_cache.seq_stride", -1, "negative"),
+    ("attend", "v_cache.mutant_stride", 3, "overlap"), ("attend", "k_cache.mutant_stride", 0, "share"), ("attend", "q.p", None, "q is NULL"),
+    ("attend", "v.p", None, "v is NULL"), ("attend", "out.p", None, "out is NULL"), ("attend", "out.mutant_stride", 0, "rows overlap"),
+    ("gated", "dtype", 7, "unknown type"), ("gated", "inner", 0, "inner"), ("gated", "outer", (1 << 20) + 1, "outer"),
+    ("gated", "rows", -1, "rows"), ("gated", "activation", 6, "activation"), ("gated", "reserved", 1, "reserved"),
+    ("gated", "gate.p", None, "gate is NULL"), ("gated", "up.p", None, "up is NULL"), ("gated", "x.p", None, "x is NULL"),
+    ("gated", "out.row_stride", 9, "rows overlap"), ("gated", "gate.row_stride", 1 << 61, "address space"), ("gated", "x.row_stride", -2, "negative")])
+def test_invalid_arguments(mure, op, path, value, word):
+    a = MAKE[op](Buffers())
+    put(a, path, value)
+    st, msg = call(mure, op, a)
+    assert st == MURE_E_INVALID and word in msg, (st, msg)
+
+
+@pytest.mark.parametrize("op,out,other", [("rotate", "q_out", "k"), ("rotate", "k_out", "q"), ("rotate", "q_out", "frequencies"), ("rotate", "k_out", "q_out"),
+                                          ("rotate", "q_out", "past"), ("attend", "out", "q"), ("attend", "out", "v"), ("attend", "out", "past"),
+                                          ("attend", "out", "k_cache"), ("attend", "k_cache", "k"), ("attend", "v_cache", "q"),
+                                          ("attend", "v_cache", "k_cache"), ("attend", "k_cache", "past"), ("gated", "out", "x"), ("gated", "out", "gate"),
+                                          ("gated", "out", "up_bias")])
+def test_overlaps(mure, op, out, other):
+    a = MAKE[op](Buffers())
+    o = getattr(a, other)
+    put(a, out + ".p", (o if isinstance(o, int) else o.p) + 8)
+    st, msg = call(mure, op, a)
+    assert st == MURE_E_INVALID and "overlap" in msg, msg
+
+
+def test_results_in_place_of_their_inputs(mure):
+    a = rotate_args(Buffers())
+    a.q_out = a.q
+    st, msg = call(mure, "rotate", a)
+    assert st == MURE_E_UNSUPPORTED, msg
+    a.k_out = a.k                              # which all mutants share
+    st, msg = call(mure, "rotate", a)
+    assert st == MURE_E_INVALID and "overlap" in msg
+
+
+def test_caches_beside_each_other(mure):
+    """Keys and values as the columns of one buffer's rows, and mutants that share all of it."""
+    a = attend_args(Buffers())
+    p = a.k_cache.p
+    a.k_cache = Cache(p, 3 * CAP * 2 * G * D, CAP * 2 * G * D, 2 * G * D)
+    a.v_cache = Cache(p + 2 * G * D, 3 * CAP * 2 * G * D, CAP * 2 * G * D, 2 * G * D)
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_UNSUPPORTED and "planning-only" in msg, msg
+    a.v_cache.p = p + 2 * G * D - 2
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_INVALID and "overlaps" in msg
+    a = attend_args(Buffers())
+    for x in (a.k, a.v, a.k_cache, a.v_cache):
+        x.mutant_stride = 0
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_UNSUPPORTED and "planning-only" in msg, msg
+
+
+def test_positions(mure):
+    m = Buffers()
+    a = rotate_args(m)
+    a.positions, a.axes, a.section = m(), 2, (C.c_int32 * 4)(1, 2, 0, 0)
+    st, msg = call(mure, "rotate", a)
+    assert st == MURE_E_INVALID and "exclude" in msg
+    a.past = None
+    st, msg = call(mure, "rotate", a)
+    assert st == MURE_E_UNSUPPORTED, msg
+    for axes, section, word in ((2, (1, 1, 0, 0), "sections"), (5, (1, 2, 0, 0), "axes"), (0, (0, 0, 0, 0), "axes"), (2, (-1, 4, 0, 0), "section")):
+        a.axes, a.section = axes, (C.c_int32 * 4)(*section)
+        st, msg = call(mure, "rotate", a)
+        assert st == MURE_E_INVALID and word in msg
+
+
+def test_past_needs_caches(mure):
+    a = attend_args(Buffers())
+    a.k_cache = a.v_cache = Cache()
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_INVALID and "past" in msg
+    a.past = None
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_UNSUPPORTED and "planning-only" in msg
+
+
+def test_too_many_blocks(mure):
+    a = attend_args(Buffers())
+    a.capacity, a.n_mutants = (1 << 31) - 1, 1
+    for c in (a.k_cache, a.v_cache):
+        c.seq_stride = a.capacity * G * D
+    a.v_cache.p = a.k_cache.p + 3 * 2 * a.capacity * G * D
+    for name in ("q", "k", "v", "past", "out"):                              # nothing is read there
+        o = a.v_cache.p + (1 << 40)
+        put(a, name if name == "past" else name + ".p", o + ["q", "k", "v", "past", "out"].index(name) * (1 << 20))
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_UNSUPPORTED and "too many" in msg
+
+
+def test_null_handles():
+    lib = load_library()
+    assert lib.mure_attn_rotate(None, C.byref(mure_attn_rotate_args())) == MURE_E_INVALID
+    assert lib.mure_attn_attend(None, C.byref(mure_attn_attend_args())) == MURE_E_INVALID
+    assert lib.mure_attn_gated(None, C.byref(mure_attn_gated_args())) == MURE_E_INVALID
+    m = Mure(device=-1)
+    assert lib.mure_attn_gated(m.ctx, None) == MURE_E_INVALID
+    assert lib.mure_attn_attend(m.sequences([1]).handle, None) == MURE_E_INVALID
+    m.close()
+
+
+# ---- the binding's
+
+def ones(*s, **k):
+    return torch.ones(*s, **k)
+
+
+def test_valid_calls_end_at_the_device(mure):
+    s = mure.sequences([4, 3])
+    f, p = ones(4), torch.zeros(2, dtype=torch.int32)
+    cache = (ones(2, 9, 16), ones(2, 9, 16))
+    for call_ in (lambda: s.rotate(ones(7, 32), ones(7, 16), f, head_dim=8), lambda: s.rotate(ones(3, 7, 32), None, f, head_dim=8, norm="rms", q_weight=ones(8)),
+                  lambda: s.rotate(ones(7, 32), None, f, head_dim=8, positions=torch.zeros(2, 7, dtype=torch.int32), sections=[1, 3]),
+                  lambda: s.attend(ones(7, 32), ones(7, 16), ones(7, 16), head_dim=8), lambda: s.attend(ones(7, 32), ones(7, 16), ones(7, 16), head_dim=8, cache=cache, past=p),
+                  lambda: s.attend(ones(5, 7, 32), ones(7, 16), ones(7, 16), head_dim=8, cache=cache, past=p, window=3, causal=False, scale=1),
+                  lambda: mure.gated(ones(7, 8), ones(6, 8), ones(6, 8)), lambda: mure.gated(ones(2, 7, 8), ones(6, 8), ones(2, 6, 8), gate_bias=ones(6), activation="gelu")):
+        with pytest.raises(MureError, match="planning-only"):
+            call_()
+
+
+def refused(kind, word, call_):
+    with pytest.raises(kind, match=word):
+        call_()
+
+
+def test_invalid_calls(mure):
+    s = mure.sequences([4, 3])
+    q, k, f, p = ones(7, 32), ones(7, 16), ones(4), torch.zeros(2, dtype=torch.int32)
+    at = torch.zeros(1, 7, dtype=torch.int32)
+    cache = (ones(2, 9, 16), ones(2, 9, 16))
+    refused(ValueError, "multiple of head_dim", lambda: s.rotate(q, k, f, head_dim=5))
+    refused(ValueError, "multiple of head_dim", lambda: s.rotate(q, k, f, head_dim=0))
+    refused(ValueError, "frequencies", lambda: s.rotate(q, k, ones(5), head_dim=8))
+    refused(TypeError, "frequencies", lambda: s.rotate(q, k, f.double(), head_dim=8))
+    refused(ValueError, "norm", lambda: s.rotate(q, k, f, head_dim=8, norm="l2"))
+    refused(ValueError, "k_weight", lambda: s.rotate(q, None, f, head_dim=8, norm="rms", k_weight=ones(8)))
+    refused(ValueError, "k has shape", lambda: s.rotate(q, ones(6, 16), f, head_dim=8))
+    refused(TypeError, "past", lambda: s.rotate(q, k, f, head_dim=8, past=p.long()))
+    refused(ValueError, "past has shape", lambda: s.rotate(q, k, f, head_dim=8, past=p[:1]))
+    refused(ValueError, "positions has shape", lambda: s.rotate(q, k, f, head_dim=8, positions=at[:, :6]))
+    refused(ValueError, "sections without", lambda: s.rotate(q, k, f, head_dim=8, sections=[4]))
+    refused(MureError, "sections are 3", lambda: s.rotate(q, k, f, head_dim=8, positions=at, sections=[3]))
+    refused(MureError, "exclude", lambda: s.rotate(q, k, f, head_dim=8, positions=at, past=p))
+    refused(MureError, "overlaps", lambda: s.rotate(q, k, f, head_dim=8, k_out=q[:, :16]))
+    refused(ValueError, "mutants", lambda: s.rotate(ones(2, 7, 32), ones(3, 7, 16), f, head_dim=8))
+    refused(ValueError, "v has shape", lambda: s.attend(q, k, ones(7, 8), head_dim=8))
+    refused(MureError, "multiple of kv_heads", lambda: s.attend(q, ones(7, 24), ones(7, 24), head_dim=8))
+    refused(TypeError, "v is", lambda: s.attend(q, k, k.bfloat16(), head_dim=8))
+    refused(TypeError, "float32 or bfloat16", lambda: s.attend(q.half(), k.half(), k.half(), head_dim=8))
+    for w in (0, -3):
+        refused(ValueError, "window", lambda: s.attend(q, k, k + 0, head_dim=8, window=w))
+    refused(MureError, "past without", lambda: s.attend(q, k, k + 0, head_dim=8, past=p))
+    refused(TypeError, "pair", lambda: s.attend(q, k, k + 0, head_dim=8, cache=cache[:1]))
+    refused(ValueError, "cache of values has shape", lambda: s.attend(q, k, k + 0, head_dim=8, cache=(cache[0], ones(2, 8, 16))))
+    refused(ValueError, "cache of keys has shape", lambda: s.attend(q, k, k + 0, head_dim=8, cache=(ones(3, 9, 16), ones(3, 9, 16))))
+    refused(MureError, "overlaps", lambda: s.attend(q, k, k + 0, head_dim=8, cache=(cache[0], cache[0])))
+    refused(MureError, "share", lambda: s.attend(q, ones(2, 7, 16), ones(2, 7, 16), head_dim=8, cache=cache))
+    refused(MureError, "overlap", lambda: s.attend(q, k, k + 0, head_dim=8, cache=(ones(1, 9, 16).expand(2, -1, -1), cache[1])))
+    refused(ValueError, "contiguous", lambda: s.attend(q, ones(16, 7).T, k, head_dim=8))
+    refused(MureError, "scale", lambda: s.attend(q, k, k + 0, head_dim=8, scale=float("nan")))
+    refused(ValueError, "up has shape", lambda: mure.gated(ones(7, 8), ones(6, 8), ones(5, 8)))
+    refused(ValueError, "gate has shape", lambda: mure.gated(ones(7, 8), ones(8), ones(6, 8)))
+    refused(ValueError, "gate_bias has shape", lambda: mure.gated(ones(7, 8), ones(6, 8), ones(6, 8), gate_bias=ones(8)))
+    refused(ValueError, "activation", lambda: mure.gated(ones(7, 8), ones(6, 8), ones(6, 8), activation="tanh"))
+    refused(TypeError, "up must", lambda: mure.gated(ones(7, 8), ones(6, 8), None))
+    refused(ValueError, "out has shape", lambda: mure.gated(ones(2, 7, 8), ones(6, 8), ones(6, 8), out=ones(7, 6)))
+    refused(MureError, "overlaps", lambda: mure.gated(ones(7, 8), q[:6, :8], ones(6, 8), out=q[:, :6]))
+
+
+def test_gradients_tangents_and_views(mure):
+    s = mure.sequences([4, 3])
+    q, k, f, w = ones(7, 32), ones(7, 16), ones(4), ones(6, 8)
+    leaf = ones(7, 32, requires_grad=True)
+    calls = [lambda t: s.rotate(t, k, f, head_dim=8), lambda t: s.attend(t, k, k + 0, head_dim=8), lambda t: s.attend(q, t[:, :16], k, head_dim=8),
+             lambda t: s.attend(q, k, k + 0, head_dim=8, out=t), lambda t: mure.gated(t[:, :8], w, w + 0), lambda t: mure.gated(q[:, :8], t[:6, :8], w)]
+    for c in calls:
+        refused(ValueError, "requires a gradient", lambda: c(leaf))
+        with torch.no_grad(), pytest.raises(MureError, match="planning-only"):
+            c(leaf)
+        refused(ValueError, "no memory", lambda: c(torch._efficientzerotensor((7, 32))))
+        with fwd.dual_level():
+            refused(ValueError, "tangent", lambda: c(fwd.make_dual(q, q)))
+    held = ones(2, 9, 16, requires_grad=True)
+    refused(ValueError, "requires a gradient", lambda: s.attend(q, k, k + 0, head_dim=8, cache=(held, ones(2, 9, 16))))
+
+
+def test_closed(mure):
+    s = mure.sequences([4, 3])
+    s.close()
+    refused(ValueError, "closed", lambda: s.attend(ones(7, 32), ones(7, 16), ones(7, 16), head_dim=8))
+    refused(ValueError, "closed", lambda: s.rotate(ones(7, 32), None, ones(4), head_dim=8))
+    mure.close()
+    refused(ValueError, "closed", lambda: mure.gated(ones(7, 8), ones(6, 8), ones(6, 8)))

@@ -117,7 +117,6 @@ __device__ __forceinline__ void copy16(const void* p, int bytes, unsigned off, c
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)to;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform((int)lds)), "v"(off), "s"(r) : "memory", "m0");
 }
-#pragma clang diagnostic pop
 
 // Copies of KT keys' rows into a tile by W waves, 1024 bytes a wave and step.
 template <typename T, int DB, int KT, int W, Reads R> struct Copy {
@@ -205,6 +204,7 @@ template <typename T, int DB, int KT, int W, Reads R> struct Copy {
     }
   }
 };
+#pragma clang diagnostic pop
 
 // A row of queries times the scale's sign, as the second operand of S^T: pieces W s + w of it.  Scores are then scaled by a
 // positive number, which keeps their order and hides a key by -inf.

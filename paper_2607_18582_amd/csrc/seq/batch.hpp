@@ -145,19 +145,22 @@ inline void check_output(const Span& s) {
   if (!rows_inside && !muts_inside) invalid(std::string(s.name) + ": its rows overlap");
 }
 
-// Whether two tensors may share memory.  Rows side by side in one buffer (the
-// same pitch, at different columns) do not.
+// Whether two tensors may share memory.  Rows side by side in one buffer (at
+// different columns, whichever axis goes around which) do not.
 inline bool meet(const Span& a, const Span& b) {
   if (a.extent() == 0 || b.extent() == 0) return false;
   const wide pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
   if (pa + a.extent() <= pb || pb + b.extent() <= pa) return false;
-  // The pitch in bytes of a tensor of several rows, and of one with one row
-  // per mutant, or none.
-  auto pitch = [](const Span& s) { return (s.rows > 1 ? s.row_stride : s.outers > 1 ? s.outer_stride : s.mutant_stride) * (wide)s.esize; };
-  const wide q = pitch(a);
-  if (q == 0 || pitch(b) != q) return true;
+  // What divides all strides of both, in bytes: each has its elements in the same columns of every piece of that many.
+  wide q = 0;
   for (const Span* s : {&a, &b})
-    if ((wide)s->mutant_stride * s->esize % q || (wide)s->outer_stride * s->esize % q || (wide)s->width * s->esize > q) return true;
+    for (const int64_t stride : {s->row_stride, s->outer_stride, s->mutant_stride})
+      for (wide x = (wide)stride * s->esize; x;) {
+        const wide rest = q % x;
+        q = x;
+        x = rest;
+      }
+  if (q == 0 || (wide)a.width * a.esize > q || (wide)b.width * b.esize > q) return true;
   const wide d = ((pb - pa) % q + q) % q;      // b's first column, as a's rows see it
   return d < (wide)a.width * a.esize || d + (wide)b.width * b.esize > q;
 }

@@ -209,6 +209,14 @@ def test_caches_beside_each_other(mure):
     a.v_cache.p = p + 2 * G * D - 2
     st, msg = call(mure, "attend", a)
     assert st == MURE_E_INVALID and "overlaps" in msg
+    # sequences inside rows, and mutants inside those
+    a.k_cache = Cache(p, 2 * G * D, 2 * 2 * G * D, 3 * 2 * 2 * G * D)
+    a.v_cache = Cache(p + 2 * G * D, 2 * G * D, 2 * 2 * G * D, 3 * 2 * 2 * G * D)
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_UNSUPPORTED and "planning-only" in msg, msg
+    a.v_cache.mutant_stride += 1
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_INVALID and "overlaps" in msg
     a = attend_args(Buffers())
     for x in (a.k, a.v, a.k_cache, a.v_cache):
         x.mutant_stride = 0

@@ -224,7 +224,7 @@ def test_a_block_against_float64(mure):
     h = normal(torch.Generator().manual_seed(11), sum(lengths), 96)
     got = block(mure, mure.sequences(lengths), h.cuda(), w)
     c = {n: t.double().cpu() for n, t in w.items()}
-    norm = lambda x, weight: x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-6) * weight  # noqa: E731
+    norm = lambda x, weight: x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-5) * weight  # noqa: E731
     x = norm(h.double(), c["norm"])
     q = R.rotate((x @ c["q"])[None], c["f"][None], lengths, 32, "rms", c["qn"][None])[0]
     k = R.rotate((x @ c["k"])[None], c["f"][None], lengths, 32, "rms")[0]

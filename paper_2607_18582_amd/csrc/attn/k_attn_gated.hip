@@ -85,8 +85,23 @@ template <typename T> __device__ __forceinline__ void finish(const mure_attn_gat
   store4<T>(static_cast<T*>(a.out.p) + m * a.out.mutant_stride + row * a.out.row_stride, n, a.outer, v[0], v[1], v[2], v[3]);
 }
 
-// WM x WN waves; BYTES of the summed axis a stage (64 or 128)
-template <typename T, int MT, int NT, int WM, int WN, int BYTES, bool FAST>
+// Few outputs over a long summed axis make few tiles, each with a long chain of products.  Their axis is summed in
+// eighths, which are added in order: in one block after the other, or side by side (gated_split_kernel).  This follows from
+// the weights' sizes alone, as a row's results do.
+constexpr int SPLIT = 8, SPLIT_OUTPUTS = 512, SPLIT_BYTES = 2048;
+
+template <typename T> __host__ __device__ __forceinline__ bool splits(const mure_attn_gated_args& a) {
+  return a.outer <= SPLIT_OUTPUTS && a.inner * (int)sizeof(T) >= SPLIT_BYTES;
+}
+
+// Elements of an eighth: pieces of 256 bytes
+template <typename T> __device__ __forceinline__ int eighth(int inner) {
+  constexpr int KS = 256 / (int)sizeof(T);
+  return ((inner + KS - 1) / KS + SPLIT - 1) / SPLIT * KS;
+}
+
+// WM x WN waves; BYTES of the summed axis a stage (64 or 128); PARTS: the axis in eighths
+template <typename T, int MT, int NT, int WM, int WN, int BYTES, bool FAST, bool PARTS>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(mure_attn_gated_args a, int n_tiles, int m_tiles) {
   constexpr int WAVES = WM * WN, ROWS = MT + 2 * NT, STAGE = ROWS * BYTES, E = 16 / (int)sizeof(T), PIECES = BYTES / 16, KS = PIECES * E;
   constexpr int TM = MT / WM / 16, TN = NT / WN / 16, EACH = 64 / PIECES;      // rows of a copy of 1024 bytes
@@ -136,6 +151,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(mure_attn_gated_
   for (int i = 0; i < TN; ++i)
 #pragma unroll
     for (int j = 0; j < TM; ++j) g[i][j] = v4f{}, u[i][j] = v4f{};
+  v4f all_g[PARTS ? TN : 1][PARTS ? TM : 1] = {}, all_u[PARTS ? TN : 1][PARTS ? TM : 1] = {};
+  const int part = PARTS ? eighth<T>(a.inner) : 0;
+  int left = part;                             // of the eighth
   load(0, 0);
   put(0);
   int stage = 0;
@@ -168,14 +186,92 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_kernel(mure_attn_gated_
           }
     }
     if (k0 + KS < a.inner) put(stage ^ 1);
+    if constexpr (PARTS)
+      if ((left -= KS) == 0 || k0 + KS >= a.inner) {
+        left = part;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int j = 0; j < TM; ++j) {
+            all_g[i][j] += g[i][j], all_u[i][j] += u[i][j];
+            g[i][j] = v4f{}, u[i][j] = v4f{};
+          }
+      }
   }
 #pragma unroll
   for (int i = 0; i < TN; ++i) {
     const int n = col0 + wn * (NT / WN) + i * 16 + (lane >> 4) * 4;
     const v4f gb = bias_at(a.gate_bias, m, n, a.outer), ub = bias_at(a.up_bias, m, n, a.outer);
 #pragma unroll
-    for (int j = 0; j < TM; ++j) finish<T>(a, m, row0 + wm * (MT / WM) + j * 16 + (lane & 15), n, g[i][j], u[i][j], gb, ub);
+    for (int j = 0; j < TM; ++j)
+      finish<T>(a, m, row0 + wm * (MT / WM) + j * 16 + (lane & 15), n, PARTS ? all_g[PARTS ? i : 0][PARTS ? j : 0] : g[i][j],
+                PARTS ? all_u[PARTS ? i : 0][PARTS ? j : 0] : u[i][j], gb, ub);
   }
+}
+
+// ---- the eighths side by side: a wave each, of 16 TM rows by 16 outputs, from memory to registers; their sums meet in LDS
+
+template <typename T, int TM> __global__ __launch_bounds__(64 * SPLIT, 2) void gated_split_kernel(mure_attn_gated_args a, int n_tiles, int m_tiles) {
+  constexpr int E = 16 / (int)sizeof(T), KS = 256 / (int)sizeof(T), PITCH = 36;
+  __shared__ float sums[SPLIT][16 * TM][PITCH];                // a row: 16 of the gate, 16 of the other projection
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, quarter = lane >> 4;
+  int mt, nt, m;
+  place_of(blockIdx.x, n_tiles, m_tiles, mt, nt, m);
+  const int64_t row0 = (int64_t)mt * 16 * TM;
+  const int col0 = nt * 16;
+  const Operands<T> op(a, m);
+  const T *xr[TM], *wr[2] = {op.gate_row(a, col0 + (lane & 15)), op.up_row(a, col0 + (lane & 15))};
+#pragma unroll
+  for (int j = 0; j < TM; ++j) xr[j] = op.x_row(a, row0 + 16 * j + (lane & 15));
+  struct Pieces {
+    v4u x[4][TM], w[4][2];
+  };
+  auto load = [&](int k0, Pieces& p) {
+    const bool whole = k0 + KS <= a.inner;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = k0 + (4 * i + quarter) * E;
+#pragma unroll
+      for (int j = 0; j < TM; ++j) p.x[i][j] = whole ? *reinterpret_cast<const v4u_any*>(xr[j] + e) : piece_of<T>(xr[j], e, a.inner, op.x_end);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) p.w[i][w] = whole ? *reinterpret_cast<const v4u_any*>(wr[w] + e) : piece_of<T>(wr[w], e, a.inner, w ? op.up_end : op.gate_end);
+    }
+  };
+  v4f acc[2][TM] = {};
+  auto add = [&](const Pieces& p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < (sizeof(T) == 2 ? 1 : 4); ++e)
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int j = 0; j < TM; ++j) acc[w][j] = mma16_part<T>(p.w[i][w], p.x[i][j], e, acc[w][j]);
+  };
+  const int part = eighth<T>(a.inner), from = wave * part, to = min(a.inner, from + part);
+  Pieces one, other;
+  if (from < to) load(from, one);
+  for (int k0 = from; k0 < to; k0 += 2 * KS) {
+    if (k0 + KS < to) load(k0 + KS, other);
+    add(one);
+    if (k0 + KS >= to) break;
+    if (k0 + 2 * KS < to) load(k0 + 2 * KS, one);
+    add(other);
+  }
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) *reinterpret_cast<v4f*>(&sums[wave][16 * j + (lane & 15)][16 * w + 4 * quarter]) = acc[w][j];
+  __syncthreads();
+  const int r = tid / 16, n = col0 + tid % 16;
+  const int64_t row = row0 + r;
+  if (r >= 16 * TM || row >= a.rows || n >= a.outer) return;
+  float g = 0.f, u = 0.f;
+#pragma unroll
+  for (int w = 0; w < SPLIT; ++w) g += sums[w][r][tid % 16], u += sums[w][r][16 + tid % 16];
+  if (a.gate_bias.p) g += a.gate_bias.p[m * a.gate_bias.mutant_stride + n];
+  if (a.up_bias.p) u += a.up_bias.p[m * a.up_bias.mutant_stride + n];
+  static_cast<T*>(a.out.p)[m * a.out.mutant_stride + row * a.out.row_stride + n] = from_f<T>(activated(g, a.activation) * u);
 }
 
 // ---- few rows: bound by the weights' bytes.  W waves have 16 rows of x each; NT = 8: the gate's 8 rows of weights and the
@@ -198,34 +294,25 @@ template <typename T, int W, int NT, int STAGES, bool FAST> __global__ __launch_
     const int r = (wave * COPIES + c) * 4 + lane / 16, w = r - 16 * W;
     from[c] = w < 0 ? op.x_row(a, row0 + r) : w < NT ? op.gate_row(a, col0 + w) : op.up_row(a, col0 + w - NT);
   }
-  auto load = [&](int k0, int stage) {
+  // FAST: straight to LDS.  Otherwise through registers, which hold as many stages.
+  v4u held[FAST ? 1 : STAGES - 1][COPIES];
+  auto load = [&](int k0, int stage, int slot) {
+    const bool whole = k0 + KS <= a.inner;
 #pragma unroll
     for (int c = 0; c < COPIES; ++c) {
       const int q = wave * COPIES + c, r = q * 4 + lane / 16, e = k0 + ((lane & 15) ^ (r & 15)) * E;
-      char* to = lds + stage * STAGE + q * 1024;
       if constexpr (FAST) {
         const void* p = e < a.inner ? static_cast<const void*>(from[c] + e) : ZEROS;
-        __builtin_amdgcn_global_load_lds(p, (lds_void*)to, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(p, (lds_void*)(lds + stage * STAGE + q * 1024), 16, 0, 0);
       } else {
-        *reinterpret_cast<v4u*>(to + lane * 16) = piece_of<T>(from[c], e, a.inner, r < 16 * W ? op.x_end : r < 16 * W + NT ? op.gate_end : op.up_end);
+        held[slot][c] = whole ? *reinterpret_cast<const v4u_any*>(from[c] + e)
+                              : piece_of<T>(from[c], e, a.inner, r < 16 * W ? op.x_end : r < 16 * W + NT ? op.gate_end : op.up_end);
       }
     }
   };
   v4f acc[N] = {};                             // outputs 4 (l / 16) ... of row l % 16: NT = 8: the gate's, from l = 32 on the other's
   const int stages = (a.inner + KS - 1) / KS;
-  for (int s = 0; s < STAGES - 1 && s < stages; ++s) load(s * KS, s);
-  int at = 0;
-  for (int s = 0; s < stages; ++s) {
-    if constexpr (FAST) {                      // this stage's copies are there, the next ones' may be on their way
-      const int next = min(STAGES - 2, stages - 1 - s);
-      if (next == 2) wait_copies<2 * COPIES>();
-      else if (next == 1) wait_copies<COPIES>();
-      else wait_copies();
-    }
-    __syncthreads();
-    if (s + STAGES - 1 < stages) load((s + STAGES - 1) * KS, at ? at - 1 : STAGES - 1);
-    const char* base = lds + at * STAGE;
-    at = at + 1 == STAGES ? 0 : at + 1;
+  auto products = [&](const char* base) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int p = (i * 4 + (lane >> 4)) ^ (lane & 15);
@@ -233,6 +320,37 @@ template <typename T, int W, int NT, int STAGES, bool FAST> __global__ __launch_
 #pragma unroll
       for (int w = 0; w < N; ++w) acc[w] = mma16<T>(*reinterpret_cast<const v4u*>(base + (16 * (W + w) + (lane & 15)) * 256 + p * 16), xs, acc[w]);
     }
+  };
+  if constexpr (FAST) {
+    for (int s = 0; s < STAGES - 1 && s < stages; ++s) load(s * KS, s, 0);
+    int at = 0;
+    for (int s = 0; s < stages; ++s) {         // this stage's copies are there, the next ones' may be on their way
+      const int next = min(STAGES - 2, stages - 1 - s);
+      if (next == 2) wait_copies<2 * COPIES>();
+      else if (next == 1) wait_copies<COPIES>();
+      else wait_copies();
+      __syncthreads();
+      if (s + STAGES - 1 < stages) load((s + STAGES - 1) * KS, at ? at - 1 : STAGES - 1, 0);
+      products(lds + at * STAGE);
+      at = at + 1 == STAGES ? 0 : at + 1;
+    }
+  } else {
+    constexpr int D = STAGES - 1;
+#pragma unroll
+    for (int s = 0; s < D; ++s)
+      if (s < stages) load(s * KS, 0, s);
+    for (int s0 = 0; s0 < stages; s0 += D)
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        const int s = s0 + d;
+        if (s >= stages) break;
+        char* base = lds + s % 2 * STAGE;      // whose readers have passed the last barrier
+#pragma unroll
+        for (int c = 0; c < COPIES; ++c) *reinterpret_cast<v4u*>(base + (wave * COPIES + c) * 1024 + lane * 16) = held[d][c];
+        __syncthreads();
+        if (s + D < stages) load((s + D) * KS, 0, d);
+        products(base);
+      }
   }
   const int64_t row = row0 + 16 * wave + (lane & 15);
   const int n = col0 + (lane >> 4) * 4;
@@ -274,8 +392,9 @@ hipError_t over_tiles(const void* kernel, const mure_attn_gated_args& a, int64_t
   return hipSuccess;
 }
 
-template <typename T, int MT, int NT, int WM, int WN, int BYTES> hipError_t gated_f(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
-  return over_tiles(fast ? reinterpret_cast<const void*>(gated_kernel<T, MT, NT, WM, WN, BYTES, true>) : reinterpret_cast<const void*>(gated_kernel<T, MT, NT, WM, WN, BYTES, false>),
+template <typename T, int MT, int NT, int WM, int WN, int BYTES, bool PARTS> hipError_t gated_f(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
+  return over_tiles(fast ? reinterpret_cast<const void*>(gated_kernel<T, MT, NT, WM, WN, BYTES, true, PARTS>)
+                         : reinterpret_cast<const void*>(gated_kernel<T, MT, NT, WM, WN, BYTES, false, PARTS>),
                     a, sizeof(T), MT, NT, 64 * WM * WN, 2 * (MT + 2 * NT) * BYTES, s);
 }
 
@@ -284,13 +403,23 @@ template <typename T, int W, int NT, int STAGES> hipError_t gated_few(const mure
                     sizeof(T), 16 * W, NT, 64 * W, STAGES * (16 * W + 2 * NT) * 256, s);
 }
 
+template <typename T, int TM> hipError_t gated_split(const mure_attn_gated_args& a, hipStream_t s) {
+  return over_tiles(reinterpret_cast<const void*>(gated_split_kernel<T, TM>), a, sizeof(T), 16 * TM, 16, 64 * SPLIT, 0, s);
+}
+
 template <typename T> hipError_t gated_t(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
+  constexpr int BYTES = sizeof(T) == 4 ? 64 : 128;
+  const int64_t tiles = (a.rows + 127) / 128 * ((a.outer + 63) / 64) * a.n_mutants;
+  if (splits<T>(a)) {
+    if (tiles >= (sizeof(T) == 4 ? 128 : 64)) return gated_f<T, 128, 64, 2, 2, BYTES, true>(a, fast, s);
+    return a.rows <= 16 ? gated_split<T, 1>(a, s) : gated_split<T, 2>(a, s);
+  }
   if (a.rows <= 16) return gated_few<T, 1, 8, 4>(a, fast, s);
   if (a.rows <= 32) return gated_few<T, 2, 8, 4>(a, fast, s);
   if (a.rows <= 64) return gated_few<T, 4, 16, 3>(a, fast, s);
   if constexpr (sizeof(T) == 2)
-    if ((int64_t)((a.rows + 255) / 256) * ((a.outer + 127) / 128) * a.n_mutants >= 512) return gated_f<T, 256, 128, 2, 4, 128>(a, fast, s);
-  return gated_f<T, 128, 64, 2, 2, sizeof(T) == 4 ? 64 : 128>(a, fast, s);
+    if ((int64_t)((a.rows + 255) / 256) * ((a.outer + 127) / 128) * a.n_mutants >= 512) return gated_f<T, 256, 128, 2, 4, 128, false>(a, fast, s);
+  return gated_f<T, 128, 64, 2, 2, BYTES, false>(a, fast, s);
 }
 
 }  // namespace

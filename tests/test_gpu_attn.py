@@ -253,3 +253,22 @@ def test_gated_rows_do_not_depend_on_others(mure, dtype):
     odd[:, 1:] = x
     assert torch.equal(mure.gated(odd[:, 1:], gate, up), whole)
     assert torch.equal(mure.gated(x.expand(3, -1, -1).contiguous(), gate, up), whole.expand(3, -1, -1))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K,N", [(2048, 130), (1101, 500), (2309, 64)])
+def test_gated_long_sums(mure, dtype, K, N):
+    """Few outputs over many inputs: the same bits in few rows and many, alone and with other mutants."""
+    say(f"[gated long] {dtype} K={K} N={N}")
+    g = torch.Generator().manual_seed(10)
+    dt, rows = TYPES[dtype], 6000
+    x, gate, up, bias = cuda(normal(g, rows, K, dtype=dt), normal(g, N, K, dtype=dt, std=K ** -0.5), normal(g, N, K, dtype=dt, std=K ** -0.5), normal(g, N))
+    few = mure.gated(x[:40], gate, up, gate_bias=bias, activation="gelu")
+    R.close(few[None], R.gated(x[None, :40].cpu(), gate[None].cpu(), up[None].cpu(), bias[None].cpu(), kind="gelu"), "out")
+    whole = mure.gated(x.expand(8, -1, -1), gate, up, gate_bias=bias, activation="gelu")
+    assert torch.equal(whole, whole[:1].expand(8, -1, -1))
+    for first, n in ((0, 40), (5, 1), (17, 16), (100, 33), (650, 300), (5990, 10), (0, 6000)):
+        assert torch.equal(mure.gated(x[first:first + n], gate, up, gate_bias=bias, activation="gelu"), whole[0, first:first + n]), (first, n)
+    odd = torch.zeros(300, K + 1, dtype=dt, device="cuda")
+    odd[:, 1:] = x[:300]
+    assert torch.equal(mure.gated(odd[:, 1:], gate, up, gate_bias=bias, activation="gelu"), whole[0, :300])

@@ -96,10 +96,10 @@ Span cache_span(const char* name, const mure_attn_cache& c, int64_t es, int64_t 
   return s;
 }
 
-// Whether rows at these strides (the first between rows) are aligned pieces of 16 bytes, 64 rows within 2^31 bytes.
-bool pieces(const void* p, int64_t es, std::initializer_list<int64_t> strides) {
-  bool ok = reinterpret_cast<uintptr_t>(p) % 16 == 0 && *strides.begin() * es < 1 << 24;
-  for (int64_t v : strides) ok = ok && v * es % 16 == 0;
+// Whether `bytes` divides the address and strides (the first between rows) of rows, 64 of which lie within 2^31 bytes.
+bool aligned(int64_t bytes, const void* p, int64_t es, std::initializer_list<int64_t> strides) {
+  bool ok = reinterpret_cast<uintptr_t>(p) % bytes == 0 && *strides.begin() * es < 1 << 24;
+  for (int64_t v : strides) ok = ok && v * es % bytes == 0;
   return ok;
 }
 
@@ -151,9 +151,12 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   if ((wide)M * s->n_brief > INT32_MAX || (wide)M * s->n_runs > INT32_MAX) throw Fail{MURE_E_UNSUPPORTED, "too many sequences times mutants"};
   check_device(s->device);
   if (T == 0) return;
-  k.fast = D * es % 16 == 0 && pieces(a.k.p, es, {a.k.row_stride, a.k.mutant_stride}) && pieces(a.v.p, es, {a.v.row_stride, a.v.mutant_stride}) &&
-           (!held || (pieces(a.k_cache.p, es, {a.k_cache.row_stride, a.k_cache.seq_stride, a.k_cache.mutant_stride}) &&
-                      pieces(a.v_cache.p, es, {a.v_cache.row_stride, a.v_cache.seq_stride, a.v_cache.mutant_stride})));
+  const auto reads = [&](int64_t bytes) {
+    return D * es % bytes == 0 && aligned(bytes, a.k.p, es, {a.k.row_stride, a.k.mutant_stride}) && aligned(bytes, a.v.p, es, {a.v.row_stride, a.v.mutant_stride}) &&
+           (!held || (aligned(bytes, a.k_cache.p, es, {a.k_cache.row_stride, a.k_cache.seq_stride, a.k_cache.mutant_stride}) &&
+                      aligned(bytes, a.v_cache.p, es, {a.v_cache.row_stride, a.v_cache.seq_stride, a.v_cache.mutant_stride})));
+  };
+  k.fast = reads(16) ? PIECES : D * es >= 16 && reads(4) ? WORDS : ELEMENTS;
   const bool f32 = a.dtype == MURE_F32;
   const auto launch_short = f32 ? attn_short_f32 : attn_short_bf16;
   const auto launch_runs = f32 ? attn_runs_f32 : attn_runs_bf16;
@@ -244,8 +247,8 @@ void gated(mure_ctx* ctx, const mure_attn_gated_args* args) {
   const CtxView cv = ctx_view(ctx);
   check_device(cv.device);
   if (R == 0) return;
-  const bool fast = K * es % 16 == 0 && pieces(a.x.p, es, {a.x.row_stride, a.x.mutant_stride}) &&
-                    pieces(a.gate.p, es, {a.gate.row_stride, a.gate.mutant_stride}) && pieces(a.up.p, es, {a.up.row_stride, a.up.mutant_stride});
+  const bool fast = K * es % 16 == 0 && aligned(16, a.x.p, es, {a.x.row_stride, a.x.mutant_stride}) &&
+                    aligned(16, a.gate.p, es, {a.gate.row_stride, a.gate.mutant_stride}) && aligned(16, a.up.p, es, {a.up.row_stride, a.up.mutant_stride});
   check(launch_attn_gated(a, fast, cv.stream), "mure_attn_gated");
 }
 

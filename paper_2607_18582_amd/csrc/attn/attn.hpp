@@ -16,6 +16,10 @@ struct AttnRotateArgs {
 
 constexpr int ATTN_KEYS_SHORT = 512, ATTN_KEYS_MID = 1024;     // keys of a part, where they are worked on side by side
 
+// How rows are read: element by element, or copied to LDS in pieces of 16 bytes, of which they are a whole number, aligned, or
+// in which they are whole words of 4 bytes.
+enum AttnReads : int { ELEMENTS, WORDS, PIECES };
+
 struct AttnArgs {
   mure_attn_attend_args a;
   const SeqItem* items = nullptr;
@@ -25,7 +29,7 @@ struct AttnArgs {
   int parts = 1;                               // of the keys
   float* ws_o = nullptr;                       // [mutants][items][rows_each][heads][parts][head_dim], before the division
   float* ws_ml = nullptr;                      // ... [2]: the largest exponent (of 2), the sum
-  bool fast = false;                           // rows of k, v and the caches are whole aligned 16-byte pieces
+  int fast = 0;                                // of k, v and the caches
 };
 
 // launchers (return the launch status)
@@ -37,6 +41,6 @@ hipError_t attn_runs_f32(const AttnArgs& a, hipStream_t s);
 hipError_t attn_runs_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t attn_join_f32(const AttnArgs& a, int keys, hipStream_t s);
 hipError_t attn_join_bf16(const AttnArgs& a, int keys, hipStream_t s);
-hipError_t launch_attn_gated(const mure_attn_gated_args& a, bool fast, hipStream_t s);     // fast: as above, of x, gate and up
+hipError_t launch_attn_gated(const mure_attn_gated_args& a, bool fast, hipStream_t s);     // fast: rows of x, gate and up are whole aligned 16-byte pieces
 
 }  // namespace mure

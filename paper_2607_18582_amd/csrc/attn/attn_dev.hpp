@@ -105,6 +105,19 @@ template <typename T> __device__ __forceinline__ v4u load_piece(const T* p, int 
   return v;
 }
 
+// The same of a row of whole words, at least one piece long, without a branch: the row's last piece, moved down.
+template <typename T> __device__ __forceinline__ v4u load_words(const T* p, int first, int n) {
+  constexpr int E = 16 / sizeof(T);
+  v4u v = *reinterpret_cast<const v4u_any*>(p + min(first, n - E));
+  const int by = (first - (n - E)) * (int)sizeof(T) / 4;       // words
+  if (by > 0) {
+    if (by & 1) v = v4u{v[1], v[2], v[3], 0};
+    if (by & 2) v = v4u{v[2], v[3], 0, 0};
+    if (by >= 4) v = v4u{0, 0, 0, 0};
+  }
+  return v;
+}
+
 // 16 bytes a lane from `off` on of a buffer of `bytes` bytes at p (zeros behind it) to `to`, one lane after the other.  As the
 // compiler's builtin every later read of LDS would wait for it; this one only wait_copies waits for.  The wait states are
 // those between a scalar's write by the vector unit, or m0's, and its use here.  Nothing else in these kernels uses m0, so
@@ -178,7 +191,7 @@ template <typename T, int DB, int KT, int W, Reads R> struct Copy {
     place(wave, lane, key, e);
     const unsigned off = (unsigned)(key * pitch) + (e < n ? (unsigned)(e * (int)sizeof(T)) : 0x80000000u);
     const uint64_t at = (uint64_t)uniform(p);
-    const v4u r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)((KT - 1) * pitch + n * (int)sizeof(T)), 0x00027000u};
+    const v4u r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)uniform((KT - 1) * pitch + n * (int)sizeof(T)), 0x00027000u};
     const uint32_t lds = (uint32_t)uniform((int)(uint32_t)(uintptr_t)(lds_void*)(tile + wave * 1024));
     const int step = W * EACH * pitch;
     asm volatile(
@@ -189,8 +202,22 @@ template <typename T, int DB, int KT, int W, Reads R> struct Copy {
         : "memory", "m0", "scc");
   }
 
+  // Rows that are whole words but no whole pieces: after the copies, zeros behind the row in its last piece, each by the wave
+  // that copied it.
+  static __device__ __forceinline__ void trim(char* tile, int n, int wave, int lane) {
+    constexpr int E = 16 / (int)sizeof(T);
+    static_assert(KT <= 64, "");
+    if (n % E == 0) return;
+    const int piece = lane * H::PIECES + (n / E ^ Tw::of(lane)), words = n % E * (int)sizeof(T) / 4;
+    if (lane >= KT || piece / 64 % W != wave) return;
+    uint32_t* to = reinterpret_cast<uint32_t*>(tile + piece * 16);
+    if (words < 2) to[1] = 0;
+    if (words < 3) to[2] = 0;
+    to[3] = 0;
+  }
+
   // A tile at key t0; at least STEPS copies a wave.
-  template <bool FAST> static __device__ __forceinline__ void run(char* tile, const Rows<T>& rows, int t0, int end, int n, int wave, int lane) {
+  template <int FAST> static __device__ __forceinline__ void run(char* tile, const Rows<T>& rows, int t0, int end, int n, int wave, int lane) {
     if constexpr (FAST) {
       if constexpr (COPIES == 4 * W && W * EACH % Tw::PERIOD == 0) {
         if (t0 >= rows.past && t0 + KT <= end) return whole(tile, rows.own + (int64_t)(t0 - rows.past) * rows.own_stride, rows.own_stride, n, wave, lane);

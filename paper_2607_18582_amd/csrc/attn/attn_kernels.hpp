@@ -80,7 +80,7 @@ template <typename T, int DB> struct Run {
   static constexpr bool MIXED = sizeof(T) == 2 && DB <= 4;     // float32 is bound by its matrix instructions anyway
 };
 
-template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <= 4 ? 2 : 1) void run_kernel(AttnArgs k) {
+template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, DB <= 4 ? 2 : 1) void run_kernel(AttnArgs k) {
   using R = Run<T, DB>;
   constexpr int KT = R::KT, KB = KT / 32;
   extern __shared__ char lds[];
@@ -130,6 +130,12 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   const auto v_tile = [&](int i) { return lds + (2 + (i & 1)) * R::TILE; };
   const auto load_k = [&](int i) { Keys::template run<FAST>(k_tile(i), src.k, t0 + i * KT, src.total, a.head_dim, wave, lane); };
   const auto load_v = [&](int i) { Values::template run<FAST>(v_tile(i), src.v, t0 + i * KT, src.total, a.head_dim, wave, lane); };
+  const auto trim_k = [&](int i) {
+    if constexpr (FAST == WORDS) Keys::trim(k_tile(i), a.head_dim, wave, lane);
+  };
+  const auto trim_v = [&](int i) {
+    if constexpr (FAST == WORDS) Values::trim(v_tile(i), a.head_dim, wave, lane);
+  };
   // Blocks of 32 keys, numbered from t0 on, of which the wave's rows see any: begin ... end - 1.
   const int begin = wave * 32 >= it.len ? 0 : (max(any_lo, from) - t0) / 32, end = wave * 32 >= it.len ? 0 : (min(any_hi, to) - t0 + 31) / 32;
   const auto seen = [&](int j) { return j >= begin && j < end; };
@@ -176,6 +182,9 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
   if (KB == 2) load_v(0);
   if (tiles > 1) load_k(1);
   wait_copies();
+  trim_k(0);
+  if (KB == 2) trim_v(0);
+  if (tiles > 1) trim_k(1);
   __syncthreads();
   if (seen(0)) s[0] = read.scores(k_tile(0), 0, q);
   if constexpr (KB == 2) {
@@ -184,6 +193,10 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
     // are free.
     const auto middle = [&](int i) {
       wait_copies();
+      if (i) {
+        if (i + 1 < tiles) trim_k(i + 1);
+        trim_v(i);
+      }
       __syncthreads();
       if (i + 2 < tiles) load_k(i + 2);
       if (i + 1 < tiles) load_v(i + 1);
@@ -215,6 +228,10 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
     // Block i reads the next tile's keys and the last one's values; this tile's keys and the values before are done with.
     for (int i = 0; i < tiles; ++i) {
       wait_copies();
+      if (i) {
+        if (i + 1 < tiles) trim_k(i + 1);
+        trim_v(i - 1);
+      }
       __syncthreads();
       if (i + 2 < tiles) load_k(i + 2);
       load_v(i);
@@ -224,6 +241,7 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, DB <=
       w[0] = w[1];
     }
     wait_copies();
+    trim_v(tiles - 1);
     __syncthreads();
     put_aside(tiles - 1);
     if (seen(tiles - 1)) run.template add<T>(read, v_tile(tiles - 1), 0, w[0]);
@@ -267,7 +285,7 @@ struct Unit {
   }
 };
 
-template <typename T, int DB, bool FAST> struct ShortWave {
+template <typename T, int DB, int FAST> struct ShortWave {
   using S = Short<T, DB>;
   using H = Head<T, DB>;
   static constexpr int STEPS = H::BYTES / 64, E = 16 / (int)sizeof(T);
@@ -297,7 +315,8 @@ template <typename T, int DB, bool FAST> struct ShortWave {
 #pragma unroll
           for (int s = 0; s < STEPS; ++s) {
             const int e = (4 * s + quarter) * E;
-            if constexpr (FAST) keys[b][s] = e < n ? *reinterpret_cast<const v4u*>(p + e) : v4u{0, 0, 0, 0};
+            if constexpr (FAST == PIECES) keys[b][s] = e < n ? *reinterpret_cast<const v4u*>(p + e) : v4u{0, 0, 0, 0};
+            else if constexpr (FAST == WORDS) keys[b][s] = load_words<T>(p, e, n);
             else keys[b][s] = e < n ? load_piece<T>(p, e, n) : v4u{0, 0, 0, 0};
           }
       }
@@ -337,6 +356,7 @@ template <typename T, int DB, bool FAST> struct ShortWave {
           l += s[b][x];
         }
       wait_copies();
+      if constexpr (FAST == WORDS) Copy<T, DB, S::KT, 1, VALUES16>::trim(tile, n, 0, lane);
       settle();
       const int see_from = max(all_lo, from) - t, see_to = min(all_hi, to) - t, there = min(S::KT, src.total - t);
       bool apart = false;
@@ -384,7 +404,7 @@ template <typename T, int DB, bool FAST> struct ShortWave {
 };
 
 // Without a cache: a unit a wave, all of the sequence's keys.
-template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, (Short<T, DB>::OCCUPANCY)) void whole_kernel(AttnArgs k, int each) {
+template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short<T, DB>::OCCUPANCY)) void whole_kernel(AttnArgs k, int each) {
   using S = Short<T, DB>;
   extern __shared__ char lds[];
   const mure_attn_attend_args& a = k.a;
@@ -411,7 +431,7 @@ template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, (Shor
 }
 
 // Over a cache: a unit a block, the part's keys spread over its waves.
-template <typename T, int DB, bool FAST> __global__ __launch_bounds__(256, (Short<T, DB>::OCCUPANCY)) void short_kernel(AttnArgs k, int units) {
+template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short<T, DB>::OCCUPANCY)) void short_kernel(AttnArgs k, int units) {
   using S = Short<T, DB>;
   constexpr float LOWEST = -__builtin_inff();
   extern __shared__ char lds[];
@@ -546,7 +566,7 @@ template <typename... P, typename... A> hipError_t launch_lds(void (*kernel)(P..
       params);
 }
 
-template <typename T, int DB, bool FAST> hipError_t short_f(AttnArgs k, hipStream_t s) {
+template <typename T, int DB, int FAST> hipError_t short_f(AttnArgs k, hipStream_t s) {
   const int units = (k.longest * (k.a.heads / k.a.kv_heads) + 15) / 16;
   if (!k.a.k_cache.p) {
     const int each = (int)(((int64_t)k.a.kv_heads * k.a.n_mutants * units + 3) / 4);
@@ -556,14 +576,15 @@ template <typename T, int DB, bool FAST> hipError_t short_f(AttnArgs k, hipStrea
                     [&](unsigned grid) { return launch_lds(short_kernel<T, DB, FAST>, grid, Short<T, DB>::LDS, s, k, units); });
 }
 
-template <typename T, int DB, bool FAST> hipError_t runs_f(AttnArgs k, hipStream_t s) {
+template <typename T, int DB, int FAST> hipError_t runs_f(AttnArgs k, hipStream_t s) {
   return over_items(k, (int64_t)k.a.heads * k.a.n_mutants * k.parts,
                     [&](unsigned grid) { return launch_lds(run_kernel<T, DB, FAST>, grid, Run<T, DB>::LDS, s, k); });
 }
 
 template <typename T, int DB> hipError_t with_speed(const AttnArgs& k, bool brief, hipStream_t s) {
-  if (brief) return k.fast ? short_f<T, DB, true>(k, s) : short_f<T, DB, false>(k, s);
-  return k.fast ? runs_f<T, DB, true>(k, s) : runs_f<T, DB, false>(k, s);
+  if (k.fast == PIECES) return brief ? short_f<T, DB, PIECES>(k, s) : runs_f<T, DB, PIECES>(k, s);
+  if (k.fast == WORDS) return brief ? short_f<T, DB, WORDS>(k, s) : runs_f<T, DB, WORDS>(k, s);
+  return brief ? short_f<T, DB, ELEMENTS>(k, s) : runs_f<T, DB, ELEMENTS>(k, s);
 }
 
 template <typename T> hipError_t with_head(const AttnArgs& k, bool brief, hipStream_t s) {

@@ -75,7 +75,7 @@ def test_a_sequence_alone_and_in_a_batch(mure, dtype, window):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("dim", [64, 40, 128])
+@pytest.mark.parametrize("dim", [64, 40, 128, 98, 250, 34])
 def test_strides_and_alignment(mure, dtype, dim):
     """Rows that are no aligned pieces of 16 bytes, spread over wider ones, mutants inside tokens: the same bits."""
     say(f"[strides] {dtype} dim={dim}")
@@ -88,7 +88,7 @@ def test_strides_and_alignment(mure, dtype, dim):
     after = [c.clone() for c in held]
     over = seqs.attend(q, k, v, head_dim=dim, cache=after, past=past)
     T = q.size(1)
-    for shift in (1, 8):
+    for shift in (1, 2, 8):
         wide = torch.full((T, M, (H + 2 * G) * dim + 2 * shift), 9.0, dtype=dt, device="cuda")
         parts, at = [], shift
         for t in (q, k, v):

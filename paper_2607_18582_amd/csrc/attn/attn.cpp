@@ -66,8 +66,10 @@ void rotate(mure_seq* s, const mure_attn_rotate_args* args) {
   }
   check_device(s->device);
   if (T == 0) return;
-  // Runs of 12 tokens, or of 3 where those are few: a run's angles are computed once for all heads.
-  const int w = s->n_conv[2] && s->n_conv[1] * M < 2048 ? 2 : s->n_conv[1] ? 1 : 0;
+  // Runs of 12 tokens, or of 3 where those are few: a run's angles are computed once for all heads.  16 and 4 heads of 128
+  // bfloat16 channels, norm: 40 sequences of 24 tokens take 10.9 us in runs of 12 and 6.4 in runs of 3, 8 of 500 12.9 and
+  // 12.6, 12 of 1000 23.9 and 26.8; 65536 tokens 102 and 130.
+  const int w = s->n_conv[2] && s->n_conv[1] * M < 512 ? 2 : s->n_conv[1] ? 1 : 0;
   k.items = s->conv[w];
   k.n_items = s->n_conv[w];
   k.longest = CONV_RUNS[w];
@@ -146,7 +148,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   // blocks of an item: (heads or groups' row tiles) x mutants x parts
   const int64_t parts_short = held ? (a.capacity + ATTN_KEYS_SHORT - 1) / ATTN_KEYS_SHORT : 1;
   const int64_t parts_mid = held ? (a.capacity + ATTN_KEYS_MID - 1) / ATTN_KEYS_MID : 1;
-  if ((wide)a.heads * M * std::max(std::max(parts_short * ATTN_SHORT, parts_mid), (int64_t)ATTN_WHOLE_F32) > GRID)
+  if ((wide)a.heads * M * std::max(std::max(parts_short * ATTN_SHORT, parts_mid), (int64_t)ATTN_WHOLE) > GRID)
     throw Fail{MURE_E_UNSUPPORTED, "too many heads times mutants times parts of the cache"};
   if ((wide)M * s->n_brief > INT32_MAX || (wide)M * s->n_runs > INT32_MAX) throw Fail{MURE_E_UNSUPPORTED, "too many sequences times mutants"};
   check_device(s->device);
@@ -173,18 +175,14 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
     p.ws_o = p.ws_ml + 2 * rows;
   };
   if (!held) {
-    // Sequences of few tokens by waves on their own, whose rows come in 16: 250 of 20 to 80 tokens with 4 heads of 32
-    // float32 channels for 16 mutants take 212 us in runs.  Longer ones would read their keys too often.
-    const int whole = f32 ? ATTN_WHOLE_F32 : ATTN_WHOLE_BF16;
-    const int first = f32 ? 0 : s->n_above, n = s->n_brief - first;
-    const int n_runs = f32 ? s->n_runs - s->n_small_runs - s->n_above : s->n_runs - s->n_small_runs;
-    if (n) {
+    if (s->n_brief) {
       AttnArgs p = k;
-      p.items = s->brief ? s->brief + first : nullptr;
-      p.n_items = n;
-      p.longest = std::min(s->longest_brief, whole);
+      p.items = s->brief;
+      p.n_items = s->n_brief;
+      p.longest = s->longest_brief;
       check(launch_short(p, s->stream), "mure_attn_attend");
     }
+    const int n_runs = s->n_runs - s->n_small_runs;
     if (n_runs) {
       AttnArgs p = k;
       p.items = s->runs;

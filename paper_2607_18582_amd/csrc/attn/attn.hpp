@@ -14,7 +14,11 @@ struct AttnRotateArgs {
   int64_t tokens = 0;
 };
 
-constexpr int ATTN_KEYS_SHORT = 512, ATTN_KEYS_MID = 1024;     // keys of a part, where they are worked on side by side
+// Keys of a part, where they are worked on side by side: over a cache, for sequences of at most ATTN_SHORT tokens and of at most
+// ATTN_MID.  Heads of 128 bfloat16 channels, parts of 256, 512 and 1024 keys, us: 64 tokens over 4000 rows each 129, 122 and
+// 123; one over 100000 rows 115, 104 and 103; 8 over 1000 rows 13, 17 and 26.  512 tokens over 16000 rows, parts of 1024 and
+// 2048: 124 and 110; 64 tokens 40 and 57.
+constexpr int ATTN_KEYS_SHORT = 512, ATTN_KEYS_MID = 1024;
 
 // How rows are read: element by element, or copied to LDS in pieces of 16 bytes, of which they are a whole number, aligned, or
 // in which they are whole words of 4 bytes.

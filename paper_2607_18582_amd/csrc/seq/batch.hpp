@@ -74,13 +74,13 @@ struct mure_seq {
   const mure::SeqChunks* chunked = nullptr;
   int n_chunked = 0;
   int64_t n_slots = 0;
-  // attention: sequences of at most ATTN_WHOLE_F32 tokens, the longest first (above ATTN_WHOLE_BF16, ... at most
-  // ATTN_SHORT); runs of ATTN_ROWS tokens of those above ATTN_SHORT: of sequences above ATTN_MID, above ATTN_WHOLE_F32,
-  // above ATTN_WHOLE_BF16, the others, and in each the last runs of the longest first
+  // attention: sequences of at most ATTN_WHOLE tokens, the longest first (the last n_short have at most ATTN_SHORT); runs of
+  // ATTN_ROWS tokens of those above ATTN_SHORT: of sequences above ATTN_MID (n_long_runs), above ATTN_WHOLE, the others
+  // (n_small_runs), and in each the last runs of the longest first
   const mure::SeqItem* brief = nullptr;
-  int n_brief = 0, n_above = 0, n_short = 0, longest_brief = 0;
+  int n_brief = 0, n_short = 0, longest_brief = 0;
   const mure::SeqItem* runs = nullptr;
-  int n_runs = 0, n_long_runs = 0, n_small_runs = 0;           // ... of at most ATTN_WHOLE_BF16 tokens; n_above are those before
+  int n_runs = 0, n_long_runs = 0, n_small_runs = 0;
   mure::SeqWorkspace<mure::SeqApi> work;          // the chunks' states, attention over parts of the keys
 };
 

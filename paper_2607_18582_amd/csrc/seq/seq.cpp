@@ -70,22 +70,21 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
   for (int32_t i = 0; i < (int32_t)n_seq; row += lengths[i++]) {
     const int64_t L = lengths[i];
     if (L == 0) continue;
-    if (L <= ATTN_WHOLE_F32) {
+    if (L <= ATTN_WHOLE) {
       add_runs(brief, i, row, L, L, -1);
       s->longest_brief = std::max(s->longest_brief, (int)L);
-      s->n_above += L > ATTN_WHOLE_BF16;
       s->n_short += L <= ATTN_SHORT;
     }
     if (L > ATTN_SHORT) {
       add_runs(runs, i, row, L, ATTN_ROWS, -1);
-      s->n_small_runs += L <= ATTN_WHOLE_BF16;
+      s->n_small_runs += L <= ATTN_WHOLE;
       if (L > ATTN_MID) s->n_long_runs += (int)((L + ATTN_ROWS - 1) / ATTN_ROWS);
     }
   }
   std::stable_sort(brief.begin(), brief.end(), [](const SeqItem& a, const SeqItem& b) { return a.len > b.len; });
   // a causal run's work is that of the tokens up to its end
-  static_assert(ATTN_WHOLE_F32 <= ATTN_ROWS, "a sequence that may be taken whole is one run");
-  auto kind = [](const SeqItem& a) { return (a.total <= ATTN_MID) + (a.total <= ATTN_WHOLE_F32) + (a.total <= ATTN_WHOLE_BF16); };
+  static_assert(ATTN_WHOLE <= ATTN_ROWS, "a sequence that may be taken whole is one run");
+  auto kind = [](const SeqItem& a) { return (a.total <= ATTN_MID) + (a.total <= ATTN_WHOLE); };
   std::stable_sort(runs.begin(), runs.end(), [&](const SeqItem& a, const SeqItem& b) {
     return kind(a) != kind(b) ? kind(a) < kind(b) : a.pos0 + a.len > b.pos0 + b.len;
   });

@@ -31,9 +31,16 @@ struct SeqChunks {
 constexpr int SCAN_CHUNK = 128;                // tokens of a chunk
 constexpr int CONV_RUNS[] = {33, 12, 3};       // tokens of a convolution's runs
 constexpr int N_RUNS = 3;
-// Tokens of sequences that attention takes in other ways: by waves of their own over a cache; the same without one, by
-// type; their keys in parts over a cache.
-constexpr int ATTN_SHORT = 16, ATTN_WHOLE_BF16 = 64, ATTN_WHOLE_F32 = 128, ATTN_MID = 512;
+// Tokens of sequences that attention takes in other ways than by runs of ATTN_ROWS over all of their keys.  Heads of 128
+// channels, us:
+// at most ATTN_SHORT over a cache, by waves of 16 rows over parts of the keys: 16 sequences of 2, 16 and 32 tokens over 4000
+//   rows, 16 heads of 4, bfloat16, take 35, 70 and 109 so and 84, 91 and 99 in runs over parts of the keys;
+// at most ATTN_WHOLE without a cache, by waves of 16 rows: 200 sequences of 64, 96 and 128 tokens, 8 heads of 2, take 32, 46
+//   and 80 so and 37, 52 and 59 in runs (float32: 77, 116 and 236, in runs 96 tokens 128, 128 tokens 162);
+// at most ATTN_MID over a cache, in runs over parts of the keys: one sequence of 512 tokens over 16000 rows takes 124 so and
+//   334 in one piece; 16 of 64 over 4000 rows, enough to fill the chip, 122 and 90.  Longer ones have runs enough, and
+//   their parts' results would be many bytes: 2048 tokens over 16000 rows 409 and 364.
+constexpr int ATTN_SHORT = 16, ATTN_WHOLE = 96, ATTN_MID = 512;
 constexpr int ATTN_ROWS = 128;                 // tokens of a run of the others
 
 struct SeqConvArgs {

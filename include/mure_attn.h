@@ -18,8 +18,9 @@
  * strides, overlap, streams, planning-only contexts, captures.  In particular
  *   - a sequence's results (a row's, of mure_attn_gated) depend on its own
  *     tokens, past and parameters only, bit for bit.  Attention's sums follow
- *     from the sequence's lengths in this call and before it, so that a token
- *     may round differently when the same tokens come in other calls;
+ *     from the sequence's lengths in this call and before it, and from whether
+ *     there is a cache, so that a token may round differently when the same
+ *     tokens come in other calls;
  *   - arithmetic is float32.  Values are rounded to the tensors' type once,
  *     when they are stored; in bfloat16 so is the weight of every key and
  *     value before it meets the value.

@@ -43,7 +43,7 @@ class AttnBatch:
         of which the first turns the first sections[0] pairs, and so on.  Returns (q_out,
         k_out), which may be q and k themselves."""
         if positions is not None and sections is None:
-            sections = [frequencies.shape[-1]]
+            sections = list(getattr(frequencies, "shape", ()))[-1:]
         return call(self.mure, self.args.rotate, self._open(), self.mure.device, self.count, self.tokens, q, k, frequencies,
                     head_dim, one_of(NORMS, norm, "norm"), q_weight, k_weight, eps, positions, past,
                     () if sections is None else tuple(sections), bool(interleaved), q_out, k_out)

@@ -12,6 +12,7 @@ using namespace mure;
 namespace {
 
 constexpr int64_t GRID = (1 << 24) - 1;        // blocks of a launch: a grid has fewer than 2^32 threads
+constexpr int64_t PARTS_BYTES = 1 << 30;       // of a workspace for parts of keys, or as many as one sequence's run needs
 
 // ---- norm and rotation
 
@@ -118,6 +119,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   check_range(a.head_dim, 1, MURE_ATTN_MAX_HEAD, "head_dim");
   check_range(a.causal, 0, 1, "causal");
   if (a.window < 0) invalid("window is negative");
+  a.window = std::min(a.window, (int64_t)1 << 32);             // further than any key
   if (!std::isfinite(a.scale)) invalid("scale is not finite");
   if (a.reserved) invalid("reserved must be 0");
   const int64_t M = a.n_mutants, D = a.head_dim, T = s->tokens, W = a.kv_heads * D;
@@ -163,16 +165,27 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   const auto launch_short = f32 ? attn_short_f32 : attn_short_bf16;
   const auto launch_runs = f32 ? attn_runs_f32 : attn_runs_bf16;
   const auto launch_join = f32 ? attn_join_f32 : attn_join_bf16;
-  auto parted = [&](AttnArgs& p, int64_t parts, int rows_each) {
+  // Items over a cache whose keys are in parts, joined from the workspace: as many items at a time as it has room for.
+  auto parted = [&](const SeqItem* items, int n, int64_t parts, int rows_each, int keys, auto run) {
+    AttnArgs p = k;
     p.parts = (int)parts;
-    p.rows_each = rows_each;
-    if (parts <= 1) return;
-    const wide rows = (wide)M * p.n_items * rows_each * a.heads * parts, need = rows * (D + 2) * 4;
-    if (need > MOST) throw Fail{MURE_E_NOMEM, "attention workspace"};
-    void* work = nullptr;
-    check(s->work.get(s->stream, (size_t)need, &work), "attention workspace");
-    p.ws_ml = static_cast<float*>(work);
-    p.ws_o = p.ws_ml + 2 * rows;
+    p.rows_each = p.longest = rows_each;
+    int most = n;
+    if (parts > 1) {
+      const wide rows = (wide)M * rows_each * a.heads * parts, each = rows * (D + 2) * 4;
+      if (each > MOST) throw Fail{MURE_E_NOMEM, "attention workspace"};
+      most = (int)std::max<wide>(1, std::min<wide>(n, PARTS_BYTES / each));
+      void* work = nullptr;
+      check(s->work.get(s->stream, (size_t)(each * most), &work), "attention workspace");
+      p.ws_ml = static_cast<float*>(work);
+      p.ws_o = p.ws_ml + 2 * rows * most;
+    }
+    for (int i = 0; i < n; i += most) {
+      p.items = items ? items + i : nullptr;
+      p.n_items = std::min(most, n - i);
+      check(run(p, s->stream), "mure_attn_attend");
+      if (parts > 1) check(launch_join(p, keys, s->stream), "mure_attn_attend");
+    }
   };
   if (!held) {
     if (s->n_brief) {
@@ -192,15 +205,8 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
     return;
   }
   // one after the other: the workspace serves all
-  if (s->n_short) {
-    AttnArgs p = k;
-    p.items = s->brief ? s->brief + (s->n_brief - s->n_short) : nullptr;
-    p.n_items = s->n_short;
-    p.longest = std::min(s->longest_brief, ATTN_SHORT);
-    parted(p, parts_short, p.longest);
-    check(launch_short(p, s->stream), "mure_attn_attend");
-    if (p.parts > 1) check(launch_join(p, ATTN_KEYS_SHORT, s->stream), "mure_attn_attend");
-  }
+  if (s->n_short)
+    parted(s->brief ? s->brief + (s->n_brief - s->n_short) : nullptr, s->n_short, parts_short, std::min(s->longest_brief, ATTN_SHORT), ATTN_KEYS_SHORT, launch_short);
   // without parts the longer sequences' runs and the others' go in one launch
   const int n_mid = s->n_runs - s->n_long_runs;
   const bool split = parts_mid > 1 && n_mid;
@@ -210,14 +216,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
     p.n_items = split ? s->n_long_runs : s->n_runs;
     check(launch_runs(p, s->stream), "mure_attn_attend");
   }
-  if (split) {
-    AttnArgs p = k;
-    p.items = s->runs + s->n_long_runs;
-    p.n_items = n_mid;
-    parted(p, parts_mid, ATTN_ROWS);
-    check(launch_runs(p, s->stream), "mure_attn_attend");
-    check(launch_join(p, ATTN_KEYS_MID, s->stream), "mure_attn_attend");
-  }
+  if (split) parted(s->runs ? s->runs + s->n_long_runs : nullptr, n_mid, parts_mid, ATTN_ROWS, ATTN_KEYS_MID, launch_runs);
 }
 
 // ---- gated feed-forward layer

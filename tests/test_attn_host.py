@@ -312,6 +312,8 @@ def test_invalid_calls(mure):
     refused(TypeError, "past", lambda: s.rotate(q, k, f, head_dim=8, past=p.long()))
     refused(ValueError, "past has shape", lambda: s.rotate(q, k, f, head_dim=8, past=p[:1]))
     refused(ValueError, "positions has shape", lambda: s.rotate(q, k, f, head_dim=8, positions=at[:, :6]))
+    refused(TypeError, "frequencies", lambda: s.rotate(q, k, None, head_dim=8, positions=at))
+    refused(ValueError, "frequencies has shape", lambda: s.rotate(q, k, torch.tensor(1.0), head_dim=8, positions=at))
     refused(ValueError, "sections without", lambda: s.rotate(q, k, f, head_dim=8, sections=[4]))
     refused(MureError, "sections are 3", lambda: s.rotate(q, k, f, head_dim=8, positions=at, sections=[3]))
     refused(MureError, "exclude", lambda: s.rotate(q, k, f, head_dim=8, positions=at, past=p))

@@ -482,3 +482,27 @@ def test_many_sequences_and_mutants(mure):
     at = (M - 1, slice(T - 3, T))
     assert torch.equal(out[at], one.attend(q[at], k[at], v[at], head_dim=dim, cache=before, past=past[:2]))
     assert all(torch.equal(c[M - 1, n - 2:], b) for c, b in zip(cache, before))
+
+
+def test_parts_of_many_sequences_over_a_long_cache(mure):
+    """Parts that take more workspace than a call has: some sequences after the others, each as it is alone."""
+    say("[parts]")
+    dim, H, capacity, lengths = 64, 32, 131072, [300, 16, 512, 17, 3, 260, 1, 512]
+    g = torch.Generator(device="cuda").manual_seed(40)
+    T, n = sum(lengths), len(lengths)
+    q = torch.randn(2, T, H * dim, generator=g, device="cuda", dtype=torch.bfloat16)
+    k, v = (torch.randn(2, T, dim, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    cache = [torch.randn(2, n, capacity, dim, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    past = torch.tensor([3000, 130000, 1024, 5000, 70000, 1, 2000, 4090], dtype=torch.int32, device="cuda")
+    before = [c.clone() for c in cache]
+    out = mure.sequences(lengths).attend(q, k, v, head_dim=dim, cache=cache, past=past)
+    assert bool(out.isfinite().all())
+    for i, (s, count) in enumerate(zip(starts(lengths), lengths)):
+        for m in (0, 1):
+            at = (m, slice(s, s + count))
+            alone = mure.sequences([count]).attend(q[at], k[at], v[at], head_dim=dim, cache=[b[m, i:i + 1] for b in before], past=past[i:i + 1])
+            assert torch.equal(out[at], alone), (i, m)
+    assert all(torch.equal(c, b) for c, b in zip(cache, before))
+    # a window wider than 64 bits' half
+    wide = mure.sequences([40]).attend(q[0, :40], k[0, :40], v[0, :40], head_dim=dim, causal=False, window=(1 << 63) - 1)
+    assert torch.equal(wide, mure.sequences([40]).attend(q[0, :40], k[0, :40], v[0, :40], head_dim=dim, causal=False))

@@ -267,7 +267,6 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, DB <= 
 template <typename T, int DB> struct Short {
   using H = Head<T, DB>;
   static constexpr int KT = 32, WAVES = 4, TILE = KT * H::ROW;
-  static constexpr int PER = ATTN_KEYS_SHORT / WAVES;          // keys of a wave, where they are spread over the waves
   static constexpr int PITCH = 32 * DB + 4;                    // floats of a row of sums
   static constexpr int EACH = TILE > 16 * PITCH * 4 ? TILE : 16 * PITCH * 4;
   static constexpr int LDS = WAVES * EACH + WAVES * 16 * 2 * 4;
@@ -297,14 +296,15 @@ template <typename T, int DB, int FAST> struct ShortWave {
     for (int d = 0; d < 2 * DB; ++d) o[d] = v4f{};
   }
 
-  // Keys from ... to - 1, of which the lane's row sees lo ... hi - 1 and all of the sequence's rows all_lo ... all_hi - 1.
-  __device__ __forceinline__ void run(const Source<T>& src, const T* query, int n, float scale, int from, int to, int lo, int hi, int all_lo, int all_hi, char* tile, int lane) {
+  // Of keys from ... to - 1 the tiles at `first`, `step` further and so on, of which the lane's row sees keys lo ... hi - 1 and
+  // all of the sequence's rows all_lo ... all_hi - 1.
+  __device__ __forceinline__ void run(const Source<T>& src, const T* query, int n, float scale, int first, int step, int from, int to, int lo, int hi, int all_lo, int all_hi, char* tile, int lane) {
     constexpr float LOWEST = -__builtin_inff();
     const int quarter = lane >> 4;
     v4u q[STEPS];
     load_query<T, STEPS, 4>(q, query, n, quarter, scale);
     const float c = factor(scale);
-    for (int t = from / S::KT * S::KT; t < to; t += S::KT) {
+    for (int t = first; t < to; t += step) {
       const bool two = t + 16 < to;            // keys in the tile's second half
       // keys 16 b + l % 16; those behind the sequence's are hidden
       v4u keys[2][STEPS];
@@ -421,8 +421,8 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
   sees(a, unit * 16 / group, src.total, from, all_hi);
   sees(a, (unit * 16 + u.rows - 1) / group, src.total, all_lo, to);
   ShortWave<T, DB, FAST> sw;
-  sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale, from, to, lo,
-         hi, all_lo, all_hi, lds + wave * S::TILE, lane);
+  sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale,
+         from / S::KT * S::KT, S::KT, from, to, lo, hi, all_lo, all_hi, lds + wave * S::TILE, lane);
   if ((lane & 15) >= u.rows) return;
   T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (it.row0 + (int64_t)u.token) * a.out.row_stride + (int64_t)u.head * a.head_dim;
   const float f = 1.f / sw.l;
@@ -459,13 +459,15 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
   sees(a, src.total - 1, src.total, all_lo, to);
   const int64_t part0 = (int64_t)part * ATTN_KEYS_SHORT;
   if (max((int64_t)from, part0) >= min((int64_t)to, part0 + ATTN_KEYS_SHORT)) return;
-  from = (int)max((int64_t)from, part0 + wave * S::PER);
-  to = (int)min((int64_t)to, part0 + (wave + 1) * S::PER);
+  from = (int)max((int64_t)from, part0);
+  to = (int)min((int64_t)to, part0 + ATTN_KEYS_SHORT);
+  // the tiles go to the waves in turn, so that few keys are spread too
+  const int tile0 = from / S::KT, first = (tile0 + ((wave - tile0) & (S::WAVES - 1))) * S::KT;
   char* tile = lds + wave * S::EACH;
   ShortWave<T, DB, FAST> sw;
-  if (from < to)
-    sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale, from, to,
-           lo, hi, all_lo, all_hi, tile, lane);
+  if (first < to)
+    sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale, first,
+           S::WAVES * S::KT, from, to, lo, hi, all_lo, all_hi, tile, lane);
   // the waves' sums, added in order
   float* sums = reinterpret_cast<float*>(tile);
   float* ml = reinterpret_cast<float*>(lds + S::WAVES * S::EACH);              // [4][16][2]

@@ -407,31 +407,42 @@ template <typename T, int TM> hipError_t gated_split(const mure_attn_gated_args&
   return over_tiles(reinterpret_cast<const void*>(gated_split_kernel<T, TM>), a, sizeof(T), 16 * TM, 16, 64 * SPLIT, 0, s);
 }
 
+constexpr int64_t CUS = 256;
+
+// Whether the last round of blocks, of which a compute unit works on one at a time, is nearly full.
+bool fills(int64_t blocks) { return 6 * blocks >= 5 * ((blocks + CUS - 1) / CUS * CUS); }
+
+// Tiles of 128 rows by 64 outputs, in float32 of 64 rows where those leave the last round half empty: 2048 inputs to 1024
+// outputs, 3000 rows (384 tiles) 217 us so and 264 in tiles of 128; 512 to 1024, 2600 rows (336 tiles) 58 and 71.
+template <typename T, bool PARTS> hipError_t gated_tiles(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
+  constexpr int BYTES = sizeof(T) == 4 ? 64 : 128;             // 12500 rows of 16 mutants, 128 to 341 float32: 330 us, with 128 bytes 380
+  if constexpr (sizeof(T) == 4)
+    if (!fills((a.rows + 127) / 128 * ((a.outer + 63) / 64) * a.n_mutants)) return gated_f<T, 64, 64, 2, 2, BYTES, PARTS>(a, fast, s);
+  return gated_f<T, 128, 64, 2, 2, BYTES, PARTS>(a, fast, s);
+}
+
 // Which form, from the sizes (times in us).
-// Sums in eighths (`splits`), 2048 inputs to 512 outputs: side by side, or one after the other in tiles of 128 rows by 64
-//   outputs.  bfloat16: 64 rows 10 side by side (26 in tiles), 1000 rows 35 (27), 4000 rows 119 (30).  float32: 64 rows 21
-//   (139), 1000 rows 81 (139), 4000 rows 315 (155).  Without the eighths 16000 rows take 71 in place of 74 (float32: 520, 548).
+// Sums in eighths (`splits`), 2048 inputs to 512 outputs: side by side, or one after the other in tiles.  bfloat16: 64 rows 10
+//   side by side (26 in tiles), 1000 rows 35 (27), 4000 rows 119 (30).  float32: 64 rows 21 (139), 1000 rows 81 (88), 1200
+//   rows 100 (88), 2000 rows 160 (89).  Without the eighths 16000 rows take 71 in place of 74 (float32: 520, 548).
 // Otherwise, 2048 inputs to 5632 outputs: few rows with 8 or 16 outputs a block.  bfloat16: 64 rows 14 (tiles 26), 128 rows
-//   25 (26).  float32, whose products are slower, so that a tile takes long: 128 rows 73 (tiles 140).
+//   25 (26).  float32: 128 rows 73 (tiles 140), 170 rows 115 (147, two rounds of tiles); 1000 rows to 1024 outputs 90 (89).
+// A round of float32 tiles of 64 x 64 takes as long as these forms for 64 and 108 tiles' results of 128 x 64.
 // Larger tiles, of 256 rows by 128 outputs and bfloat16, take half the loads for a product, but one is all that a compute
 //   unit holds: where their last round is nearly full.  4096 inputs to 4096 outputs, 1024 rows (half a round) 99 (smaller
 //   tiles 69), 2048 rows (one round) 114 (137), 4096 rows 220 (260), 8192 rows 432 (511).
 template <typename T> hipError_t gated_t(const mure_attn_gated_args& a, bool fast, hipStream_t s) {
-  constexpr int BYTES = sizeof(T) == 4 ? 64 : 128;             // 12500 rows of 16 mutants, 128 to 341 float32: 330 us, with 128 bytes 380
-  constexpr int64_t CUS = 256;
-  const int64_t results = a.rows * a.outer * a.n_mutants;
+  const int64_t results = a.rows * a.outer * a.n_mutants / (128 * 64), small = (a.rows + 63) / 64 * ((a.outer + 63) / 64) * a.n_mutants, rounds = (small + CUS - 1) / CUS;
   if (splits<T>(a)) {
-    if (results >= (sizeof(T) == 4 ? 160 : 40) * 128 * 64) return gated_f<T, 128, 64, 2, 2, BYTES, true>(a, fast, s);
+    if (results >= (sizeof(T) == 4 ? 64 * rounds : 40)) return gated_tiles<T, true>(a, fast, s);
     return a.rows <= 16 ? gated_split<T, 1>(a, s) : gated_split<T, 2>(a, s);
   }
   if (a.rows <= 16) return gated_few<T, 1, 8, 4>(a, fast, s);
   if (a.rows <= 32) return gated_few<T, 2, 8, 4>(a, fast, s);
-  if (a.rows <= 64 || (sizeof(T) == 4 && results < 160 * 128 * 64)) return gated_few<T, 4, 16, 3>(a, fast, s);
-  if constexpr (sizeof(T) == 2) {
-    const int64_t tiles = (a.rows + 255) / 256 * ((a.outer + 127) / 128) * a.n_mutants;
-    if (6 * tiles >= 5 * ((tiles + CUS - 1) / CUS * CUS)) return gated_f<T, 256, 128, 2, 4, 128, false>(a, fast, s);
-  }
-  return gated_f<T, 128, 64, 2, 2, BYTES, false>(a, fast, s);
+  if (a.rows <= 64 || (sizeof(T) == 4 && results < 108 * rounds)) return gated_few<T, 4, 16, 3>(a, fast, s);
+  if constexpr (sizeof(T) == 2)
+    if (fills((a.rows + 255) / 256 * ((a.outer + 127) / 128) * a.n_mutants)) return gated_f<T, 256, 128, 2, 4, 128, false>(a, fast, s);
+  return gated_tiles<T, false>(a, fast, s);
 }
 
 }  // namespace

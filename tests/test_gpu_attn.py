@@ -272,3 +272,18 @@ def test_gated_long_sums(mure, dtype, K, N):
     odd = torch.zeros(300, K + 1, dtype=dt, device="cuda")
     odd[:, 1:] = x[:300]
     assert torch.equal(mure.gated(odd[:, 1:], gate, up, gate_bias=bias, activation="gelu"), whole[0, :300])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,K,N,M", [(2600, 72, 1024, 1), (4000, 71, 1024, 1), (2000, 72, 4100, 1), (2050, 71, 4090, 1), (900, 72, 1000, 3), (300, 71, 600, 20)])
+def test_gated_forms(mure, dtype, rows, K, N, M):
+    """Tiles of every size, their last rows and outputs included: the bits of few rows, and the definition's values."""
+    say(f"[gated forms] {dtype} {rows} x {K} -> {N}, {M}")
+    g = torch.Generator().manual_seed(11)
+    dt = TYPES[dtype]
+    x, gate, up = normal(g, 1, rows, K, dtype=dt), normal(g, M, N, K, dtype=dt, std=K ** -0.5), normal(g, M, N, K, dtype=dt, std=K ** -0.5)
+    gx, gg, gu = cuda(x[0], gate, up)
+    whole = mure.gated(gx, gg, gu)
+    for first, n in ((0, 16), (rows - 50, 50), (rows // 2, 30), (rows - 1, 1)):
+        assert torch.equal(mure.gated(gx[first:first + n], gg, gu), whole[:, first:first + n]), (first, n)
+    R.close(whole[:, -40:], R.gated(x[:, -40:], gate, up), "out")

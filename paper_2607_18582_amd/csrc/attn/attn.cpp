@@ -166,8 +166,9 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   const auto launch_runs = f32 ? attn_runs_f32 : attn_runs_bf16;
   const auto launch_join = f32 ? attn_join_f32 : attn_join_bf16;
   // Items over a cache whose keys are in parts, joined from the workspace: as many items at a time as it has room for.
-  auto parted = [&](const SeqItem* items, int n, int64_t parts, int rows_each, int keys, auto run) {
+  auto parted = [&](const SeqItem* items, int first, int n, int64_t parts, int rows_each, int keys, auto run) {
     AttnArgs p = k;
+    p.items = items;
     p.parts = (int)parts;
     p.rows_each = p.longest = rows_each;
     int most = n;
@@ -181,7 +182,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
       p.ws_o = p.ws_ml + 2 * rows * most;
     }
     for (int i = 0; i < n; i += most) {
-      p.items = items ? items + i : nullptr;
+      p.first = first + i;
       p.n_items = std::min(most, n - i);
       check(run(p, s->stream), "mure_attn_attend");
       if (parts > 1) check(launch_join(p, keys, s->stream), "mure_attn_attend");
@@ -206,7 +207,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   }
   // one after the other: the workspace serves all
   if (s->n_short)
-    parted(s->brief ? s->brief + (s->n_brief - s->n_short) : nullptr, s->n_short, parts_short, std::min(s->longest_brief, ATTN_SHORT), ATTN_KEYS_SHORT, launch_short);
+    parted(s->brief, s->n_brief - s->n_short, s->n_short, parts_short, std::min(s->longest_brief, ATTN_SHORT), ATTN_KEYS_SHORT, launch_short);
   // without parts the longer sequences' runs and the others' go in one launch
   const int n_mid = s->n_runs - s->n_long_runs;
   const bool split = parts_mid > 1 && n_mid;
@@ -216,7 +217,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
     p.n_items = split ? s->n_long_runs : s->n_runs;
     check(launch_runs(p, s->stream), "mure_attn_attend");
   }
-  if (split) parted(s->runs ? s->runs + s->n_long_runs : nullptr, n_mid, parts_mid, ATTN_ROWS, ATTN_KEYS_MID, launch_runs);
+  if (split) parted(s->runs, s->n_long_runs, n_mid, parts_mid, ATTN_ROWS, ATTN_KEYS_MID, launch_runs);
 }
 
 // ---- gated feed-forward layer

@@ -26,8 +26,8 @@ enum AttnReads : int { ELEMENTS, WORDS, PIECES };
 
 struct AttnArgs {
   mure_attn_attend_args a;
-  const SeqItem* items = nullptr;
-  int n_items = 0, item0 = 0;
+  const SeqItem* items = nullptr;              // a list (nullptr: all sequences, one token each), of which items first ... first + n_items - 1
+  int first = 0, n_items = 0, item0 = 0;       // item0: of a launch, counted from `first` as the workspace's rows are
   int longest = 0;                             // tokens of an item, at most
   int rows_each = 0;                           // rows of the workspace that an item has
   int parts = 1;                               // of the keys

@@ -58,7 +58,7 @@ template <typename T> struct Source {
 __device__ __forceinline__ void settle() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ SeqItem item_of(const AttnArgs& k, int i) {
-  const SeqItem it = seq_item(k.items, i);
+  const SeqItem it = seq_item(k.items, k.first + i);
   return {uniform(it.seq), uniform(it.row0), uniform(it.len), uniform(it.pos0), uniform(it.total), it.slot};
 }
 

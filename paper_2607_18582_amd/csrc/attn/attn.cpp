@@ -12,7 +12,7 @@ using namespace mure;
 namespace {
 
 constexpr int64_t GRID = (1 << 24) - 1;        // blocks of a launch: a grid has fewer than 2^32 threads
-constexpr int64_t PARTS_BYTES = 1 << 30;       // of a workspace for parts of keys, or as many as one sequence's run needs
+constexpr int64_t PARTS_BYTES = 1 << 30;       // of a workspace for parts of keys, or as many as one head's run needs
 
 // ---- norm and rotation
 
@@ -106,6 +106,24 @@ bool aligned(int64_t bytes, const void* p, int64_t es, std::initializer_list<int
   return ok;
 }
 
+// The call's mutants m0 ... m0 + ms - 1 and heads h0 ... h0 + hs - 1 of them: whole groups, or some of one.
+AttnArgs some_of(const AttnArgs& k, int64_t es, int64_t m0, int64_t ms, int64_t h0, int64_t hs) {
+  AttnArgs p = k;
+  const mure_attn_attend_args& a = k.a;
+  const int64_t group = a.heads / a.kv_heads, g0 = h0 / group, D = a.head_dim;
+  const auto move = [&](auto& rows, int64_t head) {
+    if (rows.p) rows.p = const_cast<char*>(static_cast<const char*>(rows.p)) + (m0 * rows.mutant_stride + head * D) * es;
+  };
+  move(p.a.q, h0);
+  move(p.a.out, h0);
+  for (mure_seq_in* t : {&p.a.k, &p.a.v}) move(*t, g0);
+  for (mure_attn_cache* t : {&p.a.k_cache, &p.a.v_cache}) move(*t, g0);
+  p.a.n_mutants = (int32_t)ms;
+  p.a.heads = (int32_t)hs;
+  p.a.kv_heads = (int32_t)std::max<int64_t>(1, hs / group);
+  return p;
+}
+
 void attend(mure_seq* s, const mure_attn_attend_args* args) {
   if (!args) invalid("args is NULL");
   AttnArgs k;
@@ -165,27 +183,39 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   const auto launch_short = f32 ? attn_short_f32 : attn_short_bf16;
   const auto launch_runs = f32 ? attn_runs_f32 : attn_runs_bf16;
   const auto launch_join = f32 ? attn_join_f32 : attn_join_bf16;
-  // Items over a cache whose keys are in parts, joined from the workspace: as many items at a time as it has room for.
-  auto parted = [&](const SeqItem* items, int first, int n, int64_t parts, int rows_each, int keys, auto run) {
-    AttnArgs p = k;
-    p.items = items;
-    p.parts = (int)parts;
-    p.rows_each = p.longest = rows_each;
-    int most = n;
+  // Items over a cache whose keys are in parts, joined from the workspace: as many items at a time as it has room for, or of
+  // one item as many mutants, or heads.
+  auto parted = [&](const SeqItem* items, int first, int n, int64_t parts, int64_t rows_each, int keys, auto run) {
+    const int64_t group = a.heads / a.kv_heads;
+    int64_t most = n, mutants = M, heads = a.heads;
+    float* work = nullptr;
+    int64_t slots = 0;
     if (parts > 1) {
-      const wide rows = (wide)M * rows_each * a.heads * parts, each = rows * (D + 2) * 4;
-      if (each > MOST) throw Fail{MURE_E_NOMEM, "attention workspace"};
-      most = (int)std::max<wide>(1, std::min<wide>(n, PARTS_BYTES / each));
-      void* work = nullptr;
-      check(s->work.get(s->stream, (size_t)(each * most), &work), "attention workspace");
-      p.ws_ml = static_cast<float*>(work);
-      p.ws_o = p.ws_ml + 2 * rows * most;
+      const int64_t each = rows_each * parts * (D + 2) * 4;    // of an item, mutant and head
+      const int64_t fit = std::max<int64_t>(1, PARTS_BYTES / each);
+      if (fit < heads) heads = fit < group ? fit : fit / group * group, mutants = most = 1;
+      else if (fit < heads * M) mutants = fit / heads, most = 1;
+      else most = std::min(most, fit / (heads * M));
+      slots = most * mutants * heads * rows_each * parts;
+      void* p = nullptr;
+      check(s->work.get(s->stream, (size_t)(slots * (D + 2) * 4), &p), "attention workspace");
+      work = static_cast<float*>(p);
     }
-    for (int i = 0; i < n; i += most) {
-      p.first = first + i;
-      p.n_items = std::min(most, n - i);
-      check(run(p, s->stream), "mure_attn_attend");
-      if (parts > 1) check(launch_join(p, keys, s->stream), "mure_attn_attend");
+    for (int64_t h0 = 0, hs; h0 < a.heads; h0 += hs) {
+      hs = heads < group ? std::min(heads, group - h0 % group) : std::min(heads, a.heads - h0);
+      for (int64_t m0 = 0; m0 < M; m0 += mutants)
+        for (int64_t i = 0; i < n; i += most) {
+          AttnArgs p = some_of(k, es, m0, std::min(mutants, M - m0), h0, hs);
+          p.items = items;
+          p.parts = (int)parts;
+          p.rows_each = p.longest = (int)rows_each;
+          p.ws_ml = work;
+          p.ws_o = work + 2 * slots;
+          p.first = (int)(first + i);
+          p.n_items = (int)std::min(most, n - i);
+          check(run(p, s->stream), "mure_attn_attend");
+          if (parts > 1) check(launch_join(p, keys, s->stream), "mure_attn_attend");
+        }
     }
   };
   if (!held) {

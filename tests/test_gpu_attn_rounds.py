@@ -45,3 +45,40 @@ def test_single_tokens_in_three_rounds(mure, dtype):
     assert not wrong
     assert all(torch.equal(c, a) for c, a in zip(cache, alone))
     assert all(torch.equal(c[torch.arange(n), past.long()], new) for c, new in zip(cache, (k, v)))
+
+
+def free_bytes():
+    torch.cuda.synchronize()
+    return torch.cuda.mem_get_info()[0]
+
+
+@pytest.mark.parametrize("lengths,M,H,G,dim,rows", [
+    ([130], 200, 16, 2, 8, 131072),            # 2.1 GB of parts: mutants in rounds
+    ([130], 1, 1024, 2, 4, 400000),            # 0.6 GB a group of heads: groups in rounds
+    ([130], 1, 1024, 1, 4, 400000),            # ... which are one: heads in rounds
+    ([16], 1, 1024, 1, 64, 300000)])           # the same of a short sequence, tokens and heads in one unit of rows
+def test_one_sequence_in_several_rounds(lengths, M, H, G, dim, rows):
+    """The workspace stays within 1 GiB where one sequence's parts take more."""
+    say(f"[rounds, one sequence] {lengths} M={M} H={H} G={G} dim={dim} rows={rows}")
+    mure = Mure(device=0)
+    g = torch.Generator(device="cuda").manual_seed(51)
+    n, past = lengths[0], torch.tensor([2500], dtype=torch.int32, device="cuda")
+    q = rand(g, M, n, H * dim, dtype=torch.bfloat16)
+    k, v = (rand(g, n, G * dim, dtype=torch.bfloat16) for _ in range(2))
+    cache = [rand(g, 1, rows, G * dim, dtype=torch.bfloat16) for _ in range(2)]
+    before = [c.clone() for c in cache]
+    out = torch.full_like(q, 77.0)
+    seqs = mure.sequences(lengths)
+    free = free_bytes()
+    seqs.attend(q, k, v, head_dim=dim, cache=cache, past=past, out=out)
+    assert free - free_bytes() <= (1 << 30) + (64 << 20)
+    for c, b, new in zip(cache, before, (k, v)):
+        b[0, 2500:2500 + n] = new
+        assert torch.equal(c, b)
+    # every mutant's heads alone
+    for m in range(M):
+        for h in {0, 1, H // 4, H // 2 - 1, H // 2, H - 2, H - 1}:
+            at, kv = slice(h * dim, (h + 1) * dim), slice(h // (H // G) * dim, (h // (H // G) + 1) * dim)
+            alone = seqs.attend(q[m, :, at], k[:, kv], v[:, kv], head_dim=dim, cache=[b[..., kv] for b in before], past=past)
+            assert torch.equal(out[m, :, at], alone), (m, h)
+    mure.close()

@@ -237,7 +237,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   }
   // one after the other: the workspace serves all
   if (s->n_short)
-    parted(s->brief, s->n_brief - s->n_short, s->n_short, parts_short, std::min(s->longest_brief, ATTN_SHORT), ATTN_KEYS_SHORT, launch_short);
+    parted(s->brief, s->n_brief - s->n_short, s->n_short, parts_short, s->longest_short, ATTN_KEYS_SHORT, launch_short);
   // without parts the longer sequences' runs and the others' go in one launch
   const int n_mid = s->n_runs - s->n_long_runs;
   const bool split = parts_mid > 1 && n_mid;
@@ -247,7 +247,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
     p.n_items = split ? s->n_long_runs : s->n_runs;
     check(launch_runs(p, s->stream), "mure_attn_attend");
   }
-  if (split) parted(s->runs, s->n_long_runs, n_mid, parts_mid, ATTN_ROWS, ATTN_KEYS_MID, launch_runs);
+  if (split) parted(s->runs, s->n_long_runs, n_mid, parts_mid, s->longest_mid_run, ATTN_KEYS_MID, launch_runs);
 }
 
 // ---- gated feed-forward layer

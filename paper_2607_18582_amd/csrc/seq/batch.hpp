@@ -74,13 +74,14 @@ struct mure_seq {
   const mure::SeqChunks* chunked = nullptr;
   int n_chunked = 0;
   int64_t n_slots = 0;
-  // attention: sequences of at most ATTN_WHOLE tokens, the longest first (the last n_short have at most ATTN_SHORT); runs of
+  // attention: sequences of at most ATTN_WHOLE tokens, the longest first (the last n_short have at most ATTN_SHORT, the first of
+  // those longest_short); runs of
   // ATTN_ROWS tokens of those above ATTN_SHORT: of sequences above ATTN_MID (n_long_runs), above ATTN_WHOLE, the others
   // (n_small_runs), and in each the last runs of the longest first
   const mure::SeqItem* brief = nullptr;
-  int n_brief = 0, n_short = 0, longest_brief = 0;
+  int n_brief = 0, n_short = 0, longest_brief = 0, longest_short = 0;
   const mure::SeqItem* runs = nullptr;
-  int n_runs = 0, n_long_runs = 0, n_small_runs = 0;
+  int n_runs = 0, n_long_runs = 0, n_small_runs = 0, longest_mid_run = 0;      // the last: tokens, of sequences up to ATTN_MID
   mure::SeqWorkspace<mure::SeqApi> work;          // the chunks' states, attention over parts of the keys
 };
 

@@ -73,12 +73,16 @@ void create(mure_ctx* ctx, int64_t n_seq, const int64_t* lengths, mure_seq** out
     if (L <= ATTN_WHOLE) {
       add_runs(brief, i, row, L, L, -1);
       s->longest_brief = std::max(s->longest_brief, (int)L);
-      s->n_short += L <= ATTN_SHORT;
+      if (L <= ATTN_SHORT) {
+        s->n_short += 1;
+        s->longest_short = std::max(s->longest_short, (int)L);
+      }
     }
     if (L > ATTN_SHORT) {
       add_runs(runs, i, row, L, ATTN_ROWS, -1);
       s->n_small_runs += L <= ATTN_WHOLE;
       if (L > ATTN_MID) s->n_long_runs += (int)((L + ATTN_ROWS - 1) / ATTN_ROWS);
+      else s->longest_mid_run = std::max(s->longest_mid_run, (int)std::min<int64_t>(L, ATTN_ROWS));
     }
   }
   std::stable_sort(brief.begin(), brief.end(), [](const SeqItem& a, const SeqItem& b) { return a.len > b.len; });

@@ -82,3 +82,22 @@ def test_one_sequence_in_several_rounds(lengths, M, H, G, dim, rows):
             alone = seqs.attend(q[m, :, at], k[:, kv], v[:, kv], head_dim=dim, cache=[b[..., kv] for b in before], past=past)
             assert torch.equal(out[m, :, at], alone), (m, h)
     mure.close()
+
+
+def test_a_workspace_of_the_rows_that_there_are():
+    """A batch of single tokens beside one of 50, and of 17 tokens: parts of as many rows as their sequences have."""
+    say("[rounds, rows]")
+    mure = Mure(device=0)
+    g = torch.Generator(device="cuda").manual_seed(52)
+    H, dim, rows = 32, 64, 65536
+    # bytes of 128 parts of 512 keys or 64 of 1024, 66 floats a part and head
+    for lengths, need in (([1] * 40 + [50], 40 * 32 * 128 * 66 * 4 + 50 * 32 * 64 * 66 * 4), ([17] * 20, 20 * 17 * 32 * 64 * 66 * 4)):
+        T, n = sum(lengths), len(lengths)
+        q, k, v = rand(g, T, H * dim, dtype=torch.bfloat16), rand(g, T, dim, dtype=torch.bfloat16), rand(g, T, dim, dtype=torch.bfloat16)
+        cache = [torch.zeros(n, rows, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        past, out, seqs = torch.full((n,), 600, dtype=torch.int32, device="cuda"), torch.empty_like(q), mure.sequences(lengths)
+        free = free_bytes()
+        seqs.attend(q, k, v, head_dim=dim, cache=cache, past=past, out=out)
+        assert free - free_bytes() <= need + (64 << 20), lengths
+        del cache
+    mure.close()

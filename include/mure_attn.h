@@ -38,6 +38,7 @@ extern "C" {
 #define MURE_ATTN_MAX_HEAD 256     /* channels of a head */
 #define MURE_ATTN_MAX_HEADS 1024
 #define MURE_ATTN_MAX_AXES 4       /* axes of a position */
+#define MURE_ATTN_MAX_ROWS (1 << 30)   /* rows of a sequence's cache */
 
 /* Norm and rotation of queries and keys.  For every token and head, with
  * v = norm(head's channels) (norm: MURE_SEQ_NO_NORM, MURE_SEQ_RMS or
@@ -97,7 +98,8 @@ typedef struct {
   int32_t reserved;
   mure_seq_in q, k, v;
   mure_attn_cache k_cache, v_cache;
-  int64_t capacity;                  /* rows of a sequence's cache, 1 .. 2^31 - 1 */
+  int64_t capacity;                  /* rows of a sequence's cache, 1 .. 2^31 - 1; more than
+                                        MURE_ATTN_MAX_ROWS: MURE_E_UNSUPPORTED */
   const int32_t* past;               /* [n_seq], device memory, optional */
   mure_seq_out out;
 } mure_attn_attend_args;

@@ -165,12 +165,10 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   } else {
     a.capacity = 0;
   }
-  // blocks of an item: (heads or groups' row tiles) x mutants x parts
   const int64_t parts_short = held ? (a.capacity + ATTN_KEYS_SHORT - 1) / ATTN_KEYS_SHORT : 1;
   const int64_t parts_mid = held ? (a.capacity + ATTN_KEYS_MID - 1) / ATTN_KEYS_MID : 1;
-  if ((wide)a.heads * M * std::max(std::max(parts_short * ATTN_SHORT, parts_mid), (int64_t)ATTN_WHOLE) > GRID)
-    throw Fail{MURE_E_UNSUPPORTED, "too many heads times mutants times parts of the cache"};
-  if ((wide)M * s->n_brief > INT32_MAX || (wide)M * s->n_runs > INT32_MAX) throw Fail{MURE_E_UNSUPPORTED, "too many sequences times mutants"};
+  // the kernels count keys, and the blocks of one head's parts, in 32 bits
+  if (a.capacity > MURE_ATTN_MAX_ROWS) throw Fail{MURE_E_UNSUPPORTED, "too many rows of a cache: 2^30 at most"};
   check_device(s->device);
   if (T == 0) return;
   const auto reads = [&](int64_t bytes) {
@@ -183,20 +181,28 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   const auto launch_short = f32 ? attn_short_f32 : attn_short_bf16;
   const auto launch_runs = f32 ? attn_runs_f32 : attn_runs_bf16;
   const auto launch_join = f32 ? attn_join_f32 : attn_join_bf16;
-  // Items over a cache whose keys are in parts, joined from the workspace: as many items at a time as it has room for, or of
-  // one item as many mutants, or heads.
-  auto parted = [&](const SeqItem* items, int first, int n, int64_t parts, int64_t rows_each, int keys, auto run) {
+  // Items of at most `longest` tokens, their keys in parts of `keys`: as many mutants and heads a round as one item may have
+  // blocks for; with several parts, which are joined from the workspace, as many items as it has room for, or of one
+  // item as many mutants, or heads.  `blocks`: of an item, mutants and heads.
+  auto rounds = [&](const SeqItem* items, int first, int n, int64_t parts, int64_t longest, int keys, auto run, auto blocks) {
     const int64_t group = a.heads / a.kv_heads;
-    int64_t most = n, mutants = M, heads = a.heads;
+    int64_t most = n, mutants = M, heads = a.heads;            // a round's
+    if (n == 0) return;
     float* work = nullptr;
     int64_t slots = 0;
     if (parts > 1) {
-      const int64_t each = rows_each * parts * (D + 2) * 4;    // of an item, mutant and head
+      const int64_t each = longest * parts * (D + 2) * 4;      // of an item, mutant and head
       const int64_t fit = std::max<int64_t>(1, PARTS_BYTES / each);
       if (fit < heads) heads = fit < group ? fit : fit / group * group, mutants = most = 1;
       else if (fit < heads * M) mutants = fit / heads, most = 1;
       else most = std::min(most, fit / (heads * M));
-      slots = most * mutants * heads * rows_each * parts;
+    }
+    if (blocks(mutants, heads) > GRID) {
+      while (blocks(1, heads) > GRID) heads = heads > group ? (heads / group + 1) / 2 * group : (heads + 1) / 2;
+      mutants = std::min(mutants, GRID / blocks(1, heads));
+    }
+    if (parts > 1) {
+      slots = most * mutants * heads * longest * parts;
       void* p = nullptr;
       check(s->work.get(s->stream, (size_t)(slots * (D + 2) * 4), &p), "attention workspace");
       work = static_cast<float*>(p);
@@ -208,7 +214,7 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
           AttnArgs p = some_of(k, es, m0, std::min(mutants, M - m0), h0, hs);
           p.items = items;
           p.parts = (int)parts;
-          p.rows_each = p.longest = (int)rows_each;
+          p.rows_each = p.longest = (int)longest;
           p.ws_ml = work;
           p.ws_o = work + 2 * slots;
           p.first = (int)(first + i);
@@ -218,36 +224,26 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
         }
     }
   };
+  const int64_t group = a.heads / a.kv_heads;
+  const auto run_blocks = [](int64_t parts) { return [=](int64_t mutants, int64_t heads) { return mutants * heads * parts; }; };
+  const auto short_blocks = [&](int64_t longest, int64_t parts) {
+    return [=](int64_t mutants, int64_t heads) {
+      const int64_t shared = std::min(group, heads);
+      return mutants * (heads / shared) * ((longest * shared + 15) / 16) * parts;
+    };
+  };
   if (!held) {
-    if (s->n_brief) {
-      AttnArgs p = k;
-      p.items = s->brief;
-      p.n_items = s->n_brief;
-      p.longest = s->longest_brief;
-      check(launch_short(p, s->stream), "mure_attn_attend");
-    }
-    const int n_runs = s->n_runs - s->n_small_runs;
-    if (n_runs) {
-      AttnArgs p = k;
-      p.items = s->runs;
-      p.n_items = n_runs;
-      check(launch_runs(p, s->stream), "mure_attn_attend");
-    }
+    rounds(s->brief, 0, s->n_brief, 1, s->longest_brief, 0, launch_short, short_blocks(s->longest_brief, 1));
+    rounds(s->runs, 0, s->n_runs - s->n_small_runs, 1, ATTN_ROWS, 0, launch_runs, run_blocks(1));
     return;
   }
   // one after the other: the workspace serves all
-  if (s->n_short)
-    parted(s->brief, s->n_brief - s->n_short, s->n_short, parts_short, s->longest_short, ATTN_KEYS_SHORT, launch_short);
+  rounds(s->brief, s->n_brief - s->n_short, s->n_short, parts_short, s->longest_short, ATTN_KEYS_SHORT, launch_short, short_blocks(s->longest_short, parts_short));
   // without parts the longer sequences' runs and the others' go in one launch
   const int n_mid = s->n_runs - s->n_long_runs;
   const bool split = parts_mid > 1 && n_mid;
-  if (split ? s->n_long_runs : s->n_runs) {
-    AttnArgs p = k;
-    p.items = s->runs;
-    p.n_items = split ? s->n_long_runs : s->n_runs;
-    check(launch_runs(p, s->stream), "mure_attn_attend");
-  }
-  if (split) parted(s->runs, s->n_long_runs, n_mid, parts_mid, s->longest_mid_run, ATTN_KEYS_MID, launch_runs);
+  rounds(s->runs, 0, split ? s->n_long_runs : s->n_runs, 1, ATTN_ROWS, 0, launch_runs, run_blocks(1));
+  if (split) rounds(s->runs, s->n_long_runs, n_mid, parts_mid, s->longest_mid_run, ATTN_KEYS_MID, launch_runs, run_blocks(parts_mid));
 }
 
 // ---- gated feed-forward layer

@@ -1,0 +1,50 @@
+"""The operators of an attention block on the host, at their limits: calls of
+many mutants, heads, sequences and rows that a cache may have reach the device."""
+import pytest
+
+from paper_2607_18582_amd import MURE_E_INVALID, MURE_E_UNSUPPORTED, Mure
+from test_attn_host import Buffers, attend_args, call, put
+
+
+@pytest.fixture()
+def mure():
+    m = Mure(device=-1)
+    yield m
+    m.close()
+
+
+def apart(a, rows):
+    """Caches of `rows` rows one behind the other, everything else behind them: nothing is read there."""
+    width, n = a.kv_heads * a.head_dim, 3
+    a.capacity = rows
+    for c in (a.k_cache, a.v_cache):
+        c.row_stride, c.seq_stride, c.mutant_stride = width, rows * width, 0
+    for t in (a.k, a.v):
+        t.mutant_stride = 0
+    a.v_cache.p = a.k_cache.p + n * 2 * rows * width
+    for i, name in enumerate(("q", "k", "v", "past", "out")):
+        put(a, name if name == "past" else name + ".p", a.v_cache.p + (1 << 42) + i * (1 << 36))
+
+
+@pytest.mark.parametrize("mutants,heads,kv_heads,dim,rows", [
+    (128, 32, 8, 128, 131072), (32, 64, 64, 64, 262144), (65535, 4, 4, 8, 4096), (1, 1024, 1, 256, 1 << 30), (65535, 1024, 1024, 1, 1 << 20)])
+@pytest.mark.parametrize("cache", [True, False])
+def test_many_blocks(mure, mutants, heads, kv_heads, dim, rows, cache):
+    a = attend_args(Buffers())
+    a.n_mutants, a.heads, a.kv_heads, a.head_dim = mutants, heads, kv_heads, dim
+    a.q.row_stride = a.out.row_stride = heads * dim
+    a.q.mutant_stride = a.out.mutant_stride = 7 * heads * dim
+    a.k.row_stride = a.v.row_stride = kv_heads * dim
+    apart(a, rows)
+    if not cache:
+        a.k_cache.p = a.v_cache.p = a.past = None
+    st, msg = call(mure, "attend", a)
+    assert st == MURE_E_UNSUPPORTED and "planning-only" in msg, msg
+
+
+def test_rows_of_a_cache(mure):
+    a = attend_args(Buffers())
+    for rows, status, word in ((1 << 30, MURE_E_UNSUPPORTED, "planning-only"), ((1 << 30) + 1, MURE_E_UNSUPPORTED, "too many rows"), (1 << 31, MURE_E_INVALID, "capacity")):
+        apart(a, rows)
+        st, msg = call(mure, "attend", a)
+        assert st == status and word in msg, (rows, msg)

@@ -101,3 +101,30 @@ def test_a_workspace_of_the_rows_that_there_are():
         assert free - free_bytes() <= need + (64 << 20), lengths
         del cache
     mure.close()
+
+
+def test_more_blocks_than_a_launch(mure):
+    """Many mutants of few tokens, without a cache and over a long one: as many mutants a launch as it has blocks for."""
+    say("[rounds, blocks]")
+    g = torch.Generator(device="cuda").manual_seed(53)
+    M, H, dim = 65535, 4, 2
+    lengths = [1, 3]
+    q, k, v = (rand(g, M, 4, H * dim) for _ in range(3))
+    out = mure.sequences(lengths).attend(q, k, v, head_dim=dim)
+    for m in (0, 1, 30000, M - 1):
+        assert torch.equal(out[m], mure.sequences(lengths).attend(q[m], k[m], v[m], head_dim=dim)), m
+    lengths = [97]
+    q, k, v = (rand(g, M, 97, w * dim, dtype=torch.bfloat16) for w in (257, 1, 1))
+    out = mure.sequences(lengths).attend(q, k, v, head_dim=dim)
+    for m in (0, 1, 30000, M - 1):
+        assert torch.equal(out[m], mure.sequences(lengths).attend(q[m], k[m], v[m], head_dim=dim)), m
+    del q, k, v, out
+    M, H, G, rows = 128, 32, 8, 131072
+    q, (k, v) = rand(g, M, 3, H * dim), (rand(g, 3, G * dim) for _ in range(2))
+    cache = [rand(g, 3, rows, G * dim) for _ in range(2)]
+    past = torch.tensor([rows - 1, 5, 40000], dtype=torch.int32, device="cuda")
+    alone = [c.clone() for c in cache]
+    out = mure.sequences([1, 1, 1]).attend(q, k, v, head_dim=dim, cache=cache, past=past)
+    for m in (0, 1, 77, M - 1):
+        assert torch.equal(out[m], mure.sequences([1, 1, 1]).attend(q[m], k, v, head_dim=dim, cache=alone, past=past)), m
+    assert all(torch.equal(c, a) for c, a in zip(cache, alone))

@@ -53,7 +53,7 @@ extern "C" {
  * turn by axis x's position, in order (their sum is rotated / 2).
  * Angles are products in float64; they are good to float32 up to 2^33.
  * dtype: of q, k and their outputs; rows of q_heads * head_dim and
- * k_heads * head_dim channels.  k_heads = 0: no keys.  frequencies: float32
+ * k_heads * head_dim channels.  k_heads = 0: no keys, no k_weight.  frequencies: float32
  * [rotated / 2], rotated even, <= head_dim (0: none turns).  q_weight, k_weight: [head_dim],
  * optional.  q_out may be q and k_out may be k (same pointer and strides, not
  * shared by several mutants). */

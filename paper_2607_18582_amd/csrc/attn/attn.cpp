@@ -32,6 +32,7 @@ void rotate(mure_seq* s, const mure_attn_rotate_args* args) {
   check_range(a.interleaved, 0, 1, "interleaved");
   if (!(a.eps >= 0.f) || !std::isfinite(a.eps)) invalid("eps is no finite value >= 0");
   if (!a.norm && (a.q_weight.p || a.k_weight.p)) invalid("a weight without a norm");
+  if (!a.k_heads && a.k_weight.p) invalid("k_weight without keys");
   const int64_t M = a.n_mutants, D = a.head_dim, T = s->tokens;
   if (a.positions) {
     check_range(a.axes, 1, MURE_ATTN_MAX_AXES, "axes");

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(AttnRotateArgs k, int t
   extern __shared__ float2 turn[];             // [tokens][pairs]
   const mure_attn_rotate_args& a = k.a;
   const int m = blockIdx.x % a.n_mutants, item = k.item0 + blockIdx.x / a.n_mutants, tid = threadIdx.x;
-  const int begin = gridDim.y == 1 ? 0 : blockIdx.y, end = gridDim.y == 1 ? 2 : begin + 1;    // of queries and keys
+  const int begin = gridDim.y == 1 ? 0 : blockIdx.y, end = gridDim.y > 1 ? begin + 1 : a.k_heads ? 2 : 1;     // of queries and keys
   const SeqItem it = seq_item(k.items, item);
   const int pairs = a.rotated / 2, D = a.head_dim;
   const float* freq = a.frequencies.p + m * a.frequencies.mutant_stride;

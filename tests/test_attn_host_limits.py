@@ -1,9 +1,10 @@
 """The operators of an attention block on the host, at their limits: calls of
-many mutants, heads, sequences and rows that a cache may have reach the device."""
+as many mutants, heads and rows as they may have reach the device, and what is
+not there is not read."""
 import pytest
 
 from paper_2607_18582_amd import MURE_E_INVALID, MURE_E_UNSUPPORTED, Mure
-from test_attn_host import Buffers, attend_args, call, put
+from test_attn_host import Buffers, attend_args, call, put, rotate_args
 
 
 @pytest.fixture()
@@ -48,3 +49,17 @@ def test_rows_of_a_cache(mure):
         apart(a, rows)
         st, msg = call(mure, "attend", a)
         assert st == status and word in msg, (rows, msg)
+
+
+@pytest.mark.parametrize("p", [None, "keys"])
+def test_a_weight_of_keys_that_are_not_there(mure, p):
+    """Nothing checks such a weight's address, so nothing may read it."""
+    a = rotate_args(Buffers())
+    a.k_heads = 0
+    a.k.p = a.k_out.p = None
+    a.k_weight.p = 8 if p else None
+    st, msg = call(mure, "rotate", a)
+    if p:
+        assert st == MURE_E_INVALID and "k_weight without" in msg, msg
+    else:
+        assert st == MURE_E_UNSUPPORTED and "planning-only" in msg, msg

@@ -87,7 +87,8 @@ typedef struct {
  * past[i] + length(i) > capacity, the sequence's results are NaN and its
  * caches are left alone.  Rows of a cache that hold no key are not read.
  * What is NaN or infinite goes on by the arithmetic of the formula to those
- * tokens that see it, and to no other.
+ * tokens that see it, and to no other: an infinite value makes a token's result
+ * infinite (or NaN, beside one of the other sign) however small its weight is.
  * dtype: of q, k, v, the caches and out.  All mutants may share a cache
  * (mutant stride 0) where they share k and v too.  k_cache and v_cache overlap
  * no other tensor and no row of their own. */

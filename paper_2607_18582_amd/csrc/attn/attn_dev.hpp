@@ -548,6 +548,50 @@ __device__ __forceinline__ void add_nonfinite(const Rows<T>& rows, int t0, int f
   }
 }
 
+// Stored sums of a row that are NaN although its weights are numbers, taken again: a weight that is 0 in float32 and not in
+// the formula makes NaN of an infinite value.  What is not finite counts by itself here, whatever its weight is (0 only
+// where the score is -inf); without such a value the sum stays NaN: finite ones have passed float32.  Keys lo ... hi - 1 of
+// the tiles of `width` at `first`, `step` further and so on; N sums a lane, at out[channel(i, lane)].
+template <int N, typename T, typename O, typename F>
+__device__ __forceinline__ void renew(O* out, const Rows<T>& keys, const Rows<T>& values, const T* query, float scale, int n, int first, int step, int width, int lo, int hi, int lane,
+                                      F&& channel) {
+  constexpr float INF = __builtin_inff();
+  constexpr int EACH = 8;                      // values on their way at a time
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // the stores
+#pragma unroll 1
+  for (int i = 0; i < N; ++i) {
+    const int c = channel(i, lane);
+    if (c >= n) continue;
+    const float y = to_f<O>(out[c]);
+    if (y == y) continue;
+    float sum = 0.f;
+#pragma unroll 1
+    for (int t = first; t < hi && sum == sum; t += step)
+#pragma unroll 1
+      for (int key0 = max(t, lo), end = min(t + width, hi); key0 < end && sum == sum; key0 += EACH) {
+        bool here = false;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) here |= !(fabsf(to_f<T>(values.at(min(key0 + j, end - 1))[c])) < INF);
+        if (!here) continue;
+#pragma unroll 1
+        for (int key = key0; key < min(key0 + EACH, end); ++key) {
+          const float v = to_f<T>(values.at(key)[c]);
+          if (fabsf(v) < INF) continue;
+          const T* p = keys.at(key);
+          float s = 0.f;
+#pragma unroll 1
+          for (int e = 0; e < n; ++e) s = fmaf(to_f<T>(query[e]), to_f<T>(p[e]), s);
+          sum += (s * scale == -INF ? 0.f : 1.f) * v;
+        }
+      }
+    if (sum != 0.f) out[c] = from_f<O>(sum);
+  }
+}
+
+// The sum v of parts' sums and the next one, x, whose base is log2(f) below: an infinite one stays infinite, however small its
+// weights are beside the others'.
+__device__ __forceinline__ float join_sum(float x, float f, float v) { return fmaf(x, fabsf(x) == __builtin_inff() ? 1.f : f, v); }
+
 // The range of keys that a token at position `pos` of a sequence of `total` sees.
 __device__ __forceinline__ void sees(const mure_attn_attend_args& a, int pos, int total, int& lo, int& hi) {
   const int64_t w = a.window;

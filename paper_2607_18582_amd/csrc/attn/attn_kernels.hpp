@@ -251,12 +251,23 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, DB <= 
   if (row >= it.len) return;
   const Halves both(run.l);
   const float l = both.a + both.b;
+  bool lost = false;                           // sums of a row whose weights are numbers
+#pragma unroll
+  for (int x = 0; x < 16 * DB; ++x) lost |= run.o[x / 16][x % 16] != run.o[x / 16][x % 16];
+  lost &= l == l;
+  const auto again = [&](auto* to_row) {
+    if (__builtin_expect(lost, false))
+      renew<16 * DB>(to_row, src.k, src.v, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)row) * a.q.row_stride + (int64_t)h * a.head_dim, a.scale, a.head_dim,
+                     max(lo, from), 32, 32, max(lo, from), min(hi, to), lane, Running<DB>::channel);
+  };
   if (k.parts > 1) {
     const int64_t at_row = (((int64_t)m * k.n_items + i) * k.rows_each + row) * a.heads + h, slot = at_row * k.parts + part;
     store_row<float, DB>(k.ws_o + slot * a.head_dim, a.head_dim, run.o, 1.f, half);
     if (!half) k.ws_ml[2 * slot] = run.m, k.ws_ml[2 * slot + 1] = l;
+    again(k.ws_o + slot * a.head_dim);
   } else {
     store_row<T, DB>(out + row * a.out.row_stride, a.head_dim, run.o, 1.f / l, half);
+    again(out + row * a.out.row_stride);
   }
 }
 
@@ -297,6 +308,16 @@ template <typename T, int DB, int FAST> struct ShortWave {
   __device__ __forceinline__ ShortWave() {
 #pragma unroll
     for (int d = 0; d < 2 * DB; ++d) o[d] = v4f{};
+  }
+
+  static __device__ __forceinline__ int channel(int x, int lane) { return x / 4 * 16 + (lane >> 4) * 4 + x % 4; }
+
+  // Whether a sum of the lane's row is NaN although the row's weights are numbers.
+  __device__ __forceinline__ bool lost() const {
+    bool nan = false;
+#pragma unroll
+    for (int x = 0; x < 8 * DB; ++x) nan |= o[x / 4][x % 4] != o[x / 4][x % 4];
+    return nan && l == l;
   }
 
   // Of keys from ... to - 1 the tiles at `first`, `step` further and so on, of which the lane's row sees keys lo ... hi - 1 and
@@ -394,7 +415,6 @@ template <typename T, int DB, int FAST> struct ShortWave {
                 o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float*>(tile + (v ^ (d << 6)) + (16 * b + x) * H::ROW), s[b][x], o[d], 0, 0, 0);
       }
       if (apart) {
-        auto channel = [](int x, int lane) { return x / 4 * 16 + (lane >> 4) * 4 + x % 4; };
         auto add = [&](int x, float v) { o[x / 4][x % 4] += v; };
         add_nonfinite<8 * DB>(src.v, t, 0, min(see_from, there), n, row_lo, row_hi, lane, channel, add);
         add_nonfinite<8 * DB>(src.v, t, max(max(0, see_from), see_to), there, n, row_lo, row_hi, lane, channel, add);
@@ -424,13 +444,20 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
   sees(a, unit * 16 / group, src.total, from, all_hi);
   sees(a, (unit * 16 + u.rows - 1) / group, src.total, all_lo, to);
   ShortWave<T, DB, FAST> sw;
-  sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale,
-         from / S::KT * S::KT, S::KT, from, to, lo, hi, all_lo, all_hi, lds + wave * S::TILE, lane);
+  const auto query = [&](const Unit& u) { return static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim; };
+  sw.run(src, query(u), a.head_dim, a.scale, from / S::KT * S::KT, S::KT, from, to, lo, hi, all_lo, all_hi, lds + wave * S::TILE, lane);
   if ((lane & 15) >= u.rows) return;
   T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (it.row0 + (int64_t)u.token) * a.out.row_stride + (int64_t)u.head * a.head_dim;
   const float f = 1.f / sw.l;
 #pragma unroll
   for (int d = 0; d < 2 * DB; ++d) store4<T>(out, 16 * d + 4 * quarter, a.head_dim, sw.o[d][0] * f, sw.o[d][1] * f, sw.o[d][2] * f, sw.o[d][3] * f);
+  if (__builtin_expect(sw.lost(), false)) {
+    int l = lane, lo, hi;
+    asm volatile("" : "+v"(l));                // the row's numbers anew, out of registers until here
+    const Unit u(it, unit, group, g, l);
+    sees(a, u.token, src.total, lo, hi);
+    renew<8 * DB>(out, src.k, src.v, query(u), a.scale, a.head_dim, lo, S::KT, S::KT, lo, hi, l, sw.channel);
+  }
 }
 
 // Over a cache: a unit a block, the part's keys spread over its waves.
@@ -468,15 +495,21 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
   const int tile0 = from / S::KT, first = (tile0 + ((wave - tile0) & (S::WAVES - 1))) * S::KT;
   char* tile = lds + wave * S::EACH;
   ShortWave<T, DB, FAST> sw;
-  if (first < to)
-    sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale, first,
-           S::WAVES * S::KT, from, to, lo, hi, all_lo, all_hi, tile, lane);
+  const auto query = [&](const Unit& u) { return static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim; };
+  if (first < to) sw.run(src, query(u), a.head_dim, a.scale, first, S::WAVES * S::KT, from, to, lo, hi, all_lo, all_hi, tile, lane);
   // the waves' sums, added in order
   float* sums = reinterpret_cast<float*>(tile);
   float* ml = reinterpret_cast<float*>(lds + S::WAVES * S::EACH);              // [4][16][2]
 #pragma unroll
   for (int d = 0; d < 2 * DB; ++d) *reinterpret_cast<v4f*>(sums + (lane & 15) * S::PITCH + 16 * d + 4 * quarter) = sw.o[d];
   if (!quarter) ml[(wave * 16 + lane) * 2] = sw.top, ml[(wave * 16 + lane) * 2 + 1] = sw.l;
+  if (__builtin_expect(sw.lost(), false)) {
+    int l = lane, lo, hi;
+    asm volatile("" : "+v"(l));                // the row's numbers anew, out of registers until here
+    const Unit u(it, unit, group, g, l);
+    sees(a, src.past + u.token, src.total, lo, hi);
+    renew<8 * DB>(sums + (l & 15) * S::PITCH, src.k, src.v, query(u), a.scale, a.head_dim, first, S::WAVES * S::KT, S::KT, max(lo, from), min(hi, to), l, sw.channel);
+  }
   __syncthreads();
   for (int x = tid; x < u.rows * a.head_dim; x += 256) {
     const int y = x / a.head_dim, e = x - y * a.head_dim, all = unit * 16 + y, tk = all / group, hd = g * group + all % group;
@@ -489,7 +522,7 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
     for (int w = 0; w < S::WAVES; ++w) {
       const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + y) * 2] - base);
       size = fmaf(ml[(w * 16 + y) * 2 + 1], f, size);
-      v = fmaf(reinterpret_cast<const float*>(lds + w * S::EACH)[y * S::PITCH + e], f, v);
+      v = join_sum(reinterpret_cast<const float*>(lds + w * S::EACH)[y * S::PITCH + e], f, v);
     }
     if (k.parts > 1) {
       const int64_t slot = ((((int64_t)m * k.n_items + i) * k.rows_each + tk) * a.heads + hd) * k.parts + part;
@@ -533,7 +566,7 @@ template <typename T> __global__ __launch_bounds__(1024) void join_kernel(AttnAr
       l = fmaf(ml[2 * p + 1], f, l);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (lane + 64 * j < a.head_dim) v[j] = fmaf(o[(int64_t)p * a.head_dim + lane + 64 * j], f, v[j]);
+        if (lane + 64 * j < a.head_dim) v[j] = join_sum(o[(int64_t)p * a.head_dim + lane + 64 * j], f, v[j]);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) sums[slot][lane + 64 * j] = v[j];

@@ -319,7 +319,7 @@ template <typename T, int DB> struct Reader {
 };
 
 // Puts zeros in the place of what is infinite or NaN in keys from ... to - 1 of a tile, and says whether there was any.
-// A hidden key's weight is 0, which must not meet it; the rows that see the key get it by add_nonfinite.
+// A hidden key's weight is 0, which must not meet it; the rows that see the key get it by add_nonfinite, when all is summed.
 template <typename T, int DB> __device__ __forceinline__ bool clean(char* tile, int from, int to, int tid, int threads) {
   // exponents of ones carry into the sign's place
   constexpr uint32_t ONES = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u, CARRY = sizeof(T) == 4 ? 0x00800000u : 0x00800080u;
@@ -531,61 +531,104 @@ template <typename T, int DB> __device__ __forceinline__ void store_row(T* p, in
     for (int i = 0; i < 16; i += 4) store4<T>(p, 32 * d + 2 * i + 4 * half, n, o[d][i] * f, o[d][i + 1] * f, o[d][i + 2] * f, o[d][i + 3] * f);
 }
 
-// Adds what clean has taken out of keys from ... to - 1 of the tile at key t0 to the rows that see it: those keys lo ... hi - 1.
-// N registers of sums a lane, of channels channel(i).
-template <int N, typename T, typename F, typename S>
-__device__ __forceinline__ void add_nonfinite(const Rows<T>& rows, int t0, int from, int to, int n, int lo, int hi, int lane, F&& channel, S&& add) {
+// What is not finite, added to the stored sums of the wave's rows that see it (`row`: the lane has a row whose weights are
+// numbers; l: their sum).  Its weight counts for nothing but where it is 0, which makes NaN:
+//   - of the keys that some row of the block does not see, below mid_lo and from mid_hi on, whose values clean has taken out
+//     (`apart`: it has found any);
+//   - of all keys, where a sum is NaN: a weight that is 0 in float32 and not in the formula makes NaN of an infinite value
+//     there.  Without such a value the sum stays NaN: finite ones have passed float32.
+// A weight is 0 in the formula where the score is -inf: where the key is not finite (any other score that such a key has
+// would make the weights NaN), or in all of a row (l = 0).
+// The row sees keys lo ... hi - 1 of the tiles of `width` at `first`, `step` further and so on below `to`; N sums a lane, at
+// out[channel(i, lane)], four neighbours each.  For all lanes of the wave.
+template <int N, typename T, typename O, typename F>
+__device__ __forceinline__ void add_nonfinite(bool row, float l, bool apart, O* out, const Rows<T>& keys, const Rows<T>& values, int n, int first, int step, int width, int to, int lo,
+                                              int hi, int mid_lo, int mid_hi, int lane, F&& channel) {
+  constexpr float INF = __builtin_inff();
+  constexpr int EACH = 4;                      // keys whose values are on their way at a time
+  // f(first, end) for the tiles' keys from `least` on and below `most`: all, or those outside mid_lo ... mid_hi - 1
+  const auto spans = [&](bool all, int least, int most, auto&& f) {
 #pragma unroll 1
-  for (int key = from; key < to; ++key) {
-    asm("" : "+v"(lane));                      // nothing of this is kept in registers elsewhere
-    const T* p = rows.at(t0 + key);
-    const bool sees = key >= lo && key < hi;
+    for (int t = first; t < most; t += step)
+#pragma unroll 1
+      for (int side = 0; side < (all ? 1 : 2); ++side) {
+        const int from = max(max(t, least), side ? max(mid_lo, mid_hi) : 0), end = min(min(t + width, most), all || side ? most : mid_lo);
+        if (from < end && !f(from, end)) return;
+      }
+  };
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // the stores
+  bool infinite = false, renewed = false;
+#pragma unroll 1
+  for (int i = 0; i < N; i += 4) {
+    const int c = channel(i, lane);
+#pragma unroll 1
+    for (int all = 1; all >= 0; --all) {       // sums that are NaN by all keys, then the others by those apart
+      if (!row || !(all || apart)) continue;
+      float y[4], sum[4] = {};
+      bool mine[4], any = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float v = to_f<T>(p[min(channel(i, lane), n - 1)]);
-      add(i, sees && !(fabsf(v) < __builtin_inff()) ? v : 0.f);
+      for (int x = 0; x < 4; ++x) {
+        y[x] = c + x < n ? to_f<O>(out[c + x]) : 0.f;
+        mine[x] = c + x < n && (y[x] != y[x]) == (bool)all;
+        any |= mine[x];
+      }
+      if (!any) continue;
+      spans(all, lo, min(to, hi), [&](int from, int end) {
+#pragma unroll 1
+        for (int key = from; key < end; key += EACH)
+#pragma unroll
+          for (int j = 0; j < EACH; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const float v = to_f<T>(values.at(min(key + j, end - 1))[min(c + x, n - 1)]);
+              sum[x] += fabsf(v) < INF ? 0.f : v;                      // the last key twice is no other sum
+            }
+        bool open = false;                     // a sum that a further value may change
+#pragma unroll
+        for (int x = 0; x < 4; ++x) open |= mine[x] && sum[x] == sum[x];
+        return open;
+      });
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (!mine[x] || sum[x] == 0.f) continue;
+        if (l == 0.f) sum[x] *= 0.f;
+        out[c + x] = from_f<O>(all ? sum[x] : y[x] + sum[x]);
+        infinite |= sum[x] == sum[x];
+        renewed |= all;
+      }
     }
   }
-}
-
-// Stored sums of a row that are NaN although its weights are numbers, taken again: a weight that is 0 in float32 and not in
-// the formula makes NaN of an infinite value.  What is not finite counts by itself here, whatever its weight is (0 only
-// where the score is -inf); without such a value the sum stays NaN: finite ones have passed float32.  Keys lo ... hi - 1 of
-// the tiles of `width` at `first`, `step` further and so on; N sums a lane, at out[channel(i, lane)].
-template <int N, typename T, typename O, typename F>
-__device__ __forceinline__ void renew(O* out, const Rows<T>& keys, const Rows<T>& values, const T* query, float scale, int n, int first, int step, int width, int lo, int hi, int lane,
-                                      F&& channel) {
-  constexpr float INF = __builtin_inff();
-  constexpr int EACH = 8;                      // values on their way at a time
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // the stores
+  if (!__any(infinite)) return;
+  // 0 times infinity: keys that are not finite
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  spans(__any(renewed), 0, to, [&](int from, int end) {
 #pragma unroll 1
-  for (int i = 0; i < N; ++i) {
-    const int c = channel(i, lane);
-    if (c >= n) continue;
-    const float y = to_f<O>(out[c]);
-    if (y == y) continue;
-    float sum = 0.f;
+    for (int key0 = from; key0 < end; key0 += 64) {
+      // exponents of ones carry into the sign's place
+      constexpr uint32_t ONES = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u, CARRY = sizeof(T) == 4 ? 0x00800000u : 0x00800080u;
+      uint32_t any = 0;
+      if (key0 + lane < end) {
+        const T* p = keys.at(key0 + lane);
 #pragma unroll 1
-    for (int t = first; t < hi && sum == sum; t += step)
-#pragma unroll 1
-      for (int key0 = max(t, lo), end = min(t + width, hi); key0 < end && sum == sum; key0 += EACH) {
-        bool here = false;
+        for (int e = 0; e < n; e += 16 / (int)sizeof(T)) {
+          const v4u w = load_piece<T>(p, e, n);
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) here |= !(fabsf(to_f<T>(values.at(min(key0 + j, end - 1))[c])) < INF);
-        if (!here) continue;
-#pragma unroll 1
-        for (int key = key0; key < min(key0 + EACH, end); ++key) {
-          const float v = to_f<T>(values.at(key)[c]);
-          if (fabsf(v) < INF) continue;
-          const T* p = keys.at(key);
-          float s = 0.f;
-#pragma unroll 1
-          for (int e = 0; e < n; ++e) s = fmaf(to_f<T>(query[e]), to_f<T>(p[e]), s);
-          sum += (s * scale == -INF ? 0.f : 1.f) * v;
+          for (int i = 0; i < 4; ++i) any |= (w[i] & ONES) + CARRY;
         }
       }
-    if (sum != 0.f) out[c] = from_f<O>(sum);
-  }
+#pragma unroll 1
+      for (uint64_t bad = __ballot((any & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)) != 0); bad; bad &= bad - 1) {
+        const int key = key0 + __builtin_ctzll(bad);
+        if (!infinite || key < lo || key >= hi) continue;
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) {
+          const int c = channel(i, lane);
+          if (c < n && !(fabsf(to_f<T>(values.at(key)[c])) < INF)) out[c] = from_f<O>(__builtin_nanf(""));
+        }
+      }
+    }
+    return true;
+  });
 }
 
 // The sum v of parts' sums and the next one, x, whose base is log2(f) below: an infinite one stays infinite, however small its

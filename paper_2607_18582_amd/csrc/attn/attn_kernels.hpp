@@ -168,17 +168,14 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, DB <= 
     const int t = t0 + i * KT;
     return max(block_lo, from) > t || min(block_hi, to) < min(t + KT, src.total);
   };
-  // Values of tile i that are not finite in places hidden from some row are put aside; its other rows get them here.
+  // Values of tile i that are not finite in places hidden from some row are put aside; its other rows get them at the end.
+  int found = 0;
   const auto put_aside = [&](int i) {
     if (!aside(i)) return;
     const int t = t0 + i * KT, see_from = max(block_lo, from) - t, see_to = min(block_hi, to) - t, there = min(KT, src.total - t);
     char* tile = v_tile(i);
     const bool before = clean<T, DB>(tile, 0, min(see_from, there), tid, 256), behind = clean<T, DB>(tile, max(0, see_to), there, tid, 256);
-    if (!__syncthreads_or(before || behind) || begin >= end) return;
-    auto add = [&](int x, float v) { run.o[x / 16][x % 16] += v; };
-    const int row_lo = max(lo, from) - t, row_hi = min(hi, to) - t;
-    add_nonfinite<16 * DB>(src.v, t, 0, min(see_from, there), a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
-    add_nonfinite<16 * DB>(src.v, t, max(max(0, see_from), see_to), there, a.head_dim, row_lo, row_hi, lane, Running<DB>::channel, add);
+    found |= __syncthreads_or(before || behind);
   };
   load_k(0);
   if (KB == 2) load_v(0);
@@ -248,26 +245,28 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, DB <= 
     put_aside(tiles - 1);
     if (seen(tiles - 1)) run.template add<T>(read, v_tile(tiles - 1), 0, w[0]);
   }
-  if (row >= it.len) return;
+  if (wave * 32 >= it.len) return;
   const Halves both(run.l);
   const float l = both.a + both.b;
-  bool lost = false;                           // sums of a row whose weights are numbers
+  bool lost = false;                           // a sum is NaN
 #pragma unroll
   for (int x = 0; x < 16 * DB; ++x) lost |= run.o[x / 16][x % 16] != run.o[x / 16][x % 16];
-  lost &= l == l;
-  const auto again = [&](auto* to_row) {
-    if (__builtin_expect(lost, false))
-      renew<16 * DB>(to_row, src.k, src.v, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)row) * a.q.row_stride + (int64_t)h * a.head_dim, a.scale, a.head_dim,
-                     max(lo, from), 32, 32, max(lo, from), min(hi, to), lane, Running<DB>::channel);
+  const bool numbers = row < it.len && l == l;
+  const auto rest = [&](auto* to_row) {
+    if (__builtin_expect(found || __any(lost && numbers), false))
+      add_nonfinite<16 * DB>(numbers, l, found, to_row, src.k, src.v, a.head_dim, max(any_lo, from), 64, 64, min(any_hi, to), lo, hi, max(block_lo, from), min(block_hi, to), lane,
+                             Running<DB>::channel);
   };
   if (k.parts > 1) {
     const int64_t at_row = (((int64_t)m * k.n_items + i) * k.rows_each + row) * a.heads + h, slot = at_row * k.parts + part;
-    store_row<float, DB>(k.ws_o + slot * a.head_dim, a.head_dim, run.o, 1.f, half);
-    if (!half) k.ws_ml[2 * slot] = run.m, k.ws_ml[2 * slot + 1] = l;
-    again(k.ws_o + slot * a.head_dim);
+    if (row < it.len) {
+      store_row<float, DB>(k.ws_o + slot * a.head_dim, a.head_dim, run.o, 1.f, half);
+      if (!half) k.ws_ml[2 * slot] = run.m, k.ws_ml[2 * slot + 1] = l;
+    }
+    rest(k.ws_o + slot * a.head_dim);
   } else {
-    store_row<T, DB>(out + row * a.out.row_stride, a.head_dim, run.o, 1.f / l, half);
-    again(out + row * a.out.row_stride);
+    if (row < it.len) store_row<T, DB>(out + row * a.out.row_stride, a.head_dim, run.o, 1.f / l, half);
+    rest(out + row * a.out.row_stride);
   }
 }
 
@@ -304,6 +303,7 @@ template <typename T, int DB, int FAST> struct ShortWave {
   static constexpr int STEPS = H::BYTES / 64, E = 16 / (int)sizeof(T);
   v4f o[2 * DB];
   float top = -__builtin_inff(), l = 0.f;
+  bool apart = false;                          // values that are not finite were taken out of some tile
 
   __device__ __forceinline__ ShortWave() {
 #pragma unroll
@@ -312,12 +312,12 @@ template <typename T, int DB, int FAST> struct ShortWave {
 
   static __device__ __forceinline__ int channel(int x, int lane) { return x / 4 * 16 + (lane >> 4) * 4 + x % 4; }
 
-  // Whether a sum of the lane's row is NaN although the row's weights are numbers.
-  __device__ __forceinline__ bool lost() const {
+  // Whether add_nonfinite has something to do: for rows whose weights are numbers.
+  __device__ __forceinline__ bool rest(bool numbers) const {
     bool nan = false;
 #pragma unroll
     for (int x = 0; x < 8 * DB; ++x) nan |= o[x / 4][x % 4] != o[x / 4][x % 4];
-    return nan && l == l;
+    return apart || __any(nan && numbers);
   }
 
   // Of keys from ... to - 1 the tiles at `first`, `step` further and so on, of which the lane's row sees keys lo ... hi - 1 and
@@ -383,10 +383,9 @@ template <typename T, int DB, int FAST> struct ShortWave {
       if constexpr (FAST == WORDS) Copy<T, DB, S::KT, 1, VALUES16>::trim(tile, n, 0, lane);
       settle();
       const int see_from = max(all_lo, from) - t, see_to = min(all_hi, to) - t, there = min(S::KT, src.total - t);
-      bool apart = false;
       if (see_from > 0 || see_to < there) {
         const bool before = clean<T, DB>(tile, 0, min(see_from, there), lane, 64), behind = clean<T, DB>(tile, max(0, see_to), there, lane, 64);
-        apart = __any(before || behind);
+        apart |= __any(before || behind);
         settle();
       }
       if constexpr (sizeof(T) == 2) {
@@ -414,11 +413,6 @@ template <typename T, int DB, int FAST> struct ShortWave {
               for (int d = 0; d < 2 * DB; ++d)
                 o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(*reinterpret_cast<const float*>(tile + (v ^ (d << 6)) + (16 * b + x) * H::ROW), s[b][x], o[d], 0, 0, 0);
       }
-      if (apart) {
-        auto add = [&](int x, float v) { o[x / 4][x % 4] += v; };
-        add_nonfinite<8 * DB>(src.v, t, 0, min(see_from, there), n, row_lo, row_hi, lane, channel, add);
-        add_nonfinite<8 * DB>(src.v, t, max(max(0, see_from), see_to), there, n, row_lo, row_hi, lane, channel, add);
-      }
       settle();
     }
     l += __shfl_xor(l, 16);
@@ -444,19 +438,22 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
   sees(a, unit * 16 / group, src.total, from, all_hi);
   sees(a, (unit * 16 + u.rows - 1) / group, src.total, all_lo, to);
   ShortWave<T, DB, FAST> sw;
-  const auto query = [&](const Unit& u) { return static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim; };
-  sw.run(src, query(u), a.head_dim, a.scale, from / S::KT * S::KT, S::KT, from, to, lo, hi, all_lo, all_hi, lds + wave * S::TILE, lane);
-  if ((lane & 15) >= u.rows) return;
+  sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale,
+         from / S::KT * S::KT, S::KT, from, to, lo, hi, all_lo, all_hi, lds + wave * S::TILE, lane);
   T* out = static_cast<T*>(a.out.p) + m * a.out.mutant_stride + (it.row0 + (int64_t)u.token) * a.out.row_stride + (int64_t)u.head * a.head_dim;
-  const float f = 1.f / sw.l;
+  const bool there = (lane & 15) < u.rows;
+  if (there) {
+    const float f = 1.f / sw.l;
 #pragma unroll
-  for (int d = 0; d < 2 * DB; ++d) store4<T>(out, 16 * d + 4 * quarter, a.head_dim, sw.o[d][0] * f, sw.o[d][1] * f, sw.o[d][2] * f, sw.o[d][3] * f);
-  if (__builtin_expect(sw.lost(), false)) {
+    for (int d = 0; d < 2 * DB; ++d) store4<T>(out, 16 * d + 4 * quarter, a.head_dim, sw.o[d][0] * f, sw.o[d][1] * f, sw.o[d][2] * f, sw.o[d][3] * f);
+  }
+  const bool numbers = there && sw.l == sw.l;
+  if (__builtin_expect(sw.rest(numbers), false)) {
     int l = lane, lo, hi;
     asm volatile("" : "+v"(l));                // the row's numbers anew, out of registers until here
     const Unit u(it, unit, group, g, l);
     sees(a, u.token, src.total, lo, hi);
-    renew<8 * DB>(out, src.k, src.v, query(u), a.scale, a.head_dim, lo, S::KT, S::KT, lo, hi, l, sw.channel);
+    add_nonfinite<8 * DB>(numbers, sw.l, sw.apart, out, src.k, src.v, a.head_dim, from, 64, 64, to, lo, hi, all_lo, all_hi, l, sw.channel);
   }
 }
 
@@ -495,20 +492,23 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, (Short
   const int tile0 = from / S::KT, first = (tile0 + ((wave - tile0) & (S::WAVES - 1))) * S::KT;
   char* tile = lds + wave * S::EACH;
   ShortWave<T, DB, FAST> sw;
-  const auto query = [&](const Unit& u) { return static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim; };
-  if (first < to) sw.run(src, query(u), a.head_dim, a.scale, first, S::WAVES * S::KT, from, to, lo, hi, all_lo, all_hi, tile, lane);
+  if (first < to)
+    sw.run(src, static_cast<const T*>(a.q.p) + m * a.q.mutant_stride + (it.row0 + (int64_t)u.token) * a.q.row_stride + (int64_t)u.head * a.head_dim, a.head_dim, a.scale, first,
+           S::WAVES * S::KT, from, to, lo, hi, all_lo, all_hi, tile, lane);
   // the waves' sums, added in order
   float* sums = reinterpret_cast<float*>(tile);
   float* ml = reinterpret_cast<float*>(lds + S::WAVES * S::EACH);              // [4][16][2]
 #pragma unroll
   for (int d = 0; d < 2 * DB; ++d) *reinterpret_cast<v4f*>(sums + (lane & 15) * S::PITCH + 16 * d + 4 * quarter) = sw.o[d];
   if (!quarter) ml[(wave * 16 + lane) * 2] = sw.top, ml[(wave * 16 + lane) * 2 + 1] = sw.l;
-  if (__builtin_expect(sw.lost(), false)) {
+  const bool numbers = sw.l == sw.l;
+  if (__builtin_expect(sw.rest(numbers), false)) {
     int l = lane, lo, hi;
     asm volatile("" : "+v"(l));                // the row's numbers anew, out of registers until here
     const Unit u(it, unit, group, g, l);
     sees(a, src.past + u.token, src.total, lo, hi);
-    renew<8 * DB>(sums + (l & 15) * S::PITCH, src.k, src.v, query(u), a.scale, a.head_dim, first, S::WAVES * S::KT, S::KT, max(lo, from), min(hi, to), l, sw.channel);
+    add_nonfinite<8 * DB>(numbers, sw.l, sw.apart, sums + (l & 15) * S::PITCH, src.k, src.v, a.head_dim, first, S::WAVES * S::KT, S::KT, to, max(lo, from), hi, all_lo, all_hi, l,
+                          sw.channel);
   }
   __syncthreads();
   for (int x = tid; x < u.rows * a.head_dim; x += 256) {

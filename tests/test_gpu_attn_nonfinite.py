@@ -6,7 +6,7 @@ import torch
 
 import attn_reference as R
 from paper_2607_18582_amd import Mure
-from test_gpu_attn import TYPES, cuda, held, normal, say
+from test_gpu_attn import TYPES, cuda, normal, say
 
 pytestmark = pytest.mark.gpu
 
@@ -35,18 +35,21 @@ def steep(seed, count, past, dim, dtype, peaks):
     return q, k, normal(g, 1, total, dim, dtype=dtype)
 
 
-def check(mure, q, k, v, count, past, dim, what, scale=1.0, **how):
-    if past is None:
-        out = mure.sequences([count]).attend(*cuda(q, k, v), head_dim=dim, scale=scale, **how)
-        expected = R.attend(q, k, v, [count], dim, scale=scale, **how)[0]
-    else:
-        cache = held(9, 1, past + count + 3, dim, q.dtype)
-        for c, t in zip(cache, (k, v)):
-            c[0, 0, :past] = t[0, :past]
-            c[0, 0, past:] = NAN
-        p = torch.tensor([past], dtype=torch.int32)
-        out = mure.sequences([count]).attend(*cuda(q, k[:, past:], v[:, past:]), head_dim=dim, scale=scale, cache=cuda(*cache), past=p.cuda(), **how)
-        expected = R.attend(q, k[:, past:], v[:, past:], [count], dim, scale=scale, cache=cache, past=p, **how)[0]
+def check(mure, q, k, v, count, past, dim, what, bound_from=None, **how):
+    """bound_from: keys and values whose results have the bounds that are meant."""
+    at = past or 0
+    cache, p = None, None
+    if past is not None:
+        cache, p = [], torch.tensor([past], dtype=torch.int32)
+        for t in (k, v):
+            cache.append(torch.full((1, 1, past + count + 3, dim), NAN, dtype=q.dtype))
+            cache[-1][0, 0, :past] = t[0, :past]
+    expected = R.attend(q, k[:, at:], v[:, at:], [count], dim, scale=1.0, cache=cache, past=p, **how)[0]
+    if bound_from:
+        held = None if past is None else [t[:, None].clone() for t in bound_from]
+        bound = R.attend(q, *(t[:, at:] for t in bound_from), [count], dim, scale=1.0, cache=held, past=p, **how)[0][1]
+        expected = expected[0], bound
+    out = mure.sequences([count]).attend(*cuda(q, k[:, at:], v[:, at:]), head_dim=dim, scale=1.0, cache=cache and cuda(*cache), past=cuda(p)[0], **how)
     R.close(out, expected, what)
 
 
@@ -70,3 +73,18 @@ def test_infinite_values_of_small_weight(mure, dtype, count, past, dim, how):
         v[0, total // 5, dim - 2], v[0, total - 1 - total // 5, dim - 2] = INF, -INF
         check(mure, q, k, v, count, past, dim, f"peak at {peak}", **how)
 
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("count,past", SHAPES)
+@pytest.mark.parametrize("dim,how", [(64, {}), (66, {"causal": False}), (128, {"window": 40}), (200, {})])
+def test_infinite_values_of_no_weight(mure, dtype, count, past, dim, how):
+    """A score of -inf is a weight of 0: a finite value counts for nothing, and 0 times infinity is NaN."""
+    say(f"[no weight, inf] {dtype} {count} {past} dim={dim} {how}")
+    total = (past or 0) + count
+    q, k, v = steep(80, count, past, dim, TYPES[dtype], {total // 3: 192})
+    plain = k.clone(), v.clone()               # the same finite results, by weights of e^-480
+    for c, j in enumerate(places(total)):
+        if c % 2 and j != total // 3:
+            k[0, j, 0], plain[0][0, j, 0], plain[1][0, j] = -INF, -30, 0
+        v[0, j, c] = INF
+    check(mure, q, k, v, count, past, dim, "values beside keys of -inf", plain, **how)

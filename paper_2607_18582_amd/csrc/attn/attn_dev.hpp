@@ -379,9 +379,6 @@ struct Halves {
   }
 };
 
-// The factor of sums whose base rises by -d: never 0, so that an infinite sum stays infinite.
-__device__ __forceinline__ float shrink(float d) { return fmaxf(__builtin_amdgcn_exp2f(d), 0x1p-126f); }
-
 // The running softmax of a wave's rows: exponents of 2, their base and the sum of the lane's half of the keys' weights.
 template <int DB> struct Running {
   v16f o[DB];
@@ -404,7 +401,7 @@ template <int DB> struct Running {
     const Halves both(top);
     top = fmaxf(both.a, both.b) * c;
     const bool grows = top > m + 8.f;
-    old = grows ? shrink(m - top) : 1.f;
+    old = grows ? __builtin_amdgcn_exp2f(m - top) : 1.f;       // 0 of an infinite sum is NaN, which add_nonfinite mends
     m = grows ? top : m;
     l *= old;
     return grows;

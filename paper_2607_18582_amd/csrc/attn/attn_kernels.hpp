@@ -365,7 +365,7 @@ template <typename T, int DB, int FAST> struct ShortWave {
       most = fmaxf(most, __shfl_xor(most, 32)) * c;
       const bool grows = most > top + 8.f;
       if (__any(grows)) {
-        const float old = grows ? shrink(top - most) : 1.f;
+        const float old = grows ? __builtin_amdgcn_exp2f(top - most) : 1.f;    // 0 of an infinite sum is NaN, which add_nonfinite mends
         top = grows ? most : top;
         l *= old;
 #pragma unroll

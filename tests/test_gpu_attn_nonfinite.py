@@ -88,3 +88,18 @@ def test_infinite_values_of_no_weight(mure, dtype, count, past, dim, how):
             k[0, j, 0], plain[0][0, j, 0], plain[1][0, j] = -INF, -30, 0
         v[0, j, c] = INF
     check(mure, q, k, v, count, past, dim, "values beside keys of -inf", plain, **how)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("count,past", SHAPES)
+@pytest.mark.parametrize("dim", [64, 200])
+def test_huge_values_of_small_weight(mure, dtype, count, past, dim):
+    """1e38 times e^-200 and less is nothing beside the peak's own values."""
+    say(f"[small weights, huge] {dtype} {count} {past} dim={dim}")
+    total = (past or 0) + count
+    for n, peak in enumerate((total - 1, total // 2, min(40, total - 1))):
+        q, k, v = steep(70 + n, count, past, dim, TYPES[dtype], {peak: 400})
+        for c, j in enumerate(places(total)):
+            if j != peak:
+                v[0, j, c % dim] = (1e38, -1e38)[c % 2]
+        check(mure, q, k, v, count, past, dim, f"peak at {peak}")

@@ -172,8 +172,11 @@ void attend(mure_seq* s, const mure_attn_attend_args* args) {
   if (a.capacity > MURE_ATTN_MAX_ROWS) throw Fail{MURE_E_UNSUPPORTED, "too many rows of a cache: 2^30 at most"};
   check_device(s->device);
   if (T == 0) return;
+  if (T == 1) a.k.row_stride = a.v.row_stride = W;             // one row has no stride
+  // A copied tile's buffer ends with its last row, and what lies behind a row reads as zeros: rows that begin inside the one
+  // before them go element by element.
   const auto reads = [&](int64_t bytes) {
-    return D * es % bytes == 0 && aligned(bytes, a.k.p, es, {a.k.row_stride, a.k.mutant_stride}) && aligned(bytes, a.v.p, es, {a.v.row_stride, a.v.mutant_stride}) &&
+    return D * es % bytes == 0 && a.k.row_stride >= D && a.v.row_stride >= D && aligned(bytes, a.k.p, es, {a.k.row_stride, a.k.mutant_stride}) && aligned(bytes, a.v.p, es, {a.v.row_stride, a.v.mutant_stride}) &&
            (!held || (aligned(bytes, a.k_cache.p, es, {a.k_cache.row_stride, a.k_cache.seq_stride, a.k_cache.mutant_stride}) &&
                       aligned(bytes, a.v_cache.p, es, {a.v_cache.row_stride, a.v_cache.seq_stride, a.v_cache.mutant_stride})));
   };

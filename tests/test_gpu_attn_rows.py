@@ -1,0 +1,47 @@
+"""Attention where rows of keys and values share memory."""
+import pytest
+import torch
+
+from paper_2607_18582_amd import Mure
+from test_gpu_attn import TYPES, cuda, held, normal, qkv, say
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mure():
+    m = Mure(device=0)
+    yield m
+    m.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 66, 128])
+@pytest.mark.parametrize("lengths,past", [([40, 1], None), ([300, 129], None), ([3, 1], [700, 20]), ([40, 20], [1100, 3]), ([600], [90])])
+def test_rows_that_share_memory(mure, dtype, dim, lengths, past):
+    """Keys and values whose rows are one row, or lie over each other by all but one piece: as copies of them."""
+    say(f"[shared rows] {dtype} dim={dim} {lengths} {past}")
+    dt, T, inf = TYPES[dtype], sum(lengths), float("inf")
+    seqs = mure.sequences(lengths)
+    g = torch.Generator().manual_seed(23)
+    q = normal(g, T, 2 * dim, dtype=dt).cuda()
+    p = None if past is None else torch.tensor(past, dtype=torch.int32).cuda()
+    for step in (0, 16 // q.element_size(), 4 // q.element_size()):
+        k, v = (normal(g, T * step + dim, dtype=dt).cuda().as_strided((T, dim), (step, 1)) for _ in range(2))
+        v[T // 2, 7] = inf
+        if step:
+            v[T - 1, dim - 2] = inf
+        made = [None if past is None else cuda(*(c[0] for c in held(24, len(lengths), max(past) + 610, dim, dt))) for _ in range(2)]
+        got = seqs.attend(q, k, v, head_dim=dim, cache=made[0], past=p)
+        expected = seqs.attend(q, k.contiguous(), v.contiguous(), head_dim=dim, cache=made[1], past=p)
+        assert not expected.isnan().any()
+        assert torch.equal(got, expected), step
+
+
+def test_one_token_of_any_row_stride(mure):
+    say("[one row]")
+    dim = 64
+    q, k, v = cuda(*qkv(25, [1], 2, 1, dim, torch.bfloat16))
+    v[0, 0, 3] = float("inf")
+    got = mure.sequences([1]).attend(q[0], k[0].as_strided((1, dim), (0, 1)), v[0].as_strided((1, dim), (0, 1)), head_dim=dim)
+    assert torch.equal(got, torch.cat((v[0], v[0]), 1))

@@ -252,8 +252,8 @@ template <typename T, int STEPS, int W> __device__ __forceinline__ void load_que
   }
 }
 
-// The factor of the scores, for exponents of 2.
-__device__ __forceinline__ float factor(float scale) { return (scale == 0.f ? 1.f : fabsf(scale)) * 1.44269504088896340736f; }
+// The factor of the scores, for exponents of 2: finite, so that scores of 0 stay 0.
+__device__ __forceinline__ float factor(float scale) { return fminf((scale == 0.f ? 1.f : fabsf(scale)) * 1.44269504088896340736f, 3.402823466e38f); }
 
 template <typename T> __device__ __forceinline__ v16f mma_piece(v4u a, v4u b, v16f c) {
   if constexpr (sizeof(T) == 2) return Mma<T>::mma(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c);

@@ -1,4 +1,5 @@
-"""Attention where rows of keys and values share memory."""
+"""Attention where rows of keys and values share memory, and at the largest
+scales."""
 import pytest
 import torch
 
@@ -45,3 +46,12 @@ def test_one_token_of_any_row_stride(mure):
     v[0, 0, 3] = float("inf")
     got = mure.sequences([1]).attend(q[0], k[0].as_strided((1, dim), (0, 1)), v[0].as_strided((1, dim), (0, 1)), head_dim=dim)
     assert torch.equal(got, torch.cat((v[0], v[0]), 1))
+
+
+def test_queries_of_nothing_at_the_largest_scale(mure):
+    """Scores of 0 stay 0 at scales whose product with log2(e) passes float32."""
+    say("[largest scale]")
+    for lengths in ([20], [200]):
+        q, k, v = cuda(*qkv(26, lengths, 2, 1, 32, torch.float32))
+        out = mure.sequences(lengths).attend(q * 0, k, v, head_dim=32, scale=3.4e38)
+        assert torch.equal(out, mure.sequences(lengths).attend(q * 0, k, v, head_dim=32, scale=1.0))

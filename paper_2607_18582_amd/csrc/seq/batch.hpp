@@ -146,24 +146,41 @@ inline void check_output(const Span& s) {
   if (!rows_inside && !muts_inside) invalid(std::string(s.name) + ": its rows overlap");
 }
 
-// Whether two tensors may share memory.  Rows side by side in one buffer (at
-// different columns, whichever axis goes around which) do not.
+// Whether two tensors may share memory.  Blocks side by side in one buffer (rows at different columns, caches as an axis of
+// one tensor, whichever axis goes around which) do not.
 inline bool meet(const Span& a, const Span& b) {
   if (a.extent() == 0 || b.extent() == 0) return false;
   const wide pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
   if (pa + a.extent() <= pb || pb + b.extent() <= pa) return false;
-  // What divides all strides of both, in bytes: each has its elements in the same columns of every piece of that many.
-  wide q = 0;
-  for (const Span* s : {&a, &b})
-    for (const int64_t stride : {s->row_stride, s->outer_stride, s->mutant_stride})
-      for (wide x = (wide)stride * s->esize; x;) {
-        const wide rest = q % x;
-        q = x;
-        x = rest;
+  struct Axis { wide stride, n; };
+  const Axis axes[2][3] = {{{a.row_stride, a.rows}, {a.outer_stride, a.outers}, {a.mutant_stride, a.mutants}},
+                           {{b.row_stride, b.rows}, {b.outer_stride, b.outers}, {b.mutant_stride, b.mutants}}};
+  const Span* const spans[2] = {&a, &b};
+  // With any stride as the border: the axes of smaller ones make a block, and what divides the others, in bytes, is the
+  // length of pieces in each of which a tensor has its blocks in the same place.
+  for (int which = 0; which < 6; ++which) {
+    const wide border = axes[which / 3][which % 3].stride * spans[which / 3]->esize;
+    if (border == 0) continue;
+    wide q = 0, block[2];
+    for (int s = 0; s < 2; ++s) {
+      block[s] = (wide)spans[s]->width * spans[s]->esize;
+      for (const Axis& x : axes[s]) {
+        wide stride = x.stride * spans[s]->esize;
+        if (stride < border) {
+          block[s] += (x.n - 1) * stride;
+          continue;
+        }
+        while (stride) {
+          const wide rest = q % stride;
+          q = stride;
+          stride = rest;
+        }
       }
-  if (q == 0 || (wide)a.width * a.esize > q || (wide)b.width * b.esize > q) return true;
-  const wide d = ((pb - pa) % q + q) % q;      // b's first column, as a's rows see it
-  return d < (wide)a.width * a.esize || d + (wide)b.width * b.esize > q;
+    }
+    const wide d = ((pb - pa) % q + q) % q;    // b's first block, as a's pieces see it
+    if (block[0] <= q && block[1] <= q && d >= block[0] && d + block[1] <= q) return false;
+  }
+  return true;
 }
 
 inline bool same(const Span& a, const Span& b) {

@@ -89,6 +89,10 @@ typedef struct {
  * What is NaN or infinite goes on by the arithmetic of the formula to those
  * tokens that see it, and to no other: an infinite value makes a token's result
  * infinite (or NaN, beside one of the other sign) however small its weight is.
+ * Over caches of more than 512 rows parts of the keys meet in the batch's
+ * workspace (mure_seq.h).  A call takes 1 GiB of it at most (more only where
+ * one head of one sequence needs it): where it would need more, it takes
+ * sequences, mutants or heads in rounds.
  * dtype: of q, k, v, the caches and out.  All mutants may share a cache
  * (mutant stride 0) where they share k and v too.  k_cache and v_cache overlap
  * no other tensor and no row of their own. */

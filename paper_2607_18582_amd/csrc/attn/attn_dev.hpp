@@ -18,7 +18,6 @@ namespace mure {
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef v4u __attribute__((aligned(2))) v4u_any;  // the GPU's global loads and stores take any address
 
@@ -343,7 +342,10 @@ template <typename T, int DB> __device__ __forceinline__ bool clean(char* tile, 
   return found;
 }
 
-// The weights of 32 keys, as operands of O^T.
+// The weights of 32 keys, as operands of O^T.  In bfloat16 each is rounded once, to half a step of 2^-8 of itself: in two
+// halves they would double the second product, half of the matrix instructions.  The sum below a result adds them
+// unrounded.  The measured cases' errors against float64 are 0.0020 to 0.0023 of the result's norm so, and 0.0016 from the
+// rounding of the results alone.
 template <typename T> struct Weights {
   static constexpr int N = 16 / Mma<T>::N;
   typename Mma<T>::frag p[N];

@@ -72,7 +72,13 @@ __device__ __forceinline__ int spread(int i, int n) { return n % 8 ? i : i % 8 *
 // half a maximum and a conversion per score).  Two waves on a SIMD overlap them by a fifth only, so a wave does it itself:
 // the softmax of one block goes between the products of the next and of the last one.  16384 tokens, 16 heads of 4, 128
 // bfloat16 channels, causal: 1.08 to 1.12 ms, about 1000 TFLOP/s, at which the chip lowers its clock to 1.7 GHz (one after the other,
-// with the same tiles: 1.20 ms).  A batch of prompts is bound by its longest run, 1.5 us a tile of 64 keys.
+// with the same tiles: 1.20 ms); on a card that is held to 1.6 GHz 1.23 to 1.27.  A batch of prompts is bound by its longest
+// run, 1.5 us a tile of 64 keys.
+//
+// Heads of more than 128 channels leave one wave a SIMD, and their sums fill the accumulation registers: 4096 tokens of the
+// same heads take 112 us with 128 channels, 294 with 192 and 409 with 256; in float32 809, 1184 and 4739, the last with 1.5 KB
+// of scratch a lane.  Rows of whole words (126 channels: 309 us) and of elements (127: 761) have about 0.6 KB of it up to
+// 128 bfloat16 channels.
 
 template <typename T, int DB> struct Run {
   using H = Head<T, DB>;
@@ -275,7 +281,7 @@ template <typename T, int DB, int FAST> __global__ __launch_bounds__(256, DB <= 
 // As above in 16x16 products: a lane has row l % 16 of the queries and of every 16 keys those numbered 4 (l / 16) + i.
 // Little is used twice here, so keys go straight into registers, values through a small tile of the wave's own, and
 // nobody waits for another wave: what counts is how many loads are on their way.  64 tokens over caches of 500 to 8000
-// rows, 16 heads of 4, 128 bfloat16 channels: 94 us, 4.6 TB/s (32 rows a wave, tiles in LDS: 160).
+// rows, 16 heads of 4, 128 bfloat16 channels: 91 to 95 us, 3.8 TB/s (32 rows a wave, tiles in LDS: 160).
 
 template <typename T, int DB> struct Short {
   using H = Head<T, DB>;

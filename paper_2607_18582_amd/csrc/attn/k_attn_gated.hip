@@ -279,7 +279,8 @@ template <typename T, int TM> __global__ __launch_bounds__(64 * SPLIT, 2) void g
 
 // ---- few rows: bound by the weights' bytes.  W waves have 16 rows of x each; NT = 8: the gate's 8 rows of weights and the
 // other projection's share an operand of 16, so that even few outputs make many blocks; NT = 16: an operand each, as 64
-// rows of x would be read too often otherwise.  All but one of the stages of 256 bytes of the summed axis are on their way.
+// rows of x would be read too often otherwise.  A block of one wave has all but one of the stages of 256 bytes of the summed
+// axis on their way; with more waves the barrier waits for all copies, so that it has those issued since the last one.
 // 64 rows, 2048 to 5632, bfloat16: 14 us, 3.3 TB/s.
 
 template <typename T, int W, int NT, int STAGES, bool FAST> __global__ __launch_bounds__(64 * W) void gated_few_kernel(mure_attn_gated_args a, int n_tiles, int m_tiles) {
@@ -413,7 +414,9 @@ template <typename T, int TM> hipError_t gated_split(const mure_attn_gated_args&
 
 constexpr int64_t CUS = 256;
 
-// Whether the last round of blocks, of which a compute unit works on one at a time, is nearly full.
+// Whether the last round of blocks is nearly full, counted as if a compute unit worked on one at a time.  Two and more of the
+// smaller tiles fit, so that a launch just past a round of either counts as worse than it is: 4 mutants' weights over 2724 shared
+// float32 rows, 2667 inputs to 175 outputs, 264 tiles of 128 rows or 516 of 64, take 332 us.
 bool fills(int64_t blocks) { return 6 * blocks >= 5 * ((blocks + CUS - 1) / CUS * CUS); }
 
 // Tiles of 128 rows by 64 outputs, in float32 of 64 rows where those leave the last round half empty: 2048 inputs to 1024

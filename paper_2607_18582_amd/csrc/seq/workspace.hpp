@@ -1,4 +1,4 @@
-// Device memory of a batch's scans of long sequences: the chunks' states.
+// Device memory of a batch's scans of long sequences, the chunks' states, and of attention over parts of keys.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -128,3 +128,36 @@ def test_more_blocks_than_a_launch(mure):
     for m in (0, 1, 77, M - 1):
         assert torch.equal(out[m], mure.sequences([1, 1, 1]).attend(q[m], k, v, head_dim=dim, cache=alone, past=past)), m
     assert all(torch.equal(c, a) for c, a in zip(cache, alone))
+
+
+def test_rounds_in_a_graph():
+    """Rounds over sequences and over heads, captured: every replay follows the pasts, beside direct calls."""
+    say("[rounds, graph]")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        mure = Mure(device=0)
+    g = torch.Generator(device="cuda").manual_seed(54)
+    for n, M, H, dim, rows in ((300, 64, 64, 2, 32768), (1, 2, 1024, 64, 300000)):
+        lengths = [1] * n if n > 1 else [16]
+        T = sum(lengths)
+        q = rand(g, M, T, H * dim, dtype=torch.bfloat16)
+        k, v = (rand(g, T, dim, dtype=torch.bfloat16) for _ in range(2))
+        cache = [rand(g, n, rows, dim, dtype=torch.bfloat16) for _ in range(2)]
+        start = (torch.arange(n, device="cuda") * 37 % 3000 + 100).to(torch.int32)
+        past, held, seqs = start.clone(), [c.clone() for c in cache], mure.sequences(lengths)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = seqs.attend(q, k, v, head_dim=dim, cache=cache, past=past)
+            past.add_(lengths[0])
+        for i in range(4):
+            graph.replay()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                expected = seqs.attend(q, k, v, head_dim=dim, cache=held, past=start + i * lengths[0])
+                side.synchronize()
+            assert torch.equal(out, expected), (n, i)
+            assert all(torch.equal(c, h) for c, h in zip(cache, held)), (n, i)
+    torch.cuda.synchronize()
+    del graph
+    mure.close()
